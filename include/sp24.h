@@ -436,6 +436,148 @@ sp24_status sp24_conv2d_dense_i8_scaled(const void* A, const void* X, void* D, i
                                         const float* w_scale, float x_scale, const float* bias, int relu,
                                         float inv_y_scale, sp24_dtype out, void* stream);
 
+/*
+ * ---------------------------------------------------------------------------
+ * The operators around the products in a transformer's feed-forward block: the
+ * norm in front, the product with its bias, activation and residual, tokens
+ * sorted to experts and back, and the gradients of each.  (Not part of the
+ * paper; the products are those of Sec. 3.2.)  Here every matrix has one row per
+ * token, ld* are row strides in elements, and pointers need the alignment of
+ * their element type only, unless said otherwise; vectors of floats and of
+ * 32-bit integers are contiguous.  Sums, statistics and every intermediate value
+ * are binary32; a result is rounded once, to nearest even.  The general
+ * conventions above hold: no allocation, no synchronisation, errors before any
+ * launch.  Buffers that a call writes may not overlap its others, except in place
+ * (the same address and row stride) where said.  Results are the same from call
+ * to call.
+ * ---------------------------------------------------------------------------
+ */
+
+/*
+ * h = X + residual (residual NULL: h = X);  rstd[n] = (mean_i h[n][i]^2 + eps)^(-1/2)
+ * Y[n][i] = h[n][i] * rstd[n] * weight[i]
+ * X, residual: N x H of type t (SP24_F16, SP24_BF16 or SP24_F32).  weight: H floats.
+ * hidden (may be NULL): receives h rounded to t; it may be X or residual in place
+ * (the residual stream's own buffer).  rstd (may be NULL): N floats.
+ * out = SP24_F32, SP24_F16, SP24_BF16, or an 8-bit type with one scale per row:
+ *   m = max(max_i |Y[n][i]|, 2^-100), scale[n] = m / 127 (SP24_I8) or m / 448 (SP24_F8),
+ *   code = Y[n][i] * (127 or 448) / m to the nearest code (ties to even).
+ * A NaN in a row makes its scale NaN (and, SP24_F8, the code).  Y may be X or residual in place when
+ * out == t.  scale: N floats, ignored unless out is an 8-bit type.  1 <= H <= 32768, eps >= 0 and finite, else SP24_ERR_SHAPE.
+ */
+sp24_status sp24_rmsnorm(const void* X, const void* residual, const float* weight, float eps, void* Y, float* scale,
+                         void* hidden, float* rstd, int64_t N, int64_t H, int64_t ldx, int64_t ldr, int64_t ldy, int64_t ldh,
+                         sp24_dtype t, sp24_dtype out, void* stream);
+
+/* The 8-bit rows alone: Q and scale as sp24_rmsnorm writes them for Y = X.  1 <= H <= 65536. */
+sp24_status sp24_quantize_rows(const void* X, void* Q, float* scale, int64_t N, int64_t H, int64_t ldx, int64_t ldq,
+                               sp24_dtype t, sp24_dtype out, void* stream);
+
+/*
+ * The gradients of sp24_rmsnorm (float results) from dY, the `hidden` and rstd that it wrote, and dhidden, the
+ * gradient that reaches hidden from elsewhere (NULL: none):
+ *   g = dY * weight;  dX = rstd * (g - h * rstd^2 * mean_i(g h)) + dhidden   (the residual's gradient is the same)
+ *   dweight[i] = sum_n dY[n][i] h[n][i] rstd[n]
+ * All matrices N x H of type t; dX may be dY, hidden or dhidden in place.  workspace: device, 16-byte aligned, at least
+ * sp24_rmsnorm_backward_workspace_bytes(N, H) bytes, else SP24_ERR_SHAPE.  N == 0 writes zeros to dweight.
+ */
+size_t sp24_rmsnorm_backward_workspace_bytes(int64_t N, int64_t H);
+sp24_status sp24_rmsnorm_backward(const void* dY, const void* hidden, const float* weight, const float* rstd,
+                                  const void* dhidden, void* dX, float* dweight, int64_t N, int64_t H, int64_t lddy, int64_t ldh,
+                                  int64_t lddh, int64_t lddx, sp24_dtype t, void* workspace, size_t workspace_bytes, void* stream);
+
+typedef enum {
+    SP24_ACT_NONE = 0,
+    SP24_ACT_RELU = 1, /* max(z, 0)                                                             */
+    SP24_ACT_GELU = 2, /* 0.5 z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))), the tanh form of GELU */
+    SP24_ACT_SILU = 3  /* z / (1 + exp(-z))                                                      */
+} sp24_act;
+
+/*
+ * A layer on the sparse product (Sec. 3.2, Fig. 2), one row per token in and out:
+ *   z[n][m] = (sum_k W[m][k] X[n][k]) * w_scale[m] * x_scale[n] + bias[m]      W = decompress(V, meta), M x K
+ *   Y[n][m] = act(z[n][m]) + residual[n][m]
+ * X: N x K of type in, Y N x M of type out = SP24_F32, SP24_F16 or SP24_BF16 for every input type.  w_scale (M floats),
+ * x_scale (N floats): 8-bit inputs only (else SP24_ERR_DTYPE); NULL means 1.  bias (M floats), residual (N x M of type out): NULL means none.
+ * Z (NULL or N x M of type out) receives z, which sp24_linear_backward takes.  Y may be residual in place.
+ * V, meta, layouts and K as for sp24_spmm; as there, a removed position takes no part in the sum whatever X holds.  Rows of X
+ * that are not 16-byte aligned, and a K of no whole 32 columns, take a slower kernel.
+ */
+sp24_status sp24_linear(const void* V, const void* meta, const void* X, void* Y, int64_t M, int64_t N, int64_t K, int64_t ldx,
+                        int64_t ldy, const float* w_scale, const float* x_scale, const float* bias, sp24_act act,
+                        const void* residual, int64_t ldr, void* Z, int64_t ldz, sp24_dtype in, sp24_dtype out,
+                        sp24_layout l, void* stream);
+
+/*
+ * What follows from the gradient of a layer's result:  dZ = dY * act'(Z),  dbias[m] = sum_n dZ[n][m].
+ * dY, Z, dZ: N x M of type t (SP24_F16 or SP24_BF16); Z may be NULL for SP24_ACT_NONE.  dZ (may be NULL) may be dY or Z in place.
+ * dZt (may be NULL): M x N, dZ transposed, the first operand of the weights' gradient: dW = sp24_gemm_dense(dZt, X as an N-major
+ * operand) and sp24_mask_apply; dX = sp24_linear of dZ with the compressed transpose of W.  dbias (may be NULL): M floats.
+ * With offsets (below; N a multiple of 16) dbias holds M floats for each of the experts, summed over its segment alone.
+ * workspace (dbias given): device, 16-byte aligned, sp24_linear_backward_workspace_bytes(M, N, offsets != NULL) bytes.
+ */
+size_t sp24_linear_backward_workspace_bytes(int64_t M, int64_t N, int grouped);
+sp24_status sp24_linear_backward(const void* dY, const void* Z, void* dZ, void* dZt, float* dbias, int64_t M, int64_t N,
+                                 int64_t lddy, int64_t ldz, int64_t lddz, int64_t lddzt, sp24_act act, const int32_t* offsets,
+                                 int experts, sp24_dtype t, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Tokens in order of their expert.  A choice i = n * topk + j of token n names an expert ids[i]; one outside 0 .. experts - 1
+ * has no row.  The rows of expert e are offsets[e] .. offsets[e+1] - 1 (experts + 1 entries): as many whole sixteens as its choices need, the choices in
+ * ascending order, then rows of no choice.
+ *   rows[r]:  the choice of row r, or -1 (row_count entries, at least sp24_moe_rows(choices, experts); all behind the last segment are -1)
+ *   slots[i]: the row of choice i, or -1
+ * experts <= SP24_MOST_EXPERTS.  workspace: sp24_moe_sort_workspace_bytes(choices, experts) bytes (0: may be NULL), 4-byte aligned.
+ */
+#define SP24_MOST_EXPERTS 1024
+int64_t sp24_moe_rows(int64_t choices, int experts);
+size_t sp24_moe_sort_workspace_bytes(int64_t choices, int experts);
+sp24_status sp24_moe_sort(const int32_t* ids, int32_t* offsets, int32_t* slots, int32_t* rows, int64_t choices, int experts,
+                          int64_t row_count, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Xs[r][:] = X[rows[r] / topk][:], bit for bit; zeros where rows[r] is -1 (or names no token).  X: N x H, Xs: row_count x H of type t (any but SP24_I32).
+ * scale (NULL: none), scale_out: the rows' scales alike, 0 for rows of no choice.  The gradient of X is sp24_moe_combine of Xs's with weights NULL.
+ */
+sp24_status sp24_moe_gather(const void* X, const float* scale, const int32_t* rows, void* Xs, float* scale_out, int64_t N,
+                            int64_t row_count, int topk, int64_t H, int64_t ldx, int64_t ldxs, sp24_dtype t, void* stream);
+
+/*
+ * out[n][:] = residual[n][:] + sum_j weights[n * topk + j] * Y[slots[n * topk + j]][:], j ascending; a slot of -1 (or past row_count) adds nothing.
+ * weights NULL: 1; residual NULL: 0.  Y: row_count x H, out and residual N x H, all of type t = SP24_F32, SP24_F16 or SP24_BF16.
+ * out may be residual in place.
+ */
+sp24_status sp24_moe_combine(const void* Y, const int32_t* slots, const float* weights, const void* residual, void* out, int64_t N,
+                             int64_t row_count, int topk, int64_t H, int64_t ldy, int64_t ldr, int64_t ldo, sp24_dtype t, void* stream);
+
+/*
+ * Its gradients: dY[r][:] = weights[i] * dOut[i / topk][:] for the choice i = rows[r], zeros for a row of none; dweights[i] = sum over the
+ * row of dOut[i / topk] * Y[slots[i]], 0 for a choice without a row.  (The residual's gradient is dOut.)  dY may be Y in place.
+ */
+sp24_status sp24_moe_combine_backward(const void* dOut, const void* Y, const int32_t* rows, const int32_t* slots, const float* weights,
+                                      void* dY, float* dweights, int64_t N, int64_t row_count, int topk, int64_t H, int64_t lddo,
+                                      int64_t ldy, int64_t lddy, sp24_dtype t, void* stream);
+
+/*
+ * sp24_linear for the rows of every expert with that expert's weights, in one launch.  V, meta: the experts' matrices one below the other, as
+ * sp24_compress leaves the (experts * M) x K matrix; w_scale, bias: experts * M floats.  offsets: device, experts + 1 entries in ascending order, multiples of 16, as
+ * sp24_moe_sort writes them (others give unspecified results, never an access out of range).  `rows` (a multiple of 16): of X, Y, Z and x_scale.
+ * Rows of Y and Z that belong to no expert are written zero.
+ */
+sp24_status sp24_linear_grouped(const void* V, const void* meta, const void* X, void* Y, const int32_t* offsets, int experts,
+                                int64_t M, int64_t rows, int64_t K, int64_t ldx, int64_t ldy, const float* w_scale,
+                                const float* x_scale, const float* bias, sp24_act act, void* Z, int64_t ldz, sp24_dtype in,
+                                sp24_dtype out, sp24_layout l, void* stream);
+
+/*
+ * The dense product over the rows of every segment, the gradient of the experts' weights: D_e = A[:, offsets[e] .. offsets[e+1] - 1] x
+ * B[offsets[e] .. offsets[e+1] - 1, :], M x N each, one below the other in D (row stride ldd).  A: M x rows, B: rows x N, of type SP24_F16 or
+ * SP24_BF16; D of the same type or SP24_F32.  An empty segment gives zeros.  Rows of A and B must be 16-byte aligned and N a multiple of 8;
+ * row strides below 2^21 elements, else SP24_ERR_SHAPE.  (Rows of no choice inside a segment take part: zeros in A or B there.)
+ */
+sp24_status sp24_gemm_dense_grouped(const void* A, const void* B, void* D, const int32_t* offsets, int experts, int64_t M, int64_t N,
+                                    int64_t rows, int64_t lda, int64_t ldb, int64_t ldd, sp24_dtype in, sp24_dtype out, void* stream);
+
 /* Static, NUL-terminated description of a status code. */
 const char* sp24_status_string(sp24_status s);
 

@@ -1,0 +1,344 @@
+// Tokens in order of their expert and back: the sort of the router's choices, the rows gathered, the weighted sum of what comes back, and
+// that sum's gradients.
+#include "launch.hpp"
+#include "rowops.hpp"
+
+namespace sp24 {
+
+// ---------------------------------------------------------------------------
+// The sort is a counting sort that keeps the order of equal keys: the number of choices of every expert before a wavefront's part, then the
+// place of each of its 64 at a time among the 64 (ballots over the bits of the expert's number).  Whole numbers throughout, so the
+// result is one.  Up to kSortPart choices one workgroup does all of it; more are cut into parts that count, a scan over parts and
+// experts, and parts that place.
+// ---------------------------------------------------------------------------
+constexpr int kSortWaves = 16, kSortExperts = 1024;
+
+struct SortLds {
+    int count[kSortWaves][kSortExperts];       // of a wavefront's part; then the next row it gives out
+    int scan[kSortWaves];
+};
+
+// lanes with the same key as this one, among those with `live`
+__device__ __forceinline__ uint64_t same_key(int key, bool live, int bits)
+{
+    uint64_t same = __ballot(live);
+    for (int b = 0; b < bits; ++b) {
+        const uint64_t set = __ballot((key >> b) & 1);
+        same &= (key >> b) & 1 ? set : ~set;
+    }
+    return same;
+}
+
+__device__ __forceinline__ int sort_bits(int experts) { return 32 - __clz(max(experts - 1, 1)); }
+
+// how many of ids[first .. last) each expert has, per wavefront; the wavefronts take equal runs of whole 64s
+__device__ __forceinline__ void sort_count(SortLds& s, const SortArgs& a, int64_t first, int64_t last)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int e = lane; e < a.experts; e += 64) s.count[wave][e] = 0;
+    const int64_t run = ((last - first + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
+    const int64_t from = min(first + wave * run, last), to = min(from + run, last);
+    for (int64_t i = from + lane; i < to; i += 64) {
+        const int e = a.ids[i];
+        if ((unsigned)e < (unsigned)a.experts) atomicAdd(&s.count[wave][e], 1);       // (a wavefront's own words, and sums of whole numbers)
+    }
+}
+
+// the rows of ids[first .. last), from the next rows in s.count on
+__device__ __forceinline__ void sort_place(SortLds& s, const SortArgs& a, int64_t first, int64_t last)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, bits = sort_bits(a.experts);
+    const int64_t run = ((last - first + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
+    const int64_t from = min(first + wave * run, last), to = min(from + run, last);
+    for (int64_t i0 = from; i0 < to; i0 += 64) {
+        const int64_t i = i0 + lane;
+        const int e = i < to ? a.ids[i] : -1;
+        const bool live = (unsigned)e < (unsigned)a.experts;
+        const uint64_t same = same_key(e, live, bits);
+        int row = -1;
+        if (live) {
+            row = s.count[wave][e] + __popcll(same & (((uint64_t)1 << lane) - 1));
+            a.rows[row] = (int32_t)i;
+        }
+        if (i < to) a.slots[i] = row;
+        if (live && __ffsll((unsigned long long)same) - 1 == lane) s.count[wave][e] += __popcll(same);
+    }
+}
+
+// Segments from the experts' totals (thread e holds that of expert e): whole sixteens one behind the other.  Returns the segment's first row;
+// *end: the end of the last.
+__device__ __forceinline__ int sort_segments(SortLds& s, int total, int* end)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int padded = (total + 15) & ~15;
+    int upto = padded;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int t = __shfl_up(upto, d);
+        if (lane >= d) upto += t;
+    }
+    if (lane == 63) s.scan[wave] = upto;
+    __syncthreads();
+    int before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+        if (w < wave) before += s.scan[w];
+        all += s.scan[w];
+    }
+    *end = all;
+    return before + upto - padded;
+}
+
+// offsets, and -1 in the rows that no choice has (thread e: those of expert e; all threads: those behind the last segment)
+__device__ __forceinline__ void sort_finish(const SortArgs& a, int first, int total, int end)
+{
+    const int e = threadIdx.x;
+    if (e < a.experts) {
+        a.offsets[e] = first;
+        for (int i = first + total; i < first + ((total + 15) & ~15); ++i) a.rows[i] = -1;
+    }
+    if (e == 0) a.offsets[a.experts] = end;
+    for (int64_t i = end + threadIdx.x; i < a.R; i += blockDim.x) a.rows[i] = -1;
+}
+
+__global__ __launch_bounds__(1024) void k_sort_one(SortArgs a)
+{
+    __shared__ SortLds s;
+    sort_count(s, a, 0, a.T);
+    __syncthreads();
+    const int e = threadIdx.x;
+    int total = 0;
+    if (e < a.experts)
+        for (int w = 0; w < kSortWaves; ++w) total += s.count[w][e];
+    int end;
+    const int first = sort_segments(s, total, &end);
+    if (e < a.experts) {
+        int next = first;
+        for (int w = 0; w < kSortWaves; ++w) {
+            const int n = s.count[w][e];
+            s.count[w][e] = next;
+            next += n;
+        }
+    }
+    sort_finish(a, first, total, end);
+    __syncthreads();
+    sort_place(s, a, 0, a.T);
+}
+
+__global__ __launch_bounds__(1024) void k_sort_count(SortArgs a)
+{
+    __shared__ SortLds s;
+    const int64_t first = (int64_t)blockIdx.x * kSortPart;
+    sort_count(s, a, first, min(first + kSortPart, a.T));
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.experts; e += blockDim.x) {
+        int total = 0;
+        for (int w = 0; w < kSortWaves; ++w) total += s.count[w][e];
+        a.workspace[(int64_t)blockIdx.x * a.experts + e] = total;
+    }
+}
+
+// counts of the parts -> the first row that each part gives out
+__global__ __launch_bounds__(1024) void k_sort_scan(SortArgs a, int parts)
+{
+    __shared__ SortLds s;
+    const int e = threadIdx.x;
+    int total = 0;
+    if (e < a.experts) {
+#pragma unroll 8
+        for (int p = 0; p < parts; ++p) total += a.workspace[(int64_t)p * a.experts + e];
+    }
+    int end;
+    const int first = sort_segments(s, total, &end);
+    if (e < a.experts) {
+        int next = first;
+#pragma unroll 8
+        for (int p = 0; p < parts; ++p) {
+            const int n = a.workspace[(int64_t)p * a.experts + e];
+            a.workspace[(int64_t)p * a.experts + e] = next;
+            next += n;
+        }
+    }
+    sort_finish(a, first, total, end);
+}
+
+__global__ __launch_bounds__(1024) void k_sort_place(SortArgs a)
+{
+    __shared__ SortLds s;
+    const int64_t first = (int64_t)blockIdx.x * kSortPart, last = min(first + kSortPart, a.T);
+    sort_count(s, a, first, last);
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.experts; e += blockDim.x) {
+        int next = a.workspace[(int64_t)blockIdx.x * a.experts + e];
+        for (int w = 0; w < kSortWaves; ++w) {
+            const int n = s.count[w][e];
+            s.count[w][e] = next;
+            next += n;
+        }
+    }
+    __syncthreads();
+    sort_place(s, a, first, last);
+}
+
+sp24_status launch_moe_sort(const SortArgs& a, hipStream_t st)
+{
+    const int parts = (int)((a.T + kSortPart - 1) / kSortPart);
+    if (parts <= 1) k_sort_one<<<1, 1024, 0, st>>>(a);
+    else {
+        k_sort_count<<<parts, 1024, 0, st>>>(a);
+        k_sort_scan<<<1, 1024, 0, st>>>(a, parts);
+        k_sort_place<<<parts, 1024, 0, st>>>(a);
+    }
+    return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
+}
+
+// ---------------------------------------------------------------------------
+// Rows by expert: row i is the token of choice rows[i], zeros where there is none.  16 bytes a thread.
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ uint4v load_bytes(const uint8_t* p, int64_t n)
+{
+    if (n >= 16) return load_from<uint4v>(p);
+    uint4v v = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        if (i < n) v[i / 4] |= (uint32_t)p[i] << (8 * (i % 4));
+    return v;
+}
+__device__ __forceinline__ void store_bytes(uint8_t* p, int64_t n, const uint4v& v)
+{
+    if (n >= 16) {
+        store_to(p, v);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        if (i < n) p[i] = (uint8_t)(v[i / 4] >> (8 * (i % 4)));
+}
+
+__global__ __launch_bounds__(256) void k_moe_gather(GatherArgs a, int blocks_a_row)
+{
+    const int64_t row = blockIdx.x / blocks_a_row;
+    const int64_t at = ((int64_t)(blockIdx.x % blocks_a_row) * blockDim.x + threadIdx.x) * 16;
+    const int64_t choice = a.rows[row], token = choice < 0 ? -1 : choice / a.topk;
+    const bool live = token >= 0 && token < a.N;
+    if (a.scale && at == 0) a.scale_out[row] = live ? a.scale[token] : 0.0f;
+    if (at >= a.row_bytes) return;
+    const int64_t n = a.row_bytes - at;
+    const uint4v v = live ? load_bytes(reinterpret_cast<const uint8_t*>(a.X) + token * a.ldx_bytes + at, n) : uint4v{0u, 0u, 0u, 0u};
+    store_bytes(reinterpret_cast<uint8_t*>(a.Xs) + row * a.ldxs_bytes + at, n, v);
+}
+
+// a launch of threads that hold `width` bytes (values) of a row each: threads of a workgroup, workgroups to a row
+static void row_launch(int64_t length, int width, unsigned& threads, int& blocks_a_row)
+{
+    const int64_t pieces = (length + width - 1) / width;
+    threads = (unsigned)(pieces >= 256 ? 256 : (pieces + 63) / 64 * 64);
+    blocks_a_row = (int)((pieces + threads - 1) / threads);
+}
+
+sp24_status launch_moe_gather(const GatherArgs& a, hipStream_t st)
+{
+    unsigned threads;
+    int blocks;
+    row_launch(a.row_bytes, 16, threads, blocks);
+    k_moe_gather<<<(unsigned)(a.R * blocks), threads, 0, st>>>(a, blocks);
+    return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
+}
+
+// ---------------------------------------------------------------------------
+// out[n] = residual[n] + sum over j, in that order, of weights[n][j] Y[slots[n][j]], in binary32, rounded once.  Eight values a thread.
+// ---------------------------------------------------------------------------
+template <int T>
+__global__ __launch_bounds__(256) void k_moe_combine(CombineArgs a, int blocks_a_row)
+{
+    const int64_t n = blockIdx.x / blocks_a_row;
+    const int64_t at = ((int64_t)(blockIdx.x % blocks_a_row) * blockDim.x + threadIdx.x) * 8;
+    if (at >= a.H) return;
+    const int have = (int)min(a.H - at, (int64_t)8);
+    float sum[8] = {};
+    raw8<T> first = {};
+    if (a.residual) first = load_raw8<T>(a.residual, n * a.ldr + at, have);
+    for (int j0 = 0; j0 < a.topk; j0 += 4) {                     // four rows on their way
+        raw8<T> y[4];
+        float w[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int j = j0 + u;
+            const int64_t slot = j < a.topk ? a.slots[n * a.topk + j] : -1;
+            const bool live = slot >= 0 && slot < a.R;
+            w[u] = !live ? 0.0f : a.weights ? a.weights[n * a.topk + j] : 1.0f;
+            y[u] = live ? load_raw8<T>(a.Y, slot * a.ldy + at, have) : raw8<T>{};
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            float v[8];
+            values_of<T>(y[u], v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] = __builtin_fmaf(w[u], v[i], sum[i]);
+        }
+    }
+    if (a.residual) {
+        float v[8];
+        values_of<T>(first, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] += v[i];
+    }
+    store_values8<T>(a.out, n * a.ldo + at, have, sum);
+}
+
+sp24_status launch_moe_combine(const CombineArgs& a, hipStream_t st)
+{
+    unsigned threads;
+    int blocks;
+    row_launch(a.H, 8, threads, blocks);
+    const unsigned grid = (unsigned)(a.N * blocks);
+    if (a.t == SP24_F32) k_moe_combine<SP24_F32><<<grid, threads, 0, st>>>(a, blocks);
+    else if (a.t == SP24_F16) k_moe_combine<SP24_F16><<<grid, threads, 0, st>>>(a, blocks);
+    else k_moe_combine<SP24_BF16><<<grid, threads, 0, st>>>(a, blocks);
+    return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
+}
+
+// ---------------------------------------------------------------------------
+// Its gradients: dY[i] = weight of choice rows[i] times dOut of its token (zeros where there is none), dweights = the inner product of
+// dOut and Y there, 0 for a choice without a row.  A wavefront to a row.
+// ---------------------------------------------------------------------------
+template <int T>
+__global__ __launch_bounds__(256) void k_moe_combine_grad(CombineGradArgs a)
+{
+    const int lane = threadIdx.x & 63;
+    for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < a.N * a.topk; t += (int64_t)gridDim.x * 256)
+        if (a.slots[t] < 0 || a.slots[t] >= a.R) a.dweights[t] = 0.0f;
+    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= a.R) return;
+    const int64_t choice = a.rows[row], token = choice < 0 ? -1 : choice / a.topk;
+    const bool live = token >= 0 && token < a.N;
+    const float w = live ? a.weights[choice] : 0.0f;
+    float dot = 0.0f;
+    for (int64_t at = lane * 8; at < a.H; at += 512) {
+        const int have = (int)min(a.H - at, (int64_t)8);
+        float d[8] = {}, y[8];
+        if (live) {
+            values_of<T>(load_raw8<T>(a.dOut, token * a.lddo + at, have), d);
+            values_of<T>(load_raw8<T>(a.Y, row * a.ldy + at, have), y);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                dot = __builtin_fmaf(d[i], y[i], dot);
+                d[i] *= w;
+            }
+        }
+        store_values8<T>(a.dY, row * a.lddy + at, have, d);
+    }
+    dot = __uint_as_float(over_wave<add_f>(__float_as_uint(dot)));
+    if (live && lane == 0) a.dweights[choice] = dot;
+}
+
+sp24_status launch_moe_combine_grad(const CombineGradArgs& a, hipStream_t st)
+{
+    const unsigned grid = (unsigned)((a.R + 3) / 4);
+    if (a.t == SP24_F32) k_moe_combine_grad<SP24_F32><<<grid, 256, 0, st>>>(a);
+    else if (a.t == SP24_F16) k_moe_combine_grad<SP24_F16><<<grid, 256, 0, st>>>(a);
+    else k_moe_combine_grad<SP24_BF16><<<grid, 256, 0, st>>>(a);
+    return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
+}
+
+} // namespace sp24

@@ -55,6 +55,7 @@ struct MmArgs {
     // from s * slice_steps on and writes its partial product, in the accumulator type, to image s of D
     // (M rows of ldd values each); out must then be F32 or I32, and conv and epi off.
     int k_slices, slice_steps;
+    static constexpr bool kOwnStore = false;   // (arguments derived from these may bring their own way out)
 };
 
 // General kernel: any M, N; both layouts; both B orders.  One wavefront per 32x32 tile of D.  Of the sparse products only
@@ -89,5 +90,94 @@ sp24_status launch_mm_tiled(const MmArgs& a, hipStream_t st, bool* handled);
 // each, images M * ldw values apart).
 sp24_status launch_splitk_reduce(const void* partial, int slices, int64_t M, int64_t N, int64_t ldw, void* D, int64_t ldd, bool integer,
                                  sp24_dtype out, hipStream_t st);
+
+// ---- the operators around the products (N rows of H values unless said otherwise; ld* in elements) ----
+struct RowsArgs {
+    const void *X, *residual;
+    const float* weight;                  // null: quantisation alone
+    void *Y, *hidden;
+    float *scale, *rstd;
+    int64_t N, H, ldx, ldr, ldy, ldh;
+    float eps;
+    sp24_dtype t, out;
+};
+sp24_status launch_norm_rows(const RowsArgs& a, hipStream_t st);
+
+struct NormGradArgs {
+    const void *dY, *hidden, *dhidden;
+    const float *weight, *rstd;
+    void* dX;
+    float *partial, *dweight;             // partial: norm_grad_groups() rows of H
+    int64_t N, H, lddy, ldh, lddh, lddx;
+    sp24_dtype t;
+};
+int64_t norm_grad_groups(int64_t N, int64_t H);
+sp24_status launch_norm_grad(const NormGradArgs& a, hipStream_t st);
+
+// out [segments][columns] = sums of rows of `partial` (rows x columns), all of them or (offsets) segment by segment, `unit` rows of the
+// offsets to one of partial
+sp24_status launch_column_sums(const float* partial, int64_t rows, int64_t columns, const int32_t* offsets, int segments, int unit, float* out,
+                               hipStream_t st);
+
+struct LinearGradArgs {
+    const void *dY, *Z;                   // N rows of M values
+    void *dZ, *dZt;
+    float *partial, *dbias;               // partial: a row of M for every `unit` (16 or 64) rows
+    const int32_t* offsets;
+    int64_t M, N, lddy, ldz, lddz, lddzt;
+    int act, experts, unit;
+    sp24_dtype t;
+};
+sp24_status launch_linear_grad(const LinearGradArgs& a, hipStream_t st);
+
+constexpr int kSortPart = 16384;          // choices that one workgroup sorts
+struct SortArgs {
+    const int32_t* ids;                   // T choices
+    int32_t *offsets, *slots, *rows, *workspace;      // workspace: experts words for every part where there are several
+    int64_t T, R;
+    int experts;
+};
+sp24_status launch_moe_sort(const SortArgs& a, hipStream_t st);
+
+struct GatherArgs {
+    const void* X;
+    const float* scale;
+    const int32_t* rows;
+    void* Xs;
+    float* scale_out;
+    int64_t N, R, row_bytes, ldx_bytes, ldxs_bytes;
+    int topk;
+};
+sp24_status launch_moe_gather(const GatherArgs& a, hipStream_t st);
+
+struct CombineArgs {
+    const void *Y, *residual;
+    const int32_t* slots;
+    const float* weights;                 // null: 1
+    void* out;
+    int64_t N, R, H, ldy, ldr, ldo;
+    int topk;
+    sp24_dtype t;
+};
+sp24_status launch_moe_combine(const CombineArgs& a, hipStream_t st);
+
+struct CombineGradArgs {
+    const void *dOut, *Y;
+    const int32_t *rows, *slots;
+    const float* weights;
+    void* dY;
+    float* dweights;
+    int64_t N, R, H, lddo, ldy, lddy;
+    int topk;
+    sp24_dtype t;
+};
+sp24_status launch_moe_combine_grad(const CombineGradArgs& a, hipStream_t st);
+
+struct LinearArgs;                        // linear.hpp
+struct GroupedArgs;
+struct SegmentArgs;
+sp24_status launch_linear(const LinearArgs& a, hipStream_t st);
+sp24_status launch_linear_grouped(const GroupedArgs& a, hipStream_t st);
+sp24_status launch_gemm_grouped(const SegmentArgs& a, int experts, hipStream_t st);
 
 } // namespace sp24

@@ -467,6 +467,16 @@ __device__ __forceinline__ void store_wave_tile(const MmArgs& a, typename acc_of
     }
 }
 
+// The kernels below take the plain product's arguments, or others derived from them that say by member functions what differs: where a
+// workgroup's tile lies and which operands are its own (enter), and how a wavefront's tile is stored (store_wave, with wave_bytes() of LDS).
+template <class ARGS> constexpr bool is_plain = std::is_same<ARGS, MmArgs>::value;
+template <class ARGS, int OUT, int TM, int TN>
+constexpr int store_bytes()
+{
+    if constexpr (ARGS::kOwnStore) return ARGS::template wave_bytes<TM>();
+    else return epilogue_geometry<OUT, TN>::kWaveBytes;
+}
+
 // ---------------------------------------------------------------------------
 // Sparse kernel.  Stage layout: [B: BN rows x 128 B, swizzled][V: 2 KiB per
 // 32-row block, in the tiled layout's own order][meta: 256 B per 32x64 tile].
@@ -474,8 +484,8 @@ __device__ __forceinline__ void store_wave_tile(const MmArgs& a, typename acc_of
 // first operands of step s+1 are read from LDS during the tail of step s.
 // ---------------------------------------------------------------------------
 // BSRC: where B comes from -- 0 a K-major matrix, 1 NHWC activations (implicit GEMM), 2 an N-major matrix
-template <int DT, int OUT, int WM, int WN, int TM, int TN, int NS, int BSRC>
-__global__ __launch_bounds__(64 * WM * WN, 1) void k_spmm_pipe(MmArgs a, int tiles_m, int tiles_n)
+template <int DT, int OUT, int WM, int WN, int TM, int TN, int NS, int BSRC, class ARGS = MmArgs>
+__global__ __launch_bounds__(64 * WM * WN, 1) void k_spmm_pipe(ARGS a, int tiles_m, int tiles_n)
 {
     constexpr bool CONV = BSRC == 1, NMAJ = BSRC == 2;
     constexpr int ES = is8<DT> ? 1 : 2;
@@ -492,13 +502,16 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_spmm_pipe(MmArgs a, int til
     constexpr int kVOff = BN * kRowBytes, kMOff = kVOff + RB * 2048;
     constexpr int kStageBytes = kMOff + RB * T64 * 256;
     using acc_t = typename acc_of<DT>::type;
-    constexpr int kEpiBytes = NW * epilogue_geometry<OUT, TN>::kWaveBytes;
+    constexpr int kEpiBytes = NW * store_bytes<ARGS, OUT, TM, TN>();
     static_assert(NS >= 3 && (NS - 2) * NV <= 63, "at least three stages; vmcnt is a 6-bit counter");
     constexpr int kLdsBytes = NS * kStageBytes > kEpiBytes ? NS * kStageBytes : kEpiBytes;
     __shared__ __attribute__((aligned(1024))) uint8_t lds_all[kLdsBytes];
 
     int tm, tn;
     tile_of_workgroup(tiles_m, tiles_n, tm, tn);
+    if constexpr (!is_plain<ARGS>) {
+        if (!a.template enter<BM, BN>(tm, tn)) return;
+    }
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave % WN;
@@ -805,8 +818,10 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_spmm_pipe(MmArgs a, int til
         __builtin_amdgcn_sched_barrier(0);
     }
     // LDS becomes store scratch
-    store_wave_tile<DT, OUT, TM, TN>(a, acc, lds_all + wave * epilogue_geometry<OUT, TN>::kWaveBytes,
-                                     (int64_t)tm * BM + wm * TM * 32, (int64_t)tn * BN + wn * TN * 32, lane);
+    uint8_t* const scratch = lds_all + wave * store_bytes<ARGS, OUT, TM, TN>();
+    const int64_t row_base = (int64_t)tm * BM + wm * TM * 32, col_base = (int64_t)tn * BN + wn * TN * 32;
+    if constexpr (ARGS::kOwnStore) a.template store_wave<DT, TM, TN>(acc, scratch, row_base, col_base, lane);
+    else store_wave_tile<DT, OUT, TM, TN>(a, acc, scratch, row_base, col_base, lane);
 }
 
 // ---------------------------------------------------------------------------
@@ -814,8 +829,8 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_spmm_pipe(MmArgs a, int til
 // through LDS (A is plain row-major, so its fragments are not contiguous in
 // memory); NS stages, transfers NS - 1 steps ahead.
 // ---------------------------------------------------------------------------
-template <int DT, int OUT, int WM, int WN, int TM, int TN, int NS, int BSRC>
-__global__ __launch_bounds__(64 * WM * WN, 1) void k_gemm_pipe(MmArgs a, int tiles_m, int tiles_n)
+template <int DT, int OUT, int WM, int WN, int TM, int TN, int NS, int BSRC, class ARGS = MmArgs>
+__global__ __launch_bounds__(64 * WM * WN, 1) void k_gemm_pipe(ARGS a, int tiles_m, int tiles_n)
 {
     constexpr bool CONV = BSRC == 1, NMAJ = BSRC == 2;
     constexpr int ES = is8<DT> ? 1 : 2;
@@ -827,13 +842,16 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_gemm_pipe(MmArgs a, int til
     constexpr int NJA = deal_a::each, NJB = deal_b::each;
     constexpr int kStageBytes = (BM + BN) * kRowBytes;
     using acc_t = typename acc_of<DT>::type;
-    constexpr int kEpiBytes = NW * epilogue_geometry<OUT, TN>::kWaveBytes;
+    constexpr int kEpiBytes = NW * store_bytes<ARGS, OUT, TM, TN>();
     static_assert(NS >= 2 && (NS - 2) * (NJA + NJB) <= 63, "at least two stages; vmcnt is a 6-bit counter");
     constexpr int kLdsBytes = NS * kStageBytes > kEpiBytes ? NS * kStageBytes : kEpiBytes;
     __shared__ __attribute__((aligned(1024))) uint8_t lds_all[kLdsBytes];
 
     int tm, tn;
     tile_of_workgroup(tiles_m, tiles_n, tm, tn);
+    if constexpr (!is_plain<ARGS>) {
+        if (!a.template enter<BM, BN>(tm, tn)) return;
+    }
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave % WN;
@@ -1024,8 +1042,10 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_gemm_pipe(MmArgs a, int til
         __builtin_amdgcn_sched_barrier(0);
     }
     // LDS becomes store scratch
-    store_wave_tile<DT, OUT, TM, TN>(a, acc, lds_all + wave * epilogue_geometry<OUT, TN>::kWaveBytes,
-                                     (int64_t)tm * BM + wm * TM * 32, (int64_t)tn * BN + wn * TN * 32, lane);
+    uint8_t* const scratch = lds_all + wave * store_bytes<ARGS, OUT, TM, TN>();
+    const int64_t row_base = (int64_t)tm * BM + wm * TM * 32, col_base = (int64_t)tn * BN + wn * TN * 32;
+    if constexpr (ARGS::kOwnStore) a.template store_wave<DT, TM, TN>(acc, scratch, row_base, col_base, lane);
+    else store_wave_tile<DT, OUT, TM, TN>(a, acc, scratch, row_base, col_base, lane);
 }
 
 // ---------------------------------------------------------------------------

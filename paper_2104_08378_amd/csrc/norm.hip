@@ -1,0 +1,299 @@
+// Root-mean-square norm of rows (with the residual added in front and 8-bit rows with a scale each behind), the quantisation of rows
+// alone, and the norm's gradients.
+//
+//   h = x + r,  y = h rstd w,  rstd = (mean h^2 + eps)^-1/2;   8-bit: scale = max|y| / top, code = y (top / max|y|) rounded
+//   g = w dy,  dx = rstd (g - h rstd^2 mean(g h)) + dh,  dw = sum over the rows of dy h rstd
+//
+// Bound by memory: a row is read once, stays in registers (eight values a lane and chunk, in binary32 as all sums are) and is written
+// once.  A workgroup takes a row after the other and keeps its weights.
+#include "launch.hpp"
+#include "rowops.hpp"
+
+namespace sp24 {
+
+// the value that 8-bit codes reach at the largest magnitude of their row
+template <int OUT> constexpr float top_code() { return OUT == SP24_I8 ? 127.0f : 448.0f; }
+constexpr float kLeastMagnitude = 7.888609052210118e-31f;       // 2^-100: below it a row's codes are taken against it (and are zeros)
+
+template <int OUT>
+__device__ __forceinline__ void store_codes8(void* p, int64_t first, int n, const float (&v)[8])
+{
+    uint8_t* at = reinterpret_cast<uint8_t*>(p) + first;
+    uint2v q = {0u, 0u};
+#pragma unroll
+    for (int d = 0; d < 2; ++d) {
+        if constexpr (OUT == SP24_I8) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q[d] |= ((uint32_t)(int)__builtin_rintf(v[4 * d + i]) & 0xFFu) << (8 * i);
+        } else {
+            int w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * d], v[4 * d + 1], 0, false);
+            q[d] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[4 * d + 2], v[4 * d + 3], w, true);
+        }
+    }
+    if (n >= 8) store_to(at, q);
+    else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) at[i] = (uint8_t)(q[i / 4] >> (8 * (i % 4)));
+    }
+}
+
+// C: chunks of eight values a thread holds; thread t those at (c * blockDim.x + t) * 8
+template <int T, int OUT, int C, bool NORM>
+__global__ __launch_bounds__(1024) void k_norm_rows(RowsArgs a)
+{
+    __shared__ uint32_t cells[3][16];
+    const int H = (int)a.H;
+    float w[C][8];
+    int n[C];                                                    // values of the chunk that exist
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int first = (c * blockDim.x + threadIdx.x) * 8;
+        n[c] = min(H - first, 8);
+        if (NORM && n[c] > 0) load_floats8(a.weight, first, n[c], w[c]);
+    }
+    int parity = 0;
+    for (int64_t row = blockIdx.x; row < a.N; row += gridDim.x) {
+        raw8<T> x[C], r[C];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int first = (c * blockDim.x + threadIdx.x) * 8;
+            if (n[c] > 0) x[c] = load_raw8<T>(a.X, row * a.ldx + first, n[c]);
+            if (NORM && a.residual && n[c] > 0) r[c] = load_raw8<T>(a.residual, row * a.ldr + first, n[c]);
+        }
+        float h[C][8], sum = 0.0f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            if (n[c] <= 0) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) h[c][i] = 0.0f;
+                continue;
+            }
+            values_of<T>(x[c], h[c]);
+            if constexpr (NORM) {
+                if (a.residual) {
+                    float more[8];
+                    values_of<T>(r[c], more);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) h[c][i] += more[i];
+                }
+                // (rounded to the rows' type here; the norm goes on with the unrounded sum)
+                if (a.hidden) store_values8<T>(a.hidden, row * a.ldh + (c * blockDim.x + threadIdx.x) * 8, n[c], h[c]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(h[c][i], h[c][i], sum);
+            }
+        }
+        if constexpr (NORM) {
+            const float square = __uint_as_float(over_workgroup<add_f>(__float_as_uint(sum), cells[parity]));
+            parity ^= 1;
+            const float rstd = 1.0f / __builtin_sqrtf(square / (float)H + a.eps);
+            if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+                if (n[c] > 0) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) h[c][i] = h[c][i] * rstd * w[c][i];
+                }
+        }
+        if constexpr (is8<OUT>) {
+            // magnitudes through their bit patterns, in which a NaN is the largest: it reaches the scale, and no row hides one.
+            // (Values past the row's end are zeros.)
+            uint32_t most = 0;
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) most = max(most, i < n[c] ? __float_as_uint(h[c][i]) & 0x7FFFFFFFu : 0u);
+            float top = __uint_as_float(over_workgroup<max_u>(most, cells[2]));
+            if (!NORM) __syncthreads();                          // (the norm's sum has a barrier between two uses of the cells)
+            top = top < kLeastMagnitude ? kLeastMagnitude : top;
+            if (threadIdx.x == 0) a.scale[row] = top / top_code<OUT>();
+            const float inv = top_code<OUT>() / top;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                if (n[c] <= 0) continue;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) h[c][i] *= inv;
+                store_codes8<OUT>(a.Y, row * a.ldy + (c * blockDim.x + threadIdx.x) * 8, n[c], h[c]);
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+                if (n[c] > 0) store_values8<OUT>(a.Y, row * a.ldy + (c * blockDim.x + threadIdx.x) * 8, n[c], h[c]);
+        }
+    }
+}
+
+// The gradients.  A workgroup's share of dw stays in registers over its rows and goes to its row of `partial`.
+template <int T, int C>
+__global__ __launch_bounds__(1024) void k_norm_grad(NormGradArgs a)
+{
+    __shared__ uint32_t cells[2][16];
+    const int H = (int)a.H;
+    float w[C][8], dw[C][8];
+    int n[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int first = (c * blockDim.x + threadIdx.x) * 8;
+        n[c] = min(H - first, 8);
+        if (n[c] > 0) load_floats8(a.weight, first, n[c], w[c]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dw[c][i] = 0.0f;
+    }
+    int parity = 0;
+    for (int64_t row = blockIdx.x; row < a.N; row += gridDim.x) {
+        raw8<T> dy_raw[C], h_raw[C], dh_raw[C];
+        const float rstd = a.rstd[row];
+        float along = 0.0f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int first = (c * blockDim.x + threadIdx.x) * 8;
+            if (n[c] <= 0) continue;
+            dy_raw[c] = load_raw8<T>(a.dY, row * a.lddy + first, n[c]);
+            h_raw[c] = load_raw8<T>(a.hidden, row * a.ldh + first, n[c]);
+            if (a.dhidden) dh_raw[c] = load_raw8<T>(a.dhidden, row * a.lddh + first, n[c]);
+        }
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            if (n[c] <= 0) continue;
+            float dy[8], h[8];
+            values_of<T>(dy_raw[c], dy);
+            values_of<T>(h_raw[c], h);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float t = dy[i] * h[i];
+                if (i < n[c]) along = __builtin_fmaf(t, w[c][i], along);
+                dw[c][i] = __builtin_fmaf(t, rstd, dw[c][i]);
+            }
+        }
+        along = __uint_as_float(over_workgroup<add_f>(__float_as_uint(along), cells[parity]));
+        parity ^= 1;
+        const float k = rstd * rstd * (along / (float)H);
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            if (n[c] <= 0) continue;
+            float dy[8], h[8], dx[8];
+            values_of<T>(dy_raw[c], dy);
+            values_of<T>(h_raw[c], h);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dx[i] = rstd * (dy[i] * w[c][i] - h[i] * k);
+            if (a.dhidden) {
+                float dh[8];
+                values_of<T>(dh_raw[c], dh);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) dx[i] += dh[i];
+            }
+            store_values8<T>(a.dX, row * a.lddx + (c * blockDim.x + threadIdx.x) * 8, n[c], dx);
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+        if (n[c] > 0) store_values8<SP24_F32>(a.partial, (int64_t)blockIdx.x * a.H + (c * blockDim.x + threadIdx.x) * 8, n[c], dw[c]);
+}
+
+// out[e][c] = the sum of rows first .. last - 1 of `partial` (columns wide), in a fixed order: 16 interleaved sums, then those.
+// Without offsets all rows; with them those of segment e, `unit` rows of the offsets to one of partial.
+__global__ __launch_bounds__(1024) void k_column_sums(const float* partial, int64_t rows, int64_t columns, const int32_t* offsets, int unit,
+                                                      float* out)
+{
+    __shared__ float part[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    int64_t first = 0, last = rows;
+    if (offsets) {
+        first = min(max((int64_t)offsets[blockIdx.y] / unit, (int64_t)0), rows);
+        last = min(max((int64_t)offsets[blockIdx.y + 1] / unit, first), rows);
+    }
+    float sum = 0.0f;
+    if (c < columns) {
+        int64_t i = first + wave;
+        for (; i + 48 < last; i += 64) {                          // four loads on their way
+            const float v0 = partial[i * columns + c], v1 = partial[(i + 16) * columns + c], v2 = partial[(i + 32) * columns + c],
+                        v3 = partial[(i + 48) * columns + c];
+            sum = (((sum + v0) + v1) + v2) + v3;
+        }
+        for (; i < last; i += 16) sum += partial[i * columns + c];
+    }
+    part[wave][lane] = sum;
+    __syncthreads();
+    if (wave == 0 && c < columns) {
+        sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum += part[i][lane];
+        out[(int64_t)blockIdx.y * columns + c] = sum;
+    }
+}
+
+// threads for rows of H values at C chunks a thread, in whole wavefronts; 0: too long for that
+static unsigned row_threads(int64_t H, int C)
+{
+    const int64_t chunks = (H + 7) / 8, threads = ((chunks + C - 1) / C + 63) / 64 * 64;
+    return threads <= 1024 ? (unsigned)threads : 0u;
+}
+
+template <int T, int OUT, bool NORM>
+static sp24_status run_norm(const RowsArgs& a, hipStream_t st)
+{
+    const unsigned t1 = row_threads(a.H, 1), t4 = row_threads(a.H, 4), t8 = row_threads(a.H, 8);
+    const bool one = t1 != 0 && (t4 == 64 ? t1 == 64 : a.N < 1024);
+    const unsigned threads = one ? t1 : t4 ? t4 : t8;
+    const unsigned grid = (unsigned)(a.N < (int64_t)(1 << 20) / threads ? a.N : (1 << 20) / threads);
+    if (one) k_norm_rows<T, OUT, 1, NORM><<<grid, threads, 0, st>>>(a);
+    else if (t4) k_norm_rows<T, OUT, 4, NORM><<<grid, threads, 0, st>>>(a);
+    else if constexpr (!NORM) k_norm_rows<T, OUT, 8, NORM><<<grid, threads, 0, st>>>(a);
+    return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
+}
+
+template <int T>
+static sp24_status run_norm_out(const RowsArgs& a, hipStream_t st)
+{
+    if (!a.weight) return a.out == SP24_I8 ? run_norm<T, SP24_I8, false>(a, st) : run_norm<T, SP24_F8, false>(a, st);
+    switch (a.out) {
+    case SP24_I8: return run_norm<T, SP24_I8, true>(a, st);
+    case SP24_F8: return run_norm<T, SP24_F8, true>(a, st);
+    case SP24_F32: return run_norm<T, SP24_F32, true>(a, st);
+    case SP24_F16: return run_norm<T, SP24_F16, true>(a, st);
+    default: return run_norm<T, SP24_BF16, true>(a, st);
+    }
+}
+
+sp24_status launch_norm_rows(const RowsArgs& a, hipStream_t st)
+{
+    if (a.t == SP24_F32) return run_norm_out<SP24_F32>(a, st);
+    if (a.t == SP24_F16) return run_norm_out<SP24_F16>(a, st);
+    return run_norm_out<SP24_BF16>(a, st);
+}
+
+int64_t norm_grad_groups(int64_t N, int64_t H)
+{
+    const unsigned threads = row_threads(H, H <= 8192 ? 1 : 4);
+    const int64_t most = (1 << 17) / (int64_t)threads;            // two wavefronts a SIMD
+    return N < most ? N : most;
+}
+
+template <int T>
+static sp24_status run_norm_grad(const NormGradArgs& a, hipStream_t st)
+{
+    const unsigned grid = (unsigned)norm_grad_groups(a.N, a.H);
+    if (grid > 0) {
+        if (a.H <= 8192) k_norm_grad<T, 1><<<grid, row_threads(a.H, 1), 0, st>>>(a);
+        else k_norm_grad<T, 4><<<grid, row_threads(a.H, 4), 0, st>>>(a);
+        if (hipGetLastError() != hipSuccess) return SP24_ERR_LAUNCH;
+    }
+    return launch_column_sums(a.partial, grid, a.H, nullptr, 1, 1, a.dweight, st);
+}
+
+sp24_status launch_norm_grad(const NormGradArgs& a, hipStream_t st)
+{
+    if (a.t == SP24_F32) return run_norm_grad<SP24_F32>(a, st);
+    if (a.t == SP24_F16) return run_norm_grad<SP24_F16>(a, st);
+    return run_norm_grad<SP24_BF16>(a, st);
+}
+
+sp24_status launch_column_sums(const float* partial, int64_t rows, int64_t columns, const int32_t* offsets, int segments, int unit, float* out,
+                               hipStream_t st)
+{
+    k_column_sums<<<dim3((unsigned)((columns + 63) / 64), (unsigned)segments), 1024, 0, st>>>(partial, rows, columns, offsets, unit, out);
+    return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
+}
+
+} // namespace sp24

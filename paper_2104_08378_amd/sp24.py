@@ -11,6 +11,7 @@ passes raw device pointers and the current HIP stream, and raises on a non-zero
 status.  Every arithmetic step runs in the library's HIP kernels; there is no
 fallback: if ``libsp24.so`` is not built the import of the symbols fails loudly.
 """
+import collections
 import ctypes
 import importlib.machinery
 import importlib.util
@@ -79,6 +80,28 @@ def lib():
         L.sp24_gemm_dense_i8_scaled.argtypes = [vp, vp, vp, i64, i64, i64, i64, i64, i64, vp, f32, vp, i32, f32, i32, i32, vp]
         L.sp24_spmm_conv2d_i8_scaled.argtypes = [vp, vp, vp, vp] + [i64] * 5 + [i32] * 6 + [i64, vp, f32, vp, i32, f32, i32, i32, vp]
         L.sp24_conv2d_dense_i8_scaled.argtypes = [vp, vp, vp] + [i64] * 5 + [i32] * 6 + [i64, i64, vp, f32, vp, i32, f32, i32, vp]
+        st = ctypes.c_size_t
+        L.sp24_rmsnorm.argtypes = [vp, vp, vp, f32, vp, vp, vp, vp] + [i64] * 6 + [i32, i32, vp]
+        L.sp24_quantize_rows.argtypes = [vp, vp, vp] + [i64] * 4 + [i32, i32, vp]
+        L.sp24_rmsnorm_backward_workspace_bytes.argtypes = [i64, i64]
+        L.sp24_rmsnorm_backward.argtypes = [vp] * 7 + [i64] * 6 + [i32, vp, st, vp]
+        L.sp24_linear.argtypes = [vp] * 4 + [i64] * 5 + [vp, vp, vp, i32, vp, i64, vp, i64, i32, i32, i32, vp]
+        L.sp24_linear_backward_workspace_bytes.argtypes = [i64, i64, i32]
+        L.sp24_linear_backward.argtypes = [vp] * 5 + [i64] * 6 + [i32, vp, i32, i32, vp, st, vp]
+        L.sp24_moe_rows.argtypes = [i64, i32]
+        L.sp24_moe_rows.restype = i64
+        L.sp24_moe_sort_workspace_bytes.argtypes = [i64, i32]
+        L.sp24_moe_sort.argtypes = [vp] * 4 + [i64, i32, i64, vp, st, vp]
+        L.sp24_moe_gather.argtypes = [vp] * 5 + [i64, i64, i32, i64, i64, i64, i32, vp]
+        L.sp24_moe_combine.argtypes = [vp] * 5 + [i64, i64, i32, i64, i64, i64, i64, i32, vp]
+        L.sp24_moe_combine_backward.argtypes = [vp] * 7 + [i64, i64, i32, i64, i64, i64, i64, i32, vp]
+        L.sp24_linear_grouped.argtypes = [vp] * 5 + [i32] + [i64] * 5 + [vp, vp, vp, i32, vp, i64, i32, i32, i32, vp]
+        L.sp24_gemm_dense_grouped.argtypes = [vp] * 4 + [i32] + [i64] * 6 + [i32, i32, vp]
+        for name in ("sp24_rmsnorm_backward_workspace_bytes", "sp24_linear_backward_workspace_bytes", "sp24_moe_sort_workspace_bytes"):
+            getattr(L, name).restype = st
+        for name in ("sp24_rmsnorm", "sp24_quantize_rows", "sp24_rmsnorm_backward", "sp24_linear", "sp24_linear_backward", "sp24_moe_sort", "sp24_moe_gather",
+                     "sp24_moe_combine", "sp24_moe_combine_backward", "sp24_linear_grouped", "sp24_gemm_dense_grouped"):
+            getattr(L, name).restype = i32
         L.sp24_status_string.argtypes = [i32]
         L.sp24_status_string.restype = ctypes.c_char_p
         for name in ("sp24_prune_transposable", "sp24_mask_apply", "sp24_compress_masked", "sp24_prune", "sp24_compress", "sp24_decompress", "sp24_spmm", "sp24_gemm_dense", "sp24_spmm_conv2d",
@@ -606,4 +629,239 @@ def sp24_conv2d_dense_i8_scaled(A, X, out_dtype, R, S, w_scale, x_scale, bias=No
     _check(lib().sp24_conv2d_dense_i8_scaled(A.data_ptr(), X.data_ptr(), D.data_ptr(), M, *geom, A.stride(0), D.stride(0), ws,
                                              float(x_scale), bs, int(bool(relu)), float(inv_y_scale), _DT[D.dtype], _stream()),
            "sp24_conv2d_dense_i8_scaled")
+    return D
+
+
+# ---- the operators around the products: one row per token in and out ------------------------------------------------
+
+NO_ACT, RELU, GELU, SILU = 0, 1, 2, 3
+_ACT = {"none": NO_ACT, "relu": RELU, "gelu": GELU, "silu": SILU}
+MOST_EXPERTS = 1024                # SP24_MOST_EXPERTS of the header
+
+#: What sp24_rmsnorm returns; None in the place of what was not asked for.
+RmsNorm = collections.namedtuple("RmsNorm", "y scale hidden rstd")
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _vector(t, n, name, dtype=torch.float32):
+    """A contiguous vector of n entries (any shape), or None."""
+    if t is None:
+        return None
+    _dev(t, name)
+    if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous tensor of {n} entries of {dtype}")
+    return t.data_ptr()
+
+
+def _matrix_like(t, shape, dtype, name):
+    """(pointer, row stride) of a matrix of exactly this shape and type, or of None."""
+    if t is None:
+        return None, 0
+    _out(t, shape, dtype, None, name)
+    return t.data_ptr(), _ld(t)
+
+
+def _act(act):
+    if act not in _ACT:
+        raise ValueError("act must be 'none', 'relu', 'gelu' or 'silu'")
+    return _ACT[act]
+
+
+def _scratch(workspace, need, device):
+    """(the tensor, its bytes): the caller's workspace, or a new one where some is needed."""
+    if workspace is None:
+        if need == 0:
+            return None, 0
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    _dev(workspace, "workspace")
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def sp24_rmsnorm(X, weight, eps=1e-6, residual=None, out_dtype=None, want_rstd=False, hidden=None, out=None):
+    """Root-mean-square norm of the rows of X (plus ``residual``): RmsNorm(y, scale, hidden, rstd).  ``out_dtype``: a float type
+    (default: X's), or int8 / float8_e4m3fn with a scale per row in ``scale``.  ``hidden`` holds X + residual in X's type where there
+    is a residual (written to the tensor ``hidden`` if that is given, which may be X or the residual itself)."""
+    _rowmajor(X, "X")
+    N, H = X.shape
+    out_dtype = X.dtype if out_dtype is None else out_dtype
+    if hidden is None and residual is not None:
+        hidden = torch.empty((N, H), dtype=X.dtype, device=X.device)
+    Y = _out(out, (N, H), out_dtype, X.device)
+    scale = torch.empty(N, dtype=torch.float32, device=X.device) if out_dtype in (torch.int8, torch.float8_e4m3fn) else None
+    rstd = torch.empty(N, dtype=torch.float32, device=X.device) if want_rstd else None
+    r, ldr = _matrix_like(residual, (N, H), X.dtype, "residual")
+    h, ldh = _matrix_like(hidden, (N, H), X.dtype, "hidden")
+    _check(lib().sp24_rmsnorm(X.data_ptr(), r, _vector(weight, H, "weight"), float(eps), Y.data_ptr(), _ptr(scale), h, _ptr(rstd), N, H,
+                              _ld(X), ldr, _ld(Y), ldh, _DT[X.dtype], _DT[out_dtype], _stream()), "sp24_rmsnorm")
+    return RmsNorm(Y, scale, hidden, rstd)
+
+
+def sp24_quantize_rows(X, out_dtype, out=None):
+    """(codes, scale): the rows of X as int8 or float8_e4m3fn with a scale each."""
+    _rowmajor(X, "X")
+    N, H = X.shape
+    Q = _out(out, (N, H), out_dtype, X.device)
+    scale = torch.empty(N, dtype=torch.float32, device=X.device)
+    _check(lib().sp24_quantize_rows(X.data_ptr(), Q.data_ptr(), scale.data_ptr(), N, H, _ld(X), _ld(Q), _DT[X.dtype], _DT[out_dtype], _stream()),
+           "sp24_quantize_rows")
+    return Q, scale
+
+
+def sp24_rmsnorm_backward(dY, hidden, weight, rstd, dhidden=None, workspace=None, out=None):
+    """(dX, dweight) of sp24_rmsnorm from the rows ``hidden`` that it normalised (X itself without a residual) and their rstd; dX is the
+    residual's gradient too.  ``dhidden``: the gradient that reaches ``hidden`` from elsewhere."""
+    _rowmajor(dY, "dY")
+    N, H = dY.shape
+    h, ldh = _matrix_like(hidden, (N, H), dY.dtype, "hidden")
+    dh, lddh = _matrix_like(dhidden, (N, H), dY.dtype, "dhidden")
+    dX = _out(out, (N, H), dY.dtype, dY.device)
+    dweight = torch.empty(H, dtype=torch.float32, device=dY.device)
+    ws, ws_bytes = _scratch(workspace, lib().sp24_rmsnorm_backward_workspace_bytes(N, H), dY.device)
+    _check(lib().sp24_rmsnorm_backward(dY.data_ptr(), h, _vector(weight, H, "weight"), _vector(rstd, N, "rstd"), dh, dX.data_ptr(),
+                                       dweight.data_ptr(), N, H, _ld(dY), ldh, lddh, _ld(dX), _DT[dY.dtype], _ptr(ws), ws_bytes, _stream()),
+           "sp24_rmsnorm_backward")
+    return dX, dweight
+
+
+def sp24_linear(V, meta, X, out_dtype, w_scale=None, x_scale=None, bias=None, act="none", residual=None, preact=None, layout="canonical", out=None):
+    """Y [N, M] = act((X [N, K] @ decompress(V, meta).T) * w_scale * x_scale[:, None] + bias) + residual, one row per token in and out.
+    ``preact``: a tensor [N, M] of out_dtype that receives the value before the activation, for sp24_linear_backward."""
+    M, K = _compressed(V, meta)
+    _rowmajor(X, "X")
+    N = X.shape[0]
+    if X.shape[1] != K:
+        raise ValueError("inner dimensions differ")
+    _same_type(X, V, "X")
+    Y = _out(out, (N, M), out_dtype, V.device)
+    r, ldr = _matrix_like(residual, (N, M), out_dtype, "residual")
+    z, ldz = _matrix_like(preact, (N, M), out_dtype, "preact")
+    _check(lib().sp24_linear(V.data_ptr(), meta.data_ptr(), X.data_ptr(), Y.data_ptr(), M, N, K, _ld(X), _ld(Y), _vector(w_scale, M, "w_scale"),
+                             _vector(x_scale, N, "x_scale"), _vector(bias, M, "bias"), _act(act), r, ldr, z, ldz, _DT[V.dtype], _DT[out_dtype],
+                             _LAYOUT[layout], _stream()), "sp24_linear")
+    return Y
+
+
+def sp24_linear_backward(dY, preact, act, offsets=None, workspace=None):
+    """(dZ [N, M], its transpose [M, N], dbias) of a layer's result: dZ = dY * act'(preact), which is dY itself without an activation; dbias
+    [M] in float32, with ``offsets`` (of sp24_moe_sort) [experts, M].  Input's gradient: sp24_linear of dZ with the compressed transposed
+    weights; weights' gradient: sp24_gemm_dense(transpose, X, ..., b_order="n"), masked."""
+    _rowmajor(dY, "dY")
+    N, M = dY.shape
+    code = _act(act)
+    z, ldz = (None, 0) if code == NO_ACT else _matrix_like(preact, (N, M), dY.dtype, "preact")
+    experts = 0 if offsets is None else offsets.numel() - 1
+    dZ = torch.empty((N, M), dtype=dY.dtype, device=dY.device) if code != NO_ACT else None
+    dZt = torch.empty((M, N), dtype=dY.dtype, device=dY.device)
+    dbias = torch.empty((M,) if offsets is None else (experts, M), dtype=torch.float32, device=dY.device)
+    ws, ws_bytes = _scratch(workspace, lib().sp24_linear_backward_workspace_bytes(M, N, int(offsets is not None)), dY.device)
+    _check(lib().sp24_linear_backward(dY.data_ptr(), z, _ptr(dZ), dZt.data_ptr(), dbias.data_ptr(), M, N, _ld(dY), ldz, M, N, code,
+                                      _vector(offsets, experts + 1, "offsets", torch.int32), experts, _DT[dY.dtype], _ptr(ws), ws_bytes, _stream()),
+           "sp24_linear_backward")
+    return dY if dZ is None else dZ, dZt, dbias
+
+
+def sp24_moe_rows(choices, experts):
+    """Rows that ``choices`` sorted by expert may need, whatever they are."""
+    return lib().sp24_moe_rows(choices, experts)
+
+
+def sp24_moe_sort(ids, experts, workspace=None):
+    """(offsets [experts + 1], slots like ids, rows): the router's choices ids [N, topk] (int32) in order of their expert, every segment whole
+    sixteens of rows; rows[r] is a choice's number n * topk + j or -1, slots a choice's row or -1 (an id outside 0 .. experts - 1)."""
+    _dev(ids, "ids")
+    if ids.dtype != torch.int32 or not ids.is_contiguous():
+        raise ValueError("ids must be a contiguous int32 tensor")
+    T, R = ids.numel(), sp24_moe_rows(ids.numel(), experts)
+    offsets = torch.empty(max(experts, 0) + 1, dtype=torch.int32, device=ids.device)
+    slots, rows = torch.empty_like(ids), torch.empty(R, dtype=torch.int32, device=ids.device)
+    ws, ws_bytes = _scratch(workspace, lib().sp24_moe_sort_workspace_bytes(T, experts), ids.device)
+    _check(lib().sp24_moe_sort(ids.data_ptr(), offsets.data_ptr(), slots.data_ptr(), rows.data_ptr(), T, experts, R, _ptr(ws), ws_bytes, _stream()),
+           "sp24_moe_sort")
+    return offsets, slots, rows
+
+
+def sp24_moe_gather(X, rows, topk, scale=None, out=None):
+    """The rows of X [N, H] in the order of sp24_moe_sort's ``rows``, zeros where there is no choice; with ``scale`` [N] also the rows'
+    scales: (Xs, scales).  Its gradient is sp24_moe_combine(dXs, slots)."""
+    _rowmajor(X, "X")
+    N, H = X.shape
+    R = rows.numel()
+    Xs = _out(out, (R, H), X.dtype, X.device)
+    scales = torch.empty(R, dtype=torch.float32, device=X.device) if scale is not None else None
+    _check(lib().sp24_moe_gather(X.data_ptr(), _vector(scale, N, "scale"), _vector(rows, R, "rows", torch.int32), Xs.data_ptr(), _ptr(scales), N, R,
+                                 topk, H, _ld(X), _ld(Xs), _DT[X.dtype], _stream()), "sp24_moe_gather")
+    return Xs if scale is None else (Xs, scales)
+
+
+def _slots(slots):
+    _dev(slots, "slots")
+    if slots.dim() != 2 or slots.dtype != torch.int32 or not slots.is_contiguous():
+        raise ValueError("slots must be a contiguous int32 tensor [N, topk]")
+    return slots.shape
+
+
+def sp24_moe_combine(Y, slots, weights=None, residual=None, out=None):
+    """out [N, H] = residual + the rows of Y that a token's slots [N, topk] name, times weights [N, topk] (default 1)."""
+    _rowmajor(Y, "Y")
+    (R, H), (N, topk) = Y.shape, _slots(slots)
+    O = _out(out, (N, H), Y.dtype, Y.device)
+    r, ldr = _matrix_like(residual, (N, H), Y.dtype, "residual")
+    _check(lib().sp24_moe_combine(Y.data_ptr(), slots.data_ptr(), _vector(weights, N * topk, "weights"), r, O.data_ptr(), N, R, topk, H, _ld(Y), ldr,
+                                  _ld(O), _DT[Y.dtype], _stream()), "sp24_moe_combine")
+    return O
+
+
+def sp24_moe_combine_backward(dout, Y, slots, rows, weights, out=None):
+    """(dY [R, H], dweights [N, topk]) of sp24_moe_combine; the residual's gradient is dout."""
+    _rowmajor(dout, "dout"), _rowmajor(Y, "Y")
+    (R, H), (N, topk) = Y.shape, _slots(slots)
+    d, lddo = _matrix_like(dout, (N, H), Y.dtype, "dout")
+    dY = _out(out, (R, H), Y.dtype, Y.device)
+    if weights is None:
+        raise ValueError("weights must be given")
+    dweights = torch.empty((N, topk), dtype=torch.float32, device=Y.device)
+    _check(lib().sp24_moe_combine_backward(d, Y.data_ptr(), _vector(rows, R, "rows", torch.int32), slots.data_ptr(), _vector(weights, N * topk, "weights"),
+                                           dY.data_ptr(), dweights.data_ptr(), N, R, topk, H, lddo, _ld(Y), _ld(dY), _DT[Y.dtype], _stream()),
+           "sp24_moe_combine_backward")
+    return dY, dweights
+
+
+def sp24_linear_grouped(V, meta, X, offsets, out_dtype, w_scale=None, x_scale=None, bias=None, act="none", preact=None, layout="canonical", out=None):
+    """sp24_linear for the rows of every expert with that expert's weights: V [experts * M, K/2], the experts' matrices one below the
+    other, offsets as sp24_moe_sort gives them, X [R, K], Y [R, M]; rows of no expert come out zero."""
+    EM, K = _compressed(V, meta)
+    _rowmajor(X, "X"), _dev(offsets, "offsets")
+    R, experts = X.shape[0], offsets.numel() - 1
+    if experts < 1 or EM % experts != 0:
+        raise ValueError("V must hold as many rows for each of the experts, of which offsets has one entry more")
+    if X.shape[1] != K:
+        raise ValueError("inner dimensions differ")
+    _same_type(X, V, "X")
+    M = EM // experts
+    Y = _out(out, (R, M), out_dtype, V.device)
+    z, ldz = _matrix_like(preact, (R, M), out_dtype, "preact")
+    _check(lib().sp24_linear_grouped(V.data_ptr(), meta.data_ptr(), X.data_ptr(), Y.data_ptr(), _vector(offsets, experts + 1, "offsets", torch.int32),
+                                     experts, M, R, K, _ld(X), _ld(Y), _vector(w_scale, EM, "w_scale"), _vector(x_scale, R, "x_scale"),
+                                     _vector(bias, EM, "bias"), _act(act), z, ldz, _DT[V.dtype], _DT[out_dtype], _LAYOUT[layout], _stream()),
+           "sp24_linear_grouped")
+    return Y
+
+
+def sp24_gemm_dense_grouped(A, B, offsets, out_dtype, out=None):
+    """D [experts, M, N]: A [M, R] @ B [R, N] over the rows of every segment, the gradient of the experts' weights."""
+    _rowmajor(A, "A"), _rowmajor(B, "B"), _dev(offsets, "offsets")
+    (M, R), (Rb, N), experts = A.shape, B.shape, offsets.numel() - 1
+    if Rb != R:
+        raise ValueError("inner dimensions differ")
+    _same_type(B, A)
+    D = torch.empty((experts, M, N), dtype=out_dtype, device=A.device) if out is None else out
+    if out is not None and (tuple(_dev(D, "out").shape) != (experts, M, N) or D.dtype != out_dtype or not D.is_contiguous()):
+        raise ValueError("out must be a contiguous tensor [experts, M, N] of out_dtype")
+    _check(lib().sp24_gemm_dense_grouped(A.data_ptr(), B.data_ptr(), D.data_ptr(), _vector(offsets, experts + 1, "offsets", torch.int32), experts, M, N, R,
+                                         _ld(A), _ld(B), N, _DT[A.dtype], _DT[out_dtype], _stream()), "sp24_gemm_dense_grouped")
     return D
