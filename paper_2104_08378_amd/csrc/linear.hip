@@ -44,42 +44,60 @@ __global__ __launch_bounds__(64) void k_linear_any(ARGS a, int tiles_m)
         }
     }
     if (n >= a.N) return;
-    const float xs = is8<DT> && a.x_scale ? a.x_scale[n] : 1.0f;
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
         const int64_t m = m0 + 8 * g + 4 * q;
-        const int have = (int)min(a.M - m, (int64_t)4);
-        if (have <= 0) continue;
-        float scale[4], bias[4], more[4] = {}, y[4];
-        load_feature_values(is8<DT> ? a.epi.w_scale : nullptr, m, have, 1.0f, scale);
-        load_feature_values(a.epi.bias, m, have, 0.0f, bias);
-        if (a.residual) load_row_values(a.residual, n * a.ldr + m, have, a.out, more);
+        if (m >= a.M) continue;
+        typename LinearArgs::template way_out<DT, 4> out;
+        out.fetch(a, n, m);
+        float y[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) y[i] = (float)acc[4 * g + i];
-        finish_row_values<DT>(a, n, m, have, scale, bias, xs, more, y);
+        out.finish(a, n, m, y);
     }
 }
 
-template <class ARGS, class F>
-static sp24_status by_type(const ARGS& a, F&& run)
+template <class F>
+static sp24_status by_input(const MmArgs& a, F&& run)
 {
-    if (a.in == SP24_I8) run(std::integral_constant<int, SP24_I8>{});
-    else if (a.in == SP24_F8) run(std::integral_constant<int, SP24_F8>{});
-    else if (a.in == SP24_F16) run(std::integral_constant<int, SP24_F16>{});
-    else run(std::integral_constant<int, SP24_BF16>{});
-    return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
+    if (a.in == SP24_I8) return run(std::integral_constant<int, SP24_I8>{});
+    if (a.in == SP24_F8) return run(std::integral_constant<int, SP24_F8>{});
+    if (a.in == SP24_F16) return run(std::integral_constant<int, SP24_F16>{});
+    return run(std::integral_constant<int, SP24_BF16>{});
 }
 
 template <class ARGS>
 static sp24_status run_any(const ARGS& a, int64_t tiles_n, hipStream_t st)
 {
     const int64_t tiles_m = (a.M + 31) / 32;
-    return by_type(a, [&](auto dt) { k_linear_any<decltype(dt)::value, ARGS><<<(unsigned)(tiles_m * tiles_n), 64, 0, st>>>(a, (int)tiles_m); });
+    return by_input(a, [&](auto dt) {
+        k_linear_any<decltype(dt)::value, ARGS><<<(unsigned)(tiles_m * tiles_n), 64, 0, st>>>(a, (int)tiles_m);
+        return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
+    });
 }
 
-sp24_status launch_linear(const LinearArgs& a, hipStream_t st) { return run_any(a, (a.N + 31) / 32, st); }
+// What the kernels that transfer X into LDS ask of it: rows of 16 bytes, whole 32-byte runs and (canonical codes come as words) whole words.
+static bool transferable(const LinearArgs& a)
+{
+    const int64_t es = esize_of(a.in);
+    return (reinterpret_cast<uintptr_t>(a.B) & 15u) == 0 && (a.ldb * es) % 16 == 0 && a.ldb * es < ((int64_t)1 << 22) && a.K <= ((int64_t)1 << 24) &&
+           (a.layout == SP24_LAYOUT_TILED || (a.K % 32 == 0 && a.K / 2 * es * 256 < ((int64_t)1 << 31)));
+}
 
-sp24_status launch_linear_grouped(const GroupedArgs& a, hipStream_t st) { return run_any(a, grouped_tiles(a.N, a.experts, 32), st); }
+sp24_status launch_linear(const LinearArgs& a, hipStream_t st)
+{
+    if (!transferable(a)) return run_any(a, (a.N + 31) / 32, st);
+    const int64_t tiles = (a.M + 127) / 128;
+    if (stream_workgroups(a) <= 256 || (a.N <= 32 && tiles < 86)) return launch_linear_stream(a, st);
+    return by_input(a, [&](auto dt) { return linear_tiled<decltype(dt)::value>(a, st); });
+}
+
+sp24_status launch_linear_grouped(const GroupedArgs& a, hipStream_t st)
+{
+    if (!transferable(a)) return run_any(a, grouped_tiles(a.N, a.experts, 32), st);
+    if (a.N <= 32 * (int64_t)a.experts) return launch_grouped_stream(a, st);
+    return by_input(a, [&](auto dt) { return grouped_tiled<decltype(dt)::value>(a, st); });
+}
 
 // The segments' dense products, A [M, rows] and B [rows, N]: 128 x 128 tiles, all segments in one launch.
 template <int DT, int OUT>

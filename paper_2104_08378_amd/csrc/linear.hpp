@@ -20,6 +20,7 @@ struct LinearArgs : MmArgs {            // MmArgs::B = X, D = Y, ldd = ldy; epi.
     int act;
 
     template <int BM, int BN> __device__ __forceinline__ bool enter(int, int&) { return true; }
+    template <int DT, int COUNT> struct way_out;
     template <int TM> static constexpr int wave_bytes();
     template <int DT, int TM, int TN>
     __device__ __forceinline__ void store_wave(typename acc_of<DT>::type (&acc)[TM][TN], uint8_t* scratch, int64_t row_base, int64_t col_base, int lane) const;
@@ -213,6 +214,26 @@ __device__ __forceinline__ void load_feature_values(const float* p, int64_t m, i
     for (int i = 0; i < COUNT; ++i) v[i] = p && i < have ? p[m + i] : otherwise;
 }
 
+// COUNT neighbouring features of token n's row on their way out; what has to be read for them can be asked for before the sums are there.
+template <int DT, int COUNT>
+struct LinearArgs::way_out {
+    float scale[COUNT], bias[COUNT], more[COUNT], x_scale;
+    __device__ __forceinline__ void fetch(const LinearArgs& a, int64_t n, int64_t m)
+    {
+        const int have = (int)min(a.M - m, (int64_t)COUNT);
+        load_feature_values(is8<DT> ? a.epi.w_scale : nullptr, m, have, 1.0f, scale);
+        load_feature_values(a.epi.bias, m, have, 0.0f, bias);
+        x_scale = is8<DT> && a.x_scale ? a.x_scale[n] : 1.0f;
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) more[i] = 0.0f;
+        if (a.residual) load_row_values(a.residual, n * a.ldr + m, have, a.out, more);
+    }
+    __device__ __forceinline__ void finish(const LinearArgs& a, int64_t n, int64_t m, float (&v)[COUNT]) const
+    {
+        finish_row_values<DT>(a, n, m, (int)min(a.M - m, (int64_t)COUNT), scale, bias, x_scale, more, v);
+    }
+};
+
 // A wavefront's tile on its way out, 32 tokens at a time: the sums go to LDS in binary32 as rows of 32 TM features and come back eight
 // neighbouring ones to a lane, so that every global access is 16 bytes and covers whole lines of a token's row.  Rows are 16 bytes
 // longer than their values: 16 lanes that write 16 bytes of 16 rows, or read 16 of 2 rows, meet every bank once.
@@ -250,5 +271,11 @@ __device__ __forceinline__ void LinearArgs::store_wave(typename acc_of<DT>::type
         }
     }
 }
+
+// ---- host side: the tiled and the streaming kernels, compiled per input type ----
+template <int DT> sp24_status linear_tiled(const LinearArgs& a, hipStream_t st);
+template <int DT> sp24_status grouped_tiled(const GroupedArgs& a, hipStream_t st);
+sp24_status launch_linear_stream(const LinearArgs& a, hipStream_t st);
+sp24_status launch_grouped_stream(const GroupedArgs& a, hipStream_t st);
 
 } // namespace sp24

@@ -1,0 +1,8 @@
+// Rows of experts on the tiled kernels, bf16 inputs.
+#include "linear_tiled.hpp"
+
+namespace sp24 {
+
+template sp24_status grouped_tiled<SP24_BF16>(const GroupedArgs& a, hipStream_t st);
+
+} // namespace sp24

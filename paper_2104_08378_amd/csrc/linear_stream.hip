@@ -1,0 +1,43 @@
+// Layers with few tokens, and the rows of experts that have few each, on the kernel that splits K across a workgroup's wavefronts.
+#include "linear.hpp"
+#include "mm_stream.hpp"
+
+namespace sp24 {
+
+template <int DT, int BR, int NW, int NS, class ARGS>
+static sp24_status run_layer_stream(const ARGS& a, hipStream_t st)
+{
+    const int64_t tiles_m = (a.M + 31) / 32;
+    int64_t tiles_n;
+    if constexpr (std::is_same<ARGS, GroupedArgs>::value) tiles_n = grouped_tiles(a.N, a.experts, BR);
+    else tiles_n = (a.N + BR - 1) / BR;
+    k_spmm_stream<DT, BR, NW, NS, false, ARGS><<<(unsigned)(tiles_m * tiles_n), 64 * NW, 0, st>>>(a, (int)tiles_m, (int)tiles_n);
+    return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
+}
+
+template <class ARGS, class F>
+static sp24_status by_input(const ARGS& a, F&& run)
+{
+    if (a.in == SP24_I8) return run(std::integral_constant<int, SP24_I8>{});
+    if (a.in == SP24_F8) return run(std::integral_constant<int, SP24_F8>{});
+    if (a.in == SP24_F16) return run(std::integral_constant<int, SP24_F16>{});
+    return run(std::integral_constant<int, SP24_BF16>{});
+}
+
+sp24_status launch_linear_stream(const LinearArgs& a, hipStream_t st)
+{
+    return by_input(a, [&](auto dt) {
+        constexpr int DT = decltype(dt)::value;
+        const int columns = stream_columns(a);
+        if (columns == 16) return run_layer_stream<DT, 16, 8, 4>(a, st);
+        if (columns == 32) return run_layer_stream<DT, 32, 8, 3>(a, st);
+        return run_layer_stream<DT, 64, 7, 2>(a, st);
+    });
+}
+
+sp24_status launch_grouped_stream(const GroupedArgs& a, hipStream_t st)
+{
+    return by_input(a, [&](auto dt) { return run_layer_stream<decltype(dt)::value, 16, 8, 4>(a, st); });
+}
+
+} // namespace sp24

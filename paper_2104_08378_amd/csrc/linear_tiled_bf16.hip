@@ -1,0 +1,8 @@
+// Layers on the tiled kernels, bf16 inputs.
+#include "linear_tiled.hpp"
+
+namespace sp24 {
+
+template sp24_status linear_tiled<SP24_BF16>(const LinearArgs& a, hipStream_t st);
+
+} // namespace sp24

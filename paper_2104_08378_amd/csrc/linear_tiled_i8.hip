@@ -1,0 +1,8 @@
+// Layers on the tiled kernels, i8 inputs.
+#include "linear_tiled.hpp"
+
+namespace sp24 {
+
+template sp24_status linear_tiled<SP24_I8>(const LinearArgs& a, hipStream_t st);
+
+} // namespace sp24
