@@ -537,7 +537,7 @@ sp24_status sp24_moe_sort(const int32_t* ids, int32_t* offsets, int32_t* slots, 
 
 /*
  * Xs[r][:] = X[rows[r] / topk][:], bit for bit; zeros where rows[r] is -1 (or names no token).  X: N x H, Xs: row_count x H of type t (any but SP24_I32).
- * scale (NULL: none), scale_out: the rows' scales alike, 0 for rows of no choice.  The gradient of X is sp24_moe_combine of Xs's with weights NULL.
+ * scale and scale_out (both NULL: none): the rows' scales alike, 0 for rows of no choice.  The gradient of X is sp24_moe_combine of Xs's with weights NULL.
  */
 sp24_status sp24_moe_gather(const void* X, const float* scale, const int32_t* rows, void* Xs, float* scale_out, int64_t N,
                             int64_t row_count, int topk, int64_t H, int64_t ldx, int64_t ldxs, sp24_dtype t, void* stream);

@@ -18,6 +18,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsp24.so")
 HOST = os.path.join(HERE, "_sp24_host.so")      # native marshalling of the binding's calls (csrc/host_calls.cpp)
 PROBE = os.path.join(HERE, "sp24_probe")        # stand-alone measurement of the chip's ceilings (csrc/probe.hip)
+HOST_SOURCES = ["host_calls.cpp", "host_layers.cpp"]
 _TYPES = ("f16", "bf16", "i8", "f8")
 SOURCES = ["api.hip", "api_layers.hip", "norm.hip", "linear.hip", "linear_stream.hip", "linear_grad.hip", "experts.hip", "prune_compress.hip", "permute.hip", "permute_search.hip", "permute_search_columns.hip", "splitk.hip", "mm_simple.hip", "mm_ksplit.hip", "conv_narrow.hip", "mm_skinny.hip", "mm_stream.hip", "mm_tiled.hip", "mm_staged.hip",
            "mm_staged_f16.hip", "mm_staged_bf16.hip", "mm_staged_i8.hip", "mm_staged_f8.hip"] + [
@@ -62,10 +63,11 @@ def build(verbose=False):
         objs.append(obj)
     probe_cmd = ["hipcc", *[f for f in FLAGS if f != "-fPIC"], os.path.join(CSRC, "probe.hip"), "-o", PROBE]
     procs.append(("probe.hip", subprocess.Popen(probe_cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
-    host, host_obj = host_flags(), os.path.join(CSRC, "host_calls.o")
-    if host:
-        procs.append(("host_calls.cpp", subprocess.Popen(["g++", *host[0], "-c", os.path.join(CSRC, "host_calls.cpp"), "-o", host_obj],
-                                                         stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+    host, host_objs = host_flags(), []
+    for src in HOST_SOURCES if host else ():
+        host_objs.append(os.path.join(CSRC, src.replace(".cpp", ".o")))
+        procs.append((src, subprocess.Popen(["g++", *host[0], "-c", os.path.join(CSRC, src), "-o", host_objs[-1]],
+                                            stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
     failed = False
     for src, p in procs:
         out, _ = p.communicate()
@@ -79,7 +81,7 @@ def build(verbose=False):
         raise RuntimeError("libsp24 build failed")
     subprocess.check_call(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs])
     if host:
-        subprocess.check_call(["g++", "-shared", "-o", HOST, host_obj, *host[1]])
+        subprocess.check_call(["g++", "-shared", "-o", HOST, *host_objs, *host[1]])
     else:
         print("torch or its headers are missing: _sp24_host.so is not built", file=sys.stderr)
         if os.path.exists(HOST):

@@ -314,12 +314,12 @@ sp24_status sp24_moe_gather(const void* X, const float* scale, const int32_t* ro
     SP24_TRY(check_matrix(X, N, H, ldx, es, false));
     SP24_TRY(check_matrix(Xs, row_count, H, ldxs, es, false));
     SP24_TRY(check_vector(rows));
-    if (scale) {
-        SP24_TRY(check_vector(scale));
+    if (scale || scale_out) {
+        if (N > 0) SP24_TRY(check_vector(scale));               // (no tokens: no choice has one, and the scales are zeros)
         SP24_TRY(check_vector(scale_out));
     }
     const Span x = matrix(X, N, H, ldx, es), xs = matrix(Xs, row_count, H, ldxs, es), ro = vec(rows, row_count, 4), sc = vec(scale, N, 4),
-               so = vec(scale ? scale_out : nullptr, row_count, 4);
+               so = vec(scale_out, row_count, 4);
     if (overlaps(xs, {x, ro, sc, so}) || overlaps(so, {x, ro, sc})) return SP24_ERR_SHAPE;
     return launch_moe_gather(GatherArgs{X, scale, rows, Xs, scale_out, N, row_count, H * es, ldx * es, ldxs * es, topk}, static_cast<hipStream_t>(stream));
 }

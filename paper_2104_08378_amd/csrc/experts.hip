@@ -221,7 +221,7 @@ __global__ __launch_bounds__(256) void k_moe_gather(GatherArgs a, int blocks_a_r
     const int64_t at = ((int64_t)(blockIdx.x % blocks_a_row) * blockDim.x + threadIdx.x) * 16;
     const int64_t choice = a.rows[row], token = choice < 0 ? -1 : choice / a.topk;
     const bool live = token >= 0 && token < a.N;
-    if (a.scale && at == 0) a.scale_out[row] = live ? a.scale[token] : 0.0f;
+    if (a.scale_out && at == 0) a.scale_out[row] = live ? a.scale[token] : 0.0f;
     if (at >= a.row_bytes) return;
     const int64_t n = a.row_bytes - at;
     const uint4v v = live ? load_bytes(reinterpret_cast<const uint8_t*>(a.X) + token * a.ldx_bytes + at, n) : uint4v{0u, 0u, 0u, 0u};

@@ -686,6 +686,9 @@ def sp24_rmsnorm(X, weight, eps=1e-6, residual=None, out_dtype=None, want_rstd=F
     """Root-mean-square norm of the rows of X (plus ``residual``): RmsNorm(y, scale, hidden, rstd).  ``out_dtype``: a float type
     (default: X's), or int8 / float8_e4m3fn with a scale per row in ``scale``.  ``hidden`` holds X + residual in X's type where there
     is a residual (written to the tensor ``hidden`` if that is given, which may be X or the residual itself)."""
+    done = (_host or _load_host()).sp24_rmsnorm(X, weight, eps, residual, out_dtype, want_rstd, hidden, out)
+    if done is not None:
+        return RmsNorm._make(done)
     _rowmajor(X, "X")
     N, H = X.shape
     out_dtype = X.dtype if out_dtype is None else out_dtype
@@ -703,6 +706,9 @@ def sp24_rmsnorm(X, weight, eps=1e-6, residual=None, out_dtype=None, want_rstd=F
 
 def sp24_quantize_rows(X, out_dtype, out=None):
     """(codes, scale): the rows of X as int8 or float8_e4m3fn with a scale each."""
+    done = (_host or _load_host()).sp24_quantize_rows(X, out_dtype, out)
+    if done is not None:
+        return done
     _rowmajor(X, "X")
     N, H = X.shape
     Q = _out(out, (N, H), out_dtype, X.device)
@@ -715,6 +721,9 @@ def sp24_quantize_rows(X, out_dtype, out=None):
 def sp24_rmsnorm_backward(dY, hidden, weight, rstd, dhidden=None, workspace=None, out=None):
     """(dX, dweight) of sp24_rmsnorm from the rows ``hidden`` that it normalised (X itself without a residual) and their rstd; dX is the
     residual's gradient too.  ``dhidden``: the gradient that reaches ``hidden`` from elsewhere."""
+    done = (_host or _load_host()).sp24_rmsnorm_backward(dY, hidden, weight, rstd, dhidden, workspace, out)
+    if done is not None:
+        return done
     _rowmajor(dY, "dY")
     N, H = dY.shape
     h, ldh = _matrix_like(hidden, (N, H), dY.dtype, "hidden")
@@ -731,6 +740,9 @@ def sp24_rmsnorm_backward(dY, hidden, weight, rstd, dhidden=None, workspace=None
 def sp24_linear(V, meta, X, out_dtype, w_scale=None, x_scale=None, bias=None, act="none", residual=None, preact=None, layout="canonical", out=None):
     """Y [N, M] = act((X [N, K] @ decompress(V, meta).T) * w_scale * x_scale[:, None] + bias) + residual, one row per token in and out.
     ``preact``: a tensor [N, M] of out_dtype that receives the value before the activation, for sp24_linear_backward."""
+    done = (_host or _load_host()).sp24_linear(V, meta, X, out_dtype, w_scale, x_scale, bias, act, residual, preact, layout, out)
+    if done is not None:
+        return done
     M, K = _compressed(V, meta)
     _rowmajor(X, "X")
     N = X.shape[0]
@@ -750,6 +762,9 @@ def sp24_linear_backward(dY, preact, act, offsets=None, workspace=None):
     """(dZ [N, M], its transpose [M, N], dbias) of a layer's result: dZ = dY * act'(preact), which is dY itself without an activation; dbias
     [M] in float32, with ``offsets`` (of sp24_moe_sort) [experts, M].  Input's gradient: sp24_linear of dZ with the compressed transposed
     weights; weights' gradient: sp24_gemm_dense(transpose, X, ..., b_order="n"), masked."""
+    done = (_host or _load_host()).sp24_linear_backward(dY, preact, act, offsets, workspace)
+    if done is not None:
+        return done
     _rowmajor(dY, "dY")
     N, M = dY.shape
     code = _act(act)
@@ -773,6 +788,9 @@ def sp24_moe_rows(choices, experts):
 def sp24_moe_sort(ids, experts, workspace=None):
     """(offsets [experts + 1], slots like ids, rows): the router's choices ids [N, topk] (int32) in order of their expert, every segment whole
     sixteens of rows; rows[r] is a choice's number n * topk + j or -1, slots a choice's row or -1 (an id outside 0 .. experts - 1)."""
+    done = (_host or _load_host()).sp24_moe_sort(ids, experts, workspace)
+    if done is not None:
+        return done
     _dev(ids, "ids")
     if ids.dtype != torch.int32 or not ids.is_contiguous():
         raise ValueError("ids must be a contiguous int32 tensor")
@@ -788,6 +806,9 @@ def sp24_moe_sort(ids, experts, workspace=None):
 def sp24_moe_gather(X, rows, topk, scale=None, out=None):
     """The rows of X [N, H] in the order of sp24_moe_sort's ``rows``, zeros where there is no choice; with ``scale`` [N] also the rows'
     scales: (Xs, scales).  Its gradient is sp24_moe_combine(dXs, slots)."""
+    done = (_host or _load_host()).sp24_moe_gather(X, rows, topk, scale, out)
+    if done is not None:
+        return done
     _rowmajor(X, "X")
     N, H = X.shape
     R = rows.numel()
@@ -807,6 +828,9 @@ def _slots(slots):
 
 def sp24_moe_combine(Y, slots, weights=None, residual=None, out=None):
     """out [N, H] = residual + the rows of Y that a token's slots [N, topk] name, times weights [N, topk] (default 1)."""
+    done = (_host or _load_host()).sp24_moe_combine(Y, slots, weights, residual, out)
+    if done is not None:
+        return done
     _rowmajor(Y, "Y")
     (R, H), (N, topk) = Y.shape, _slots(slots)
     O = _out(out, (N, H), Y.dtype, Y.device)
@@ -818,6 +842,9 @@ def sp24_moe_combine(Y, slots, weights=None, residual=None, out=None):
 
 def sp24_moe_combine_backward(dout, Y, slots, rows, weights, out=None):
     """(dY [R, H], dweights [N, topk]) of sp24_moe_combine; the residual's gradient is dout."""
+    done = (_host or _load_host()).sp24_moe_combine_backward(dout, Y, slots, rows, weights, out)
+    if done is not None:
+        return done
     _rowmajor(dout, "dout"), _rowmajor(Y, "Y")
     (R, H), (N, topk) = Y.shape, _slots(slots)
     d, lddo = _matrix_like(dout, (N, H), Y.dtype, "dout")
@@ -834,6 +861,9 @@ def sp24_moe_combine_backward(dout, Y, slots, rows, weights, out=None):
 def sp24_linear_grouped(V, meta, X, offsets, out_dtype, w_scale=None, x_scale=None, bias=None, act="none", preact=None, layout="canonical", out=None):
     """sp24_linear for the rows of every expert with that expert's weights: V [experts * M, K/2], the experts' matrices one below the
     other, offsets as sp24_moe_sort gives them, X [R, K], Y [R, M]; rows of no expert come out zero."""
+    done = (_host or _load_host()).sp24_linear_grouped(V, meta, X, offsets, out_dtype, w_scale, x_scale, bias, act, preact, layout, out)
+    if done is not None:
+        return done
     EM, K = _compressed(V, meta)
     _rowmajor(X, "X"), _dev(offsets, "offsets")
     R, experts = X.shape[0], offsets.numel() - 1
@@ -854,6 +884,9 @@ def sp24_linear_grouped(V, meta, X, offsets, out_dtype, w_scale=None, x_scale=No
 
 def sp24_gemm_dense_grouped(A, B, offsets, out_dtype, out=None):
     """D [experts, M, N]: A [M, R] @ B [R, N] over the rows of every segment, the gradient of the experts' weights."""
+    done = (_host or _load_host()).sp24_gemm_dense_grouped(A, B, offsets, out_dtype, out)
+    if done is not None:
+        return done
     _rowmajor(A, "A"), _rowmajor(B, "B"), _dev(offsets, "offsets")
     (M, R), (Rb, N), experts = A.shape, B.shape, offsets.numel() - 1
     if Rb != R:
