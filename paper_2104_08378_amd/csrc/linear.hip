@@ -1,5 +1,6 @@
 // Layers on the sparse product: the kernel for operands at any alignment, and which kernel takes what.
 #include <algorithm>
+#include <cmath>
 
 #include "linear.hpp"
 
@@ -57,15 +58,6 @@ __global__ __launch_bounds__(64) void k_linear_any(ARGS a, int tiles_m)
     }
 }
 
-template <class F>
-static sp24_status by_input(const MmArgs& a, F&& run)
-{
-    if (a.in == SP24_I8) return run(std::integral_constant<int, SP24_I8>{});
-    if (a.in == SP24_F8) return run(std::integral_constant<int, SP24_F8>{});
-    if (a.in == SP24_F16) return run(std::integral_constant<int, SP24_F16>{});
-    return run(std::integral_constant<int, SP24_BF16>{});
-}
-
 template <class ARGS>
 static sp24_status run_any(const ARGS& a, int64_t tiles_n, hipStream_t st)
 {
@@ -84,19 +76,79 @@ static bool transferable(const LinearArgs& a)
            (a.layout == SP24_LAYOUT_TILED || (a.K % 32 == 0 && a.K / 2 * es * 256 < ((int64_t)1 << 31)));
 }
 
+// Which kernel: the least of estimates of the form  base + max(steps * alone, (steps * step + tile) * workgroups / units)  in us, a step being
+// 128 bytes of K: one workgroup's own time, and what the workgroups of a compute unit (several at a time, except where they come in whole
+// rounds) take of it together.  Fitted to 970 layers and 1050 sets of experts' rows of 128 - 16384 rows of weights, K 256 - 8192, 1 - 16384 rows, all
+// types, from HBM: within 9 - 13 % of the measured time on average, and the choice within 3.9 % of the best of twelve kernels (layers; at worst 1.5
+// times) and 3.7 % (experts).  One shape throughout costs 26 % (64 x 32), 13 % (128 x 128 besides), 6 % (the streaming kernel besides).  E.g.
+// bf16, us: 1664 x 1158 x 1728 10.0 on 128 x 64 and 12.8 on 128 x 128; 13275 x 2198 x 384 42 and 52; experts of 4096 x 4096 on 32 rows of eight
+// segments 29.3 on 64 x 32 and 36.4 on the streaming kernel, whose workgroups come one to a unit.
+struct LayerCost {
+    LayerTile tile;
+    int rows, columns;
+    bool whole_rounds;
+    double base, alone, step, each;                             // tiled layout
+    double c_base, c_alone, c_step, c_each;                     // canonical
+};
+constexpr LayerCost kLayerCosts[] = {
+    {LayerTile::stream, 32, 16, true, 3.5, 0.034, 0.09, 0.45, 3.5, 0.05, 0.10, 0.5},
+    {LayerTile::stream, 32, 32, true, 3.6, 0.042, 0.071, 0.8, 3.5, 0.056, 0.097, 1.0},
+    {LayerTile::stream, 32, 64, true, 3.6, 0.114, 0.098, 2.6, 3.9, 0.111, 0.117, 2.6},
+    {LayerTile::t64x32, 64, 32, false, 3.8, 0.12, 0.092, 0.74, 4.1, 0.10, 0.17, 0.48},
+    {LayerTile::t128x64, 128, 64, false, 4.5, 0.16, 0.24, 2.2, 5.1, 0.19, 0.47, 1.5},
+    {LayerTile::t128x128, 128, 128, false, 4.8, 0.26, 0.43, 2.4, 5.4, 0.35, 0.74, 1.0},
+    {LayerTile::t256x128, 256, 128, true, 7.3, 0.32, 0.80, 1.0, 7.4, 0.57, 1.25, 1.0},
+};
+
+// workgroups(cost): of the launch, as far as the host knows
+template <class F>
+static LayerTile cheapest(const MmArgs& a, int stream_width, bool grouped, F&& workgroups)
+{
+    const double steps = (double)a.K * esize_of(a.in) / 128;
+    double least = 0;
+    LayerTile best = LayerTile::t64x32;
+    for (const LayerCost& c : kLayerCosts) {
+        if (c.tile == LayerTile::stream && c.columns != stream_width) continue;
+        if (c.tile == LayerTile::t256x128 && grouped) continue;
+        const bool canonical = a.layout == SP24_LAYOUT_CANONICAL;
+        double units = workgroups(c) / 256;
+        if (c.whole_rounds && units > 1) units = std::ceil(units);
+        const double us = (canonical ? c.c_base : c.base) + std::max(steps * (canonical ? c.c_alone : c.alone),
+                                                                      (steps * (canonical ? c.c_step : c.step) + (canonical ? c.c_each : c.each)) * units);
+        if (least == 0 || us < least) {
+            least = us;
+            best = c.tile;
+        }
+    }
+    return best;
+}
+
 sp24_status launch_linear(const LinearArgs& a, hipStream_t st)
 {
     if (!transferable(a)) return run_any(a, (a.N + 31) / 32, st);
-    const int64_t tiles = (a.M + 127) / 128;
-    if (stream_workgroups(a) <= 256 || (a.N <= 32 && tiles < 86)) return launch_linear_stream(a, st);
-    return by_input(a, [&](auto dt) { return linear_tiled<decltype(dt)::value>(a, st); });
+    // 256 x 256 tiles where the plain product takes them, and four steps at least (two: 24.5 - 35 us against 20 - 25 on 128 x 128)
+    const int64_t big = ((a.M + 255) / 256) * ((a.N + 255) / 256);
+    const double cover_big = (double)(((a.M + 255) / 256) * 256) * (double)(((a.N + 255) / 256) * 256);
+    const double cover_small = (double)(((a.M + 127) / 128) * 128) * (double)(((a.N + 127) / 128) * 128);
+    LayerTile tile = LayerTile::t256x256;
+    if (!(big >= 129 && cover_big <= 1.35 * cover_small && a.K * esize_of(a.in) >= 4 * 128))
+        tile = cheapest(a, stream_columns(a), false, [&](const LayerCost& c) { return (double)((a.M + c.rows - 1) / c.rows) * (double)((a.N + c.columns - 1) / c.columns); });
+    if (tile == LayerTile::stream) return launch_linear_stream(a, st);
+    return by_input(a, [&](auto dt) { return layer_tiled<decltype(dt)::value>(a, tile, st); });
 }
 
 sp24_status launch_linear_grouped(const GroupedArgs& a, hipStream_t st)
 {
     if (!transferable(a)) return run_any(a, grouped_tiles(a.N, a.experts, 32), st);
-    if (a.N <= 32 * (int64_t)a.experts) return launch_grouped_stream(a, st);
-    return by_input(a, [&](auto dt) { return grouped_tiled<decltype(dt)::value>(a, st); });
+    // The host knows the rows' number at most: a segment is taken to end in the middle of its last sixteen and of its last tile.
+    const double live = (double)std::min<int64_t>(a.experts, a.N / kSegmentRows), rows = (double)a.N - 8 * live;
+    auto columns = [&](int width) { return width == 16 ? (double)a.N / 16 : std::max(live, rows / width + 0.5 * live * (1 - 16.0 / width)); };
+    LayerTile tile = cheapest(a, 16, true, [&](const LayerCost& c) { return (double)((a.M + c.rows - 1) / c.rows) * columns(c.columns); });
+    // 256 x 256 where they make one round and have many steps: 0.84 - 0.96 of the others' time (with fewer of either up to 1.3)
+    const double big = (double)((a.M + 255) / 256) * columns(256);
+    if (big >= 129 && big <= 200 && a.K * esize_of(a.in) >= 24 * 128) tile = LayerTile::t256x256;
+    if (tile == LayerTile::stream) return launch_grouped_stream(a, st);
+    return by_input(a, [&](auto dt) { return layer_tiled<decltype(dt)::value>(a, tile, st); });
 }
 
 // The segments' dense products, A [M, rows] and B [rows, N]: 128 x 128 tiles, all segments in one launch.

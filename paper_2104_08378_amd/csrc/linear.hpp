@@ -21,9 +21,26 @@ struct LinearArgs : MmArgs {            // MmArgs::B = X, D = Y, ldd = ldy; epi.
 
     template <int BM, int BN> __device__ __forceinline__ bool enter(int, int&) { return true; }
     template <int DT, int COUNT> struct way_out;
+    // Bias and scales of a tile's BM features wait in LDS for the way out: transferred ahead of everything else, there with the first operands.
+    template <int DT, int BM> static constexpr int vector_bytes() { return (is8<DT> ? 2 : 1) * BM * 4; }
+    template <int DT, int BM, int NW> __device__ __forceinline__ void fetch_vectors(uint8_t* lds, int64_t m0, int wave, int lane) const
+    {
+#pragma unroll
+        for (int v = 0; v < (is8<DT> ? 2 : 1); ++v) {
+            const float* const p = v == 0 ? epi.bias : epi.w_scale;
+#pragma unroll
+            for (int x = 0; x < (BM / 64 + NW - 1) / NW; ++x) {
+                const int part = wave + x * NW;
+                if (!p || part >= BM / 64) continue;
+                lds_dma4_addr(reinterpret_cast<const uint8_t*>(p + min(m0 + part * 64 + lane, M - 1)), lds + v * BM * 4 + part * 256);
+            }
+        }
+    }
     template <int TM> static constexpr int wave_bytes();
+    // vectors: where fetch_vectors put them, the wavefront's first feature of BM being `first`
     template <int DT, int TM, int TN>
-    __device__ __forceinline__ void store_wave(typename acc_of<DT>::type (&acc)[TM][TN], uint8_t* scratch, int64_t row_base, int64_t col_base, int lane) const;
+    __device__ __forceinline__ void store_wave(typename acc_of<DT>::type (&acc)[TM][TN], uint8_t* scratch, const uint8_t* vectors, int BM, int first,
+                                               int64_t row_base, int64_t col_base, int lane) const;
 };
 
 constexpr int kSegmentRows = 16;        // segments begin at multiples of this
@@ -149,10 +166,18 @@ __device__ __forceinline__ void load_row_values(const void* p, int64_t at, int n
     }
 }
 
+// past_l2: the values lie on 16-byte boundaries and are not read again by this launch
 template <int COUNT>
-__device__ __forceinline__ void store_row_values(void* p, int64_t at, int n, sp24_dtype t, const float (&v)[COUNT])
+__device__ __forceinline__ void store_row_values(void* p, int64_t at, int n, sp24_dtype t, bool past_l2, const float (&v)[COUNT])
 {
     if constexpr (COUNT == 8) {
+        if (past_l2 && n >= 8 && t != SP24_F32) {
+            uint4v q;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q[i] = t == SP24_BF16 ? pack_out16<SP24_BF16>(v[2 * i], v[2 * i + 1]) : pack_out16<SP24_F16>(v[2 * i], v[2 * i + 1]);
+            __builtin_nontemporal_store(q, reinterpret_cast<uint4v*>(reinterpret_cast<uint16_t*>(p) + at));
+            return;
+        }
         if (t == SP24_F32) store_values8<SP24_F32>(p, at, n, v);
         else if (t == SP24_BF16) store_values8<SP24_BF16>(p, at, n, v);
         else store_values8<SP24_F16>(p, at, n, v);
@@ -187,23 +212,20 @@ __device__ __forceinline__ void store_row_values(void* p, int64_t at, int n, sp2
 // The way out of COUNT neighbouring values of token n's row, from feature m on (`have` of them exist): `v` are the sums.
 template <int DT, int COUNT>
 __device__ __forceinline__ void finish_row_values(const LinearArgs& a, int64_t n, int64_t m, int have, const float (&scale)[COUNT], const float (&bias)[COUNT],
-                                                  float x_scale, const float (&more)[COUNT], float (&v)[COUNT])
+                                                  float x_scale, const float (&more)[COUNT], bool past_l2, float (&v)[COUNT])
 {
 #pragma unroll
     for (int i = 0; i < COUNT; ++i) {
         if constexpr (is8<DT>) v[i] = __builtin_fmaf(v[i] * scale[i], x_scale, bias[i]);
         else v[i] += bias[i];
     }
-    if (a.Z) store_row_values(a.Z, n * a.ldz + m, have, a.out, v);
-    if (a.act != SP24_ACT_NONE) {
-#pragma unroll
-        for (int i = 0; i < COUNT; ++i) v[i] = activate(v[i], a.act);
-    }
+    if (a.Z) store_row_values(a.Z, n * a.ldz + m, have, a.out, past_l2, v);
+    activate(v, a.act);
     if (a.residual) {
 #pragma unroll
         for (int i = 0; i < COUNT; ++i) v[i] += more[i];
     }
-    store_row_values(a.D, n * a.ldd + m, have, a.out, v);
+    store_row_values(a.D, n * a.ldd + m, have, a.out, past_l2, v);
 }
 
 // COUNT values of a vector over the features, `otherwise` where there is none
@@ -230,9 +252,19 @@ struct LinearArgs::way_out {
     }
     __device__ __forceinline__ void finish(const LinearArgs& a, int64_t n, int64_t m, float (&v)[COUNT]) const
     {
-        finish_row_values<DT>(a, n, m, (int)min(a.M - m, (int64_t)COUNT), scale, bias, x_scale, more, v);
+        finish_row_values<DT>(a, n, m, (int)min(a.M - m, (int64_t)COUNT), scale, bias, x_scale, more, false, v);
     }
 };
+
+// f(integral_constant<int, 0>{}), ..., f(integral_constant<int, N - 1>{})
+template <int N, class F>
+__device__ __forceinline__ void count_up(F&& f)
+{
+    if constexpr (N > 0) {
+        count_up<N - 1>(f);
+        f(std::integral_constant<int, N - 1>{});
+    }
+}
 
 // A wavefront's tile on its way out, 32 tokens at a time: the sums go to LDS in binary32 as rows of 32 TM features and come back eight
 // neighbouring ones to a lane, so that every global access is 16 bytes and covers whole lines of a token's row.  Rows are 16 bytes
@@ -240,17 +272,35 @@ struct LinearArgs::way_out {
 template <int TM> constexpr int LinearArgs::wave_bytes() { return 32 * (TM * 128 + 16); }
 
 template <int DT, int TM, int TN>
-__device__ __forceinline__ void LinearArgs::store_wave(typename acc_of<DT>::type (&acc)[TM][TN], uint8_t* scratch, int64_t row_base, int64_t col_base, int lane) const
+__device__ __forceinline__ void LinearArgs::store_wave(typename acc_of<DT>::type (&acc)[TM][TN], uint8_t* scratch, const uint8_t* vectors, int BM, int first,
+                                                       int64_t row_base, int64_t col_base, int lane) const
 {
     constexpr int kPitch = TM * 128 + 16, CH = 4 * TM;            // chunks of eight features to a row
+    constexpr int IT = 32 * CH / 64, kRows = 64 / CH;             // instructions to 32 tokens, tokens to one
     const int r = lane & 31, q = lane >> 5, c = lane % CH;
     const int64_t m = row_base + c * 8;
     const int have = (int)min(M - m, (int64_t)8);
+    // Y (and Z) go past the L2, which keeps the panels that neighbouring tiles share: 4096 x 8192 x 1024 bf16 with GELU 54.7 -> 52.8 us,
+    // 8192 x 4096 x 4096 with SiLU 143.6 -> 132.1
+    const bool past_l2 = ((reinterpret_cast<uintptr_t>(D) | reinterpret_cast<uintptr_t>(Z)) & 15u) == 0 && ldd % 8 == 0 && (!Z || ldz % 8 == 0);
     float scale[8], b[8];
-    load_feature_values(is8<DT> ? epi.w_scale : nullptr, m, have, 1.0f, scale);
-    load_feature_values(epi.bias, m, have, 0.0f, b);
 #pragma unroll
-    for (int j = 0; j < TN; ++j) {
+    for (int i = 0; i < 8; ++i) {
+        const float* const v = reinterpret_cast<const float*>(vectors) + first + c * 8 + i;
+        b[i] = epi.bias ? v[0] : 0.0f;
+        scale[i] = is8<DT> && epi.w_scale ? v[BM] : 1.0f;
+    }
+    // (as calls, not a loop: a loop of this size the compiler may leave rolled, and then keeps the sums in memory)
+    count_up<TN>([&](auto j_c) __attribute__((always_inline)) {
+        constexpr int j = decltype(j_c)::value;
+        const int64_t n0 = col_base + j * 32 + lane / CH;
+        float more[IT][8], xs[IT];
+#pragma unroll
+        for (int it = 0; it < IT; ++it) {                          // on their way while the sums take the turn through LDS
+            const int64_t n = min(n0 + it * kRows, N - 1);
+            xs[it] = is8<DT> && x_scale ? x_scale[n] : 1.0f;
+            if (residual) load_row_values(residual, n * ldr + m, have, out, more[it]);
+        }
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -259,23 +309,31 @@ __device__ __forceinline__ void LinearArgs::store_wave(typename acc_of<DT>::type
                 *reinterpret_cast<float4v*>(scratch + r * kPitch + (i * 32 + 8 * g + 4 * q) * 4) = v;
             }
 #pragma unroll
-        for (int it = 0; it < 32 * CH / 64; ++it) {
-            const int t = it * (64 / CH) + lane / CH;
-            const int64_t n = col_base + j * 32 + t;
-            const float4v lo = *reinterpret_cast<const float4v*>(scratch + t * kPitch + c * 32);
-            const float4v hi = *reinterpret_cast<const float4v*>(scratch + t * kPitch + c * 32 + 16);
+        for (int it = 0; it < IT; ++it) {
+            const int64_t n = n0 + it * kRows;
+            const float4v lo = *reinterpret_cast<const float4v*>(scratch + (it * kRows + lane / CH) * kPitch + c * 32);
+            const float4v hi = *reinterpret_cast<const float4v*>(scratch + (it * kRows + lane / CH) * kPitch + c * 32 + 16);
             if (n >= N || have <= 0) continue;
-            float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}, more[8] = {};
-            if (residual) load_row_values(residual, n * ldr + m, have, out, more);
-            finish_row_values<DT>(*this, n, m, have, scale, b, is8<DT> && x_scale ? x_scale[n] : 1.0f, more, v);
+            float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            finish_row_values<DT>(*this, n, m, have, scale, b, xs[it], more[it], past_l2, v);
         }
-    }
+    });
 }
 
 // ---- host side: the tiled and the streaming kernels, compiled per input type ----
-template <int DT> sp24_status linear_tiled(const LinearArgs& a, hipStream_t st);
-template <int DT> sp24_status grouped_tiled(const GroupedArgs& a, hipStream_t st);
+enum class LayerTile { stream, t64x32, t128x64, t128x128, t256x128, t256x256 };
+template <int DT, class ARGS> sp24_status layer_tiled(const ARGS& a, LayerTile tile, hipStream_t st);
 sp24_status launch_linear_stream(const LinearArgs& a, hipStream_t st);
 sp24_status launch_grouped_stream(const GroupedArgs& a, hipStream_t st);
+
+// f(integral_constant<int, the input type>{})
+template <class F>
+sp24_status by_input(const MmArgs& a, F&& f)
+{
+    if (a.in == SP24_I8) return f(std::integral_constant<int, SP24_I8>{});
+    if (a.in == SP24_F8) return f(std::integral_constant<int, SP24_F8>{});
+    if (a.in == SP24_F16) return f(std::integral_constant<int, SP24_F16>{});
+    return f(std::integral_constant<int, SP24_BF16>{});
+}
 
 } // namespace sp24

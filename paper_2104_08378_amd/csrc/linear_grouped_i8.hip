@@ -3,6 +3,6 @@
 
 namespace sp24 {
 
-template sp24_status grouped_tiled<SP24_I8>(const GroupedArgs& a, hipStream_t st);
+template sp24_status layer_tiled<SP24_I8>(const GroupedArgs& a, LayerTile tile, hipStream_t st);
 
 } // namespace sp24

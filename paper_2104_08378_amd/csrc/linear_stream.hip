@@ -15,15 +15,6 @@ static sp24_status run_layer_stream(const ARGS& a, hipStream_t st)
     return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
 }
 
-template <class ARGS, class F>
-static sp24_status by_input(const ARGS& a, F&& run)
-{
-    if (a.in == SP24_I8) return run(std::integral_constant<int, SP24_I8>{});
-    if (a.in == SP24_F8) return run(std::integral_constant<int, SP24_F8>{});
-    if (a.in == SP24_F16) return run(std::integral_constant<int, SP24_F16>{});
-    return run(std::integral_constant<int, SP24_BF16>{});
-}
-
 sp24_status launch_linear_stream(const LinearArgs& a, hipStream_t st)
 {
     return by_input(a, [&](auto dt) {

@@ -3,6 +3,6 @@
 
 namespace sp24 {
 
-template sp24_status linear_tiled<SP24_BF16>(const LinearArgs& a, hipStream_t st);
+template sp24_status layer_tiled<SP24_BF16>(const LinearArgs& a, LayerTile tile, hipStream_t st);
 
 } // namespace sp24

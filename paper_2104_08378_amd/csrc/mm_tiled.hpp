@@ -476,6 +476,13 @@ constexpr int store_bytes()
     if constexpr (ARGS::kOwnStore) return ARGS::template wave_bytes<TM>();
     else return epilogue_geometry<OUT, TN>::kWaveBytes;
 }
+// LDS of a workgroup's tile beside the stages, filled before them (fetch_vectors)
+template <class ARGS, int DT, int BM>
+constexpr int vector_bytes()
+{
+    if constexpr (ARGS::kOwnStore) return ARGS::template vector_bytes<DT, BM>();
+    else return 0;
+}
 
 // ---------------------------------------------------------------------------
 // Sparse kernel.  Stage layout: [B: BN rows x 128 B, swizzled][V: 2 KiB per
@@ -505,7 +512,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_spmm_pipe(ARGS a, int tiles
     constexpr int kEpiBytes = NW * store_bytes<ARGS, OUT, TM, TN>();
     static_assert(NS >= 3 && (NS - 2) * NV <= 63, "at least three stages; vmcnt is a 6-bit counter");
     constexpr int kLdsBytes = NS * kStageBytes > kEpiBytes ? NS * kStageBytes : kEpiBytes;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds_all[kLdsBytes];
+    __shared__ __attribute__((aligned(1024))) uint8_t lds_all[kLdsBytes + vector_bytes<ARGS, DT, BM>()];
 
     int tm, tn;
     tile_of_workgroup(tiles_m, tiles_n, tm, tn);
@@ -521,6 +528,9 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_spmm_pipe(ARGS a, int tiles
     const KRange share = k_range_of_workgroup(a, (int)(a.K / BK), (int)((a.K * ES) % kRowBytes));
     const int nsteps = share.nsteps, tail = share.tail;
     const int64_t rb_total = a.M / 32;
+
+    // (ahead of the first stage's transfers, whose wait then covers these)
+    if constexpr (ARGS::kOwnStore) a.template fetch_vectors<DT, BM, NW>(lds_all + kLdsBytes, (int64_t)tm * BM, wave, lane);
 
     // ---- transfers of this wavefront ----
     const int64_t ldb_bytes = a.ldb * ES;
@@ -820,7 +830,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_spmm_pipe(ARGS a, int tiles
     // LDS becomes store scratch
     uint8_t* const scratch = lds_all + wave * store_bytes<ARGS, OUT, TM, TN>();
     const int64_t row_base = (int64_t)tm * BM + wm * TM * 32, col_base = (int64_t)tn * BN + wn * TN * 32;
-    if constexpr (ARGS::kOwnStore) a.template store_wave<DT, TM, TN>(acc, scratch, row_base, col_base, lane);
+    if constexpr (ARGS::kOwnStore) a.template store_wave<DT, TM, TN>(acc, scratch, lds_all + kLdsBytes, BM, wm * TM * 32, row_base, col_base, lane);
     else store_wave_tile<DT, OUT, TM, TN>(a, acc, scratch, row_base, col_base, lane);
 }
 
@@ -1044,8 +1054,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_gemm_pipe(ARGS a, int tiles
     // LDS becomes store scratch
     uint8_t* const scratch = lds_all + wave * store_bytes<ARGS, OUT, TM, TN>();
     const int64_t row_base = (int64_t)tm * BM + wm * TM * 32, col_base = (int64_t)tn * BN + wn * TN * 32;
-    if constexpr (ARGS::kOwnStore) a.template store_wave<DT, TM, TN>(acc, scratch, row_base, col_base, lane);
-    else store_wave_tile<DT, OUT, TM, TN>(a, acc, scratch, row_base, col_base, lane);
+    store_wave_tile<DT, OUT, TM, TN>(a, acc, scratch, row_base, col_base, lane);
 }
 
 // ---------------------------------------------------------------------------

@@ -39,21 +39,21 @@ __device__ __forceinline__ float load_value(const void* p, int64_t i)
 
 // Eight neighbouring values as they lie in memory (the unit of work of a lane: 16 bytes of a 16-bit type), the first `n` of
 // them; the others are zeros.
+// (WHOLE: there are eight)
 template <int T> struct raw8 { uint4v q[T == SP24_F32 ? 2 : 1]; };
-template <int T>
+template <int T, bool WHOLE = false>
 __device__ __forceinline__ raw8<T> load_raw8(const void* p, int64_t first, int n)
 {
     const uint8_t* at = reinterpret_cast<const uint8_t*>(p) + first * value_size<T>();
     raw8<T> r = {};
-    if (n >= 8) {
+    if (WHOLE || n >= 8) {
         r.q[0] = load_from<uint4v>(at);
         if constexpr (T == SP24_F32) r.q[1] = load_from<uint4v>(at + 16);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            if (i >= n) break;
-            if constexpr (T == SP24_F32) r.q[i / 4][i % 4] = reinterpret_cast<const uint32_t*>(at)[i];
-            else r.q[0][i / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(at)[i] << (16 * (i & 1));
+            if constexpr (T == SP24_F32) r.q[i / 4][i % 4] = i < n ? reinterpret_cast<const uint32_t*>(at)[i] : 0u;
+            else r.q[0][i / 2] |= i < n ? (uint32_t)reinterpret_cast<const uint16_t*>(at)[i] << (16 * (i & 1)) : 0u;
         }
     }
     return r;
@@ -69,12 +69,12 @@ __device__ __forceinline__ void values_of(const raw8<T>& r, float (&v)[8])
 }
 
 // The first `n` of eight values, rounded to nearest even.
-template <int T>
+template <int T, bool WHOLE = false>
 __device__ __forceinline__ void store_values8(void* p, int64_t first, int n, const float (&v)[8])
 {
     uint8_t* at = reinterpret_cast<uint8_t*>(p) + first * value_size<T>();
     if constexpr (T == SP24_F32) {
-        if (n >= 8) {
+        if (WHOLE || n >= 8) {
             store_to(at, float4v{v[0], v[1], v[2], v[3]});
             store_to(at + 16, float4v{v[4], v[5], v[6], v[7]});
         } else {
@@ -84,7 +84,7 @@ __device__ __forceinline__ void store_values8(void* p, int64_t first, int n, con
         }
     } else {
         const uint4v q = {pack_out16<T>(v[0], v[1]), pack_out16<T>(v[2], v[3]), pack_out16<T>(v[4], v[5]), pack_out16<T>(v[6], v[7])};
-        if (n >= 8) store_to(at, q);
+        if (WHOLE || n >= 8) store_to(at, q);
         else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
@@ -94,9 +94,10 @@ __device__ __forceinline__ void store_values8(void* p, int64_t first, int n, con
 }
 
 // Eight vector entries in binary32, the first `n` of them.
+template <bool WHOLE = false>
 __device__ __forceinline__ void load_floats8(const float* p, int64_t first, int n, float (&v)[8])
 {
-    values_of<SP24_F32>(load_raw8<SP24_F32>(p, first, n), v);
+    values_of<SP24_F32>(load_raw8<SP24_F32, WHOLE>(p, first, n), v);
 }
 
 // ---------------------------------------------------------------------------
@@ -110,12 +111,26 @@ __device__ __forceinline__ float logistic(float x)
 
 constexpr float kGelu2C = 1.5957691216057308f;         // 2 sqrt(2 / pi)
 
-__device__ __forceinline__ float activate(float z, int act)
+template <int ACT>
+__device__ __forceinline__ float activated(float z)
 {
-    if (act == SP24_ACT_RELU) return z > 0.0f || z != z ? z : 0.0f;        // (a NaN stays one)
-    if (act == SP24_ACT_GELU) return z * logistic(kGelu2C * z * (1.0f + 0.044715f * z * z));
-    if (act == SP24_ACT_SILU) return z * logistic(z);
-    return z;
+    if constexpr (ACT == SP24_ACT_RELU) return z > 0.0f || z != z ? z : 0.0f;        // (a NaN stays one)
+    else if constexpr (ACT == SP24_ACT_GELU) return z * logistic(z * __builtin_fmaf(0.044715f * kGelu2C, z * z, kGelu2C));
+    else if constexpr (ACT == SP24_ACT_SILU) return z * logistic(z);
+    else return z;
+}
+
+// (one branch for all of them: `act` is the same in every lane)
+template <int COUNT>
+__device__ __forceinline__ void activate(float (&v)[COUNT], int act)
+{
+    auto all = [&](auto f) {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) v[i] = f(v[i]);
+    };
+    if (act == SP24_ACT_GELU) all([](float z) { return activated<SP24_ACT_GELU>(z); });
+    else if (act == SP24_ACT_SILU) all([](float z) { return activated<SP24_ACT_SILU>(z); });
+    else if (act == SP24_ACT_RELU) all([](float z) { return activated<SP24_ACT_RELU>(z); });
 }
 
 // d activate / d z.  Past |z| = 100 the slopes are 0 and 1 (p is 0 or 1), and z^2 could overflow against a factor of 0.
