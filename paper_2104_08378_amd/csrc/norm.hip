@@ -6,6 +6,8 @@
 //
 // Bound by memory: a row is read once, stays in registers (eight values a lane and chunk, in binary32 as all sums are) and is written
 // once.  A workgroup takes a row after the other and keeps its weights.
+#include <algorithm>
+
 #include "launch.hpp"
 #include "rowops.hpp"
 
@@ -15,7 +17,7 @@ namespace sp24 {
 template <int OUT> constexpr float top_code() { return OUT == SP24_I8 ? 127.0f : 448.0f; }
 constexpr float kLeastMagnitude = 7.888609052210118e-31f;       // 2^-100: below it a row's codes are taken against it (and are zeros)
 
-template <int OUT>
+template <int OUT, bool WHOLE>
 __device__ __forceinline__ void store_codes8(void* p, int64_t first, int n, const float (&v)[8])
 {
     uint8_t* at = reinterpret_cast<uint8_t*>(p) + first;
@@ -30,7 +32,7 @@ __device__ __forceinline__ void store_codes8(void* p, int64_t first, int n, cons
             q[d] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[4 * d + 2], v[4 * d + 3], w, true);
         }
     }
-    if (n >= 8) store_to(at, q);
+    if (WHOLE || n >= 8) store_to(at, q);
     else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -38,19 +40,21 @@ __device__ __forceinline__ void store_codes8(void* p, int64_t first, int n, cons
     }
 }
 
-// C: chunks of eight values a thread holds; thread t those at (c * blockDim.x + t) * 8
-template <int T, int OUT, int C, bool NORM>
-__global__ __launch_bounds__(1024) void k_norm_rows(RowsArgs a)
+// C: chunks of eight values a thread holds; thread t those at (c * blockDim.x + t) * 8.  WHOLE: rows of whole chunks (the code for a
+// part of one at every load and store costs registers that the many rows in flight need).  MOST: threads at most
+template <int T, int OUT, int C, bool NORM, bool WHOLE, int MOST>
+__global__ __launch_bounds__(MOST) void k_norm_rows(RowsArgs a)
 {
+    constexpr bool KEEP = C <= 2;                                // the weights of all rows in registers; else from the L2, row by row
     __shared__ uint32_t cells[3][16];
     const int H = (int)a.H;
-    float w[C][8];
+    float w[KEEP ? C : 1][8];
     int n[C];                                                    // values of the chunk that exist
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         const int first = (c * blockDim.x + threadIdx.x) * 8;
-        n[c] = min(H - first, 8);
-        if (NORM && n[c] > 0) load_floats8(a.weight, first, n[c], w[c]);
+        n[c] = WHOLE ? (first < H ? 8 : 0) : min(H - first, 8);
+        if (NORM && KEEP && n[c] > 0) load_floats8<WHOLE>(a.weight, first, n[c], w[c]);
     }
     int parity = 0;
     for (int64_t row = blockIdx.x; row < a.N; row += gridDim.x) {
@@ -58,8 +62,8 @@ __global__ __launch_bounds__(1024) void k_norm_rows(RowsArgs a)
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int first = (c * blockDim.x + threadIdx.x) * 8;
-            if (n[c] > 0) x[c] = load_raw8<T>(a.X, row * a.ldx + first, n[c]);
-            if (NORM && a.residual && n[c] > 0) r[c] = load_raw8<T>(a.residual, row * a.ldr + first, n[c]);
+            if (n[c] > 0) x[c] = load_raw8<T, WHOLE>(a.X, row * a.ldx + first, n[c]);
+            if (NORM && a.residual && n[c] > 0) r[c] = load_raw8<T, WHOLE>(a.residual, row * a.ldr + first, n[c]);
         }
         float h[C][8], sum = 0.0f;
 #pragma unroll
@@ -78,7 +82,7 @@ __global__ __launch_bounds__(1024) void k_norm_rows(RowsArgs a)
                     for (int i = 0; i < 8; ++i) h[c][i] += more[i];
                 }
                 // (rounded to the rows' type here; the norm goes on with the unrounded sum)
-                if (a.hidden) store_values8<T>(a.hidden, row * a.ldh + (c * blockDim.x + threadIdx.x) * 8, n[c], h[c]);
+                if (a.hidden) store_values8<T, WHOLE>(a.hidden, row * a.ldh + (c * blockDim.x + threadIdx.x) * 8, n[c], h[c]);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(h[c][i], h[c][i], sum);
             }
@@ -91,8 +95,9 @@ __global__ __launch_bounds__(1024) void k_norm_rows(RowsArgs a)
 #pragma unroll
             for (int c = 0; c < C; ++c)
                 if (n[c] > 0) {
+                    if (!KEEP) load_floats8<WHOLE>(a.weight, (c * blockDim.x + threadIdx.x) * 8, n[c], w[0]);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) h[c][i] = h[c][i] * rstd * w[c][i];
+                    for (int i = 0; i < 8; ++i) h[c][i] = h[c][i] * rstd * w[KEEP ? c : 0][i];
                 }
         }
         if constexpr (is8<OUT>) {
@@ -102,7 +107,7 @@ __global__ __launch_bounds__(1024) void k_norm_rows(RowsArgs a)
 #pragma unroll
             for (int c = 0; c < C; ++c)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) most = max(most, i < n[c] ? __float_as_uint(h[c][i]) & 0x7FFFFFFFu : 0u);
+                for (int i = 0; i < 8; ++i) most = max(most, (WHOLE ? n[c] > 0 : i < n[c]) ? __float_as_uint(h[c][i]) & 0x7FFFFFFFu : 0u);
             float top = __uint_as_float(over_workgroup<max_u>(most, cells[2]));
             if (!NORM) __syncthreads();                          // (the norm's sum has a barrier between two uses of the cells)
             top = top < kLeastMagnitude ? kLeastMagnitude : top;
@@ -113,29 +118,30 @@ __global__ __launch_bounds__(1024) void k_norm_rows(RowsArgs a)
                 if (n[c] <= 0) continue;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) h[c][i] *= inv;
-                store_codes8<OUT>(a.Y, row * a.ldy + (c * blockDim.x + threadIdx.x) * 8, n[c], h[c]);
+                store_codes8<OUT, WHOLE>(a.Y, row * a.ldy + (c * blockDim.x + threadIdx.x) * 8, n[c], h[c]);
             }
         } else {
 #pragma unroll
             for (int c = 0; c < C; ++c)
-                if (n[c] > 0) store_values8<OUT>(a.Y, row * a.ldy + (c * blockDim.x + threadIdx.x) * 8, n[c], h[c]);
+                if (n[c] > 0) store_values8<OUT, WHOLE>(a.Y, row * a.ldy + (c * blockDim.x + threadIdx.x) * 8, n[c], h[c]);
         }
     }
 }
 
 // The gradients.  A workgroup's share of dw stays in registers over its rows and goes to its row of `partial`.
-template <int T, int C>
-__global__ __launch_bounds__(1024) void k_norm_grad(NormGradArgs a)
+template <int T, int C, bool WHOLE, int MOST>
+__global__ __launch_bounds__(MOST) void k_norm_grad(NormGradArgs a)
 {
+    constexpr bool KEEP = C <= 2;
     __shared__ uint32_t cells[2][16];
     const int H = (int)a.H;
-    float w[C][8], dw[C][8];
+    float w[KEEP ? C : 1][8], dw[C][8];
     int n[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         const int first = (c * blockDim.x + threadIdx.x) * 8;
-        n[c] = min(H - first, 8);
-        if (n[c] > 0) load_floats8(a.weight, first, n[c], w[c]);
+        n[c] = WHOLE ? (first < H ? 8 : 0) : min(H - first, 8);
+        if (KEEP && n[c] > 0) load_floats8<WHOLE>(a.weight, first, n[c], w[c]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) dw[c][i] = 0.0f;
     }
@@ -148,9 +154,9 @@ __global__ __launch_bounds__(1024) void k_norm_grad(NormGradArgs a)
         for (int c = 0; c < C; ++c) {
             const int first = (c * blockDim.x + threadIdx.x) * 8;
             if (n[c] <= 0) continue;
-            dy_raw[c] = load_raw8<T>(a.dY, row * a.lddy + first, n[c]);
-            h_raw[c] = load_raw8<T>(a.hidden, row * a.ldh + first, n[c]);
-            if (a.dhidden) dh_raw[c] = load_raw8<T>(a.dhidden, row * a.lddh + first, n[c]);
+            dy_raw[c] = load_raw8<T, WHOLE>(a.dY, row * a.lddy + first, n[c]);
+            h_raw[c] = load_raw8<T, WHOLE>(a.hidden, row * a.ldh + first, n[c]);
+            if (a.dhidden) dh_raw[c] = load_raw8<T, WHOLE>(a.dhidden, row * a.lddh + first, n[c]);
         }
 #pragma unroll
         for (int c = 0; c < C; ++c) {
@@ -158,10 +164,11 @@ __global__ __launch_bounds__(1024) void k_norm_grad(NormGradArgs a)
             float dy[8], h[8];
             values_of<T>(dy_raw[c], dy);
             values_of<T>(h_raw[c], h);
+            if (!KEEP) load_floats8<WHOLE>(a.weight, (c * blockDim.x + threadIdx.x) * 8, n[c], w[0]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float t = dy[i] * h[i];
-                if (i < n[c]) along = __builtin_fmaf(t, w[c][i], along);
+                if (WHOLE || i < n[c]) along = __builtin_fmaf(t, w[KEEP ? c : 0][i], along);
                 dw[c][i] = __builtin_fmaf(t, rstd, dw[c][i]);
             }
         }
@@ -174,6 +181,71 @@ __global__ __launch_bounds__(1024) void k_norm_grad(NormGradArgs a)
             float dy[8], h[8], dx[8];
             values_of<T>(dy_raw[c], dy);
             values_of<T>(h_raw[c], h);
+            if (!KEEP) load_floats8<WHOLE>(a.weight, (c * blockDim.x + threadIdx.x) * 8, n[c], w[0]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dx[i] = rstd * (dy[i] * w[KEEP ? c : 0][i] - h[i] * k);
+            if (a.dhidden) {
+                float dh[8];
+                values_of<T>(dh_raw[c], dh);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) dx[i] += dh[i];
+            }
+            store_values8<T, WHOLE>(a.dX, row * a.lddx + (c * blockDim.x + threadIdx.x) * 8, n[c], dx);
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+        if (n[c] > 0) store_values8<SP24_F32, WHOLE>(a.partial, (int64_t)blockIdx.x * a.H + (c * blockDim.x + threadIdx.x) * 8, n[c], dw[c]);
+}
+
+// The same with a wavefront to a row: no barriers on the way, and the shares of the eight wavefronts are added at the end.
+constexpr int kGradWaves = 8;
+template <int T, int C>
+__global__ __launch_bounds__(64 * kGradWaves) void k_norm_grad_short(NormGradArgs a)
+{
+    __shared__ float share[kGradWaves / 2][C * 512];
+    const int H = (int)a.H, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    float dw[C][8];
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dw[c][i] = 0.0f;
+    for (int64_t row = (int64_t)blockIdx.x * kGradWaves + wave; row < a.N; row += (int64_t)gridDim.x * kGradWaves) {
+        raw8<T> dy_raw[C], h_raw[C], dh_raw[C];
+        float w[C][8];
+        const float rstd = a.rstd[row];
+        float along = 0.0f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int first = (c * 64 + lane) * 8;
+            if (first >= H) continue;
+            dy_raw[c] = load_raw8<T, true>(a.dY, row * a.lddy + first, 8);
+            h_raw[c] = load_raw8<T, true>(a.hidden, row * a.ldh + first, 8);
+            if (a.dhidden) dh_raw[c] = load_raw8<T, true>(a.dhidden, row * a.lddh + first, 8);
+            load_floats8<true>(a.weight, first, 8, w[c]);
+        }
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            if ((c * 64 + lane) * 8 >= H) continue;
+            float dy[8], h[8];
+            values_of<T>(dy_raw[c], dy);
+            values_of<T>(h_raw[c], h);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float t = dy[i] * h[i];
+                along = __builtin_fmaf(t, w[c][i], along);
+                dw[c][i] = __builtin_fmaf(t, rstd, dw[c][i]);
+            }
+        }
+        along = __uint_as_float(over_wave<add_f>(__float_as_uint(along)));
+        const float k = rstd * rstd * (along / (float)H);
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int first = (c * 64 + lane) * 8;
+            if (first >= H) continue;
+            float dy[8], h[8], dx[8];
+            values_of<T>(dy_raw[c], dy);
+            values_of<T>(h_raw[c], h);
 #pragma unroll
             for (int i = 0; i < 8; ++i) dx[i] = rstd * (dy[i] * w[c][i] - h[i] * k);
             if (a.dhidden) {
@@ -182,22 +254,44 @@ __global__ __launch_bounds__(1024) void k_norm_grad(NormGradArgs a)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) dx[i] += dh[i];
             }
-            store_values8<T>(a.dX, row * a.lddx + (c * blockDim.x + threadIdx.x) * 8, n[c], dx);
+            store_values8<T, true>(a.dX, row * a.lddx + first, 8, dx);
         }
     }
+    // halves are added until one is left: wavefronts 4 - 7 to 0 - 3, 2 - 3 to 0 - 1, 1 to 0
 #pragma unroll
-    for (int c = 0; c < C; ++c)
-        if (n[c] > 0) store_values8<SP24_F32>(a.partial, (int64_t)blockIdx.x * a.H + (c * blockDim.x + threadIdx.x) * 8, n[c], dw[c]);
+    for (int half = kGradWaves / 2; half > 0; half /= 2) {
+        if (wave >= half && wave < 2 * half) {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) share[wave - half][(c * 8 + i) * 64 + lane] = dw[c][i];
+        }
+        __syncthreads();
+        if (wave < half) {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) dw[c][i] += share[wave][(c * 8 + i) * 64 + lane];
+        }
+        __syncthreads();
+    }
+    if (wave == 0) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int first = (c * 64 + lane) * 8;
+            if (first < H) store_values8<SP24_F32, true>(a.partial, (int64_t)blockIdx.x * a.H + first, 8, dw[c]);
+        }
+    }
 }
 
-// out[e][c] = the sum of rows first .. last - 1 of `partial` (columns wide), in a fixed order: 16 interleaved sums, then those.
+// out[e][c] = the sum of rows first .. last - 1 of `partial` (columns wide), in a fixed order: 32 interleaved sums, then those.
 // Without offsets all rows; with them those of segment e, `unit` rows of the offsets to one of partial.
 __global__ __launch_bounds__(1024) void k_column_sums(const float* partial, int64_t rows, int64_t columns, const int32_t* offsets, int unit,
                                                       float* out)
 {
-    __shared__ float part[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    __shared__ float part[32][33];
+    const int at = threadIdx.x & 31, stream = threadIdx.x >> 5;
+    const int64_t c = (int64_t)blockIdx.x * 32 + at;
     int64_t first = 0, last = rows;
     if (offsets) {
         first = min(max((int64_t)offsets[blockIdx.y] / unit, (int64_t)0), rows);
@@ -205,42 +299,53 @@ __global__ __launch_bounds__(1024) void k_column_sums(const float* partial, int6
     }
     float sum = 0.0f;
     if (c < columns) {
-        int64_t i = first + wave;
-        for (; i + 48 < last; i += 64) {                          // four loads on their way
-            const float v0 = partial[i * columns + c], v1 = partial[(i + 16) * columns + c], v2 = partial[(i + 32) * columns + c],
-                        v3 = partial[(i + 48) * columns + c];
+        int64_t i = first + stream;
+        for (; i + 96 < last; i += 128) {                         // four loads on their way
+            const float v0 = partial[i * columns + c], v1 = partial[(i + 32) * columns + c], v2 = partial[(i + 64) * columns + c],
+                        v3 = partial[(i + 96) * columns + c];
             sum = (((sum + v0) + v1) + v2) + v3;
         }
-        for (; i < last; i += 16) sum += partial[i * columns + c];
+        for (; i < last; i += 32) sum += partial[i * columns + c];
     }
-    part[wave][lane] = sum;
+    part[stream][at] = sum;
     __syncthreads();
-    if (wave == 0 && c < columns) {
+    if (stream == 0 && c < columns) {
         sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sum += part[i][lane];
+        for (int i = 0; i < 32; ++i) sum += part[i][at];
         out[(int64_t)blockIdx.y * columns + c] = sum;
     }
 }
 
-// threads for rows of H values at C chunks a thread, in whole wavefronts; 0: too long for that
-static unsigned row_threads(int64_t H, int C)
-{
-    const int64_t chunks = (H + 7) / 8, threads = ((chunks + C - 1) / C + 63) / 64 * 64;
-    return threads <= 1024 ? (unsigned)threads : 0u;
-}
+constexpr int64_t kLongRow = 32768;                               // what 1024 threads hold at four chunks each
 
+// threads for rows of H values at C chunks a thread, in whole wavefronts
+static unsigned row_threads(int64_t H, int C) { return (unsigned)(((H + 7) / 8 + C - 1) / C + 63) / 64 * 64; }
+
+// Few rows: as many threads to a row as it has chunks, so that it is on its way at once.  Many: a few chunks a thread, so that the
+// reduction (and the barrier in it) is over fewer wavefronts.
 template <int T, int OUT, bool NORM>
 static sp24_status run_norm(const RowsArgs& a, hipStream_t st)
 {
-    const unsigned t1 = row_threads(a.H, 1), t4 = row_threads(a.H, 4), t8 = row_threads(a.H, 8);
-    const bool one = t1 != 0 && (t4 == 64 ? t1 == 64 : a.N < 1024);
-    const unsigned threads = one ? t1 : t4 ? t4 : t8;
-    const unsigned grid = (unsigned)(a.N < (int64_t)(1 << 20) / threads ? a.N : (1 << 20) / threads);
-    if (one) k_norm_rows<T, OUT, 1, NORM><<<grid, threads, 0, st>>>(a);
-    else if (t4) k_norm_rows<T, OUT, 4, NORM><<<grid, threads, 0, st>>>(a);
-    else if constexpr (!NORM) k_norm_rows<T, OUT, 8, NORM><<<grid, threads, 0, st>>>(a);
-    return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
+    const bool whole = a.H % 8 == 0, many = a.N >= 1024;
+    auto run = [&](auto kernel, unsigned threads) {
+        const int64_t most = (1 << 21) / threads;                 // twice what the chip holds at a time
+        kernel<<<(unsigned)(a.N < most ? a.N : most), threads, 0, st>>>(a);
+        return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
+    };
+    if (whole && many && a.H > 512 && a.H <= 4096) return run(k_norm_rows<T, OUT, 2, NORM, true, 256>, row_threads(a.H, 2));
+    if (whole && many && a.H > 4096 && a.H <= 8192) return run(k_norm_rows<T, OUT, 4, NORM, true, 256>, row_threads(a.H, 4));
+    if (a.H <= 8192) {
+        if (whole) return run(k_norm_rows<T, OUT, 1, NORM, true, 1024>, row_threads(a.H, 1));
+        return run(k_norm_rows<T, OUT, 1, NORM, false, 1024>, row_threads(a.H, 1));
+    }
+    if (a.H <= 16384) {
+        if (whole) return run(k_norm_rows<T, OUT, 2, NORM, true, 1024>, row_threads(a.H, 2));
+        return run(k_norm_rows<T, OUT, 2, NORM, false, 1024>, row_threads(a.H, 2));
+    }
+    if (a.H <= kLongRow) return run(k_norm_rows<T, OUT, 4, NORM, false, 1024>, row_threads(a.H, 4));
+    if constexpr (!NORM) return run(k_norm_rows<T, OUT, 8, NORM, false, 1024>, row_threads(a.H, 8));
+    return SP24_ERR_SHAPE;
 }
 
 template <int T>
@@ -263,11 +368,15 @@ sp24_status launch_norm_rows(const RowsArgs& a, hipStream_t st)
     return run_norm_out<SP24_BF16>(a, st);
 }
 
+// rows of whole chunks that a wavefront holds
+static bool short_row(int64_t H) { return H % 8 == 0 && H <= 1024; }
+
 int64_t norm_grad_groups(int64_t N, int64_t H)
 {
-    const unsigned threads = row_threads(H, H <= 8192 ? 1 : 4);
-    const int64_t most = (1 << 17) / (int64_t)threads;            // two wavefronts a SIMD
-    return N < most ? N : most;
+    // as many workgroups as the chip holds at a time (short rows: 16 wavefronts a unit), for every one writes a row of sums
+    const int64_t rows = short_row(H) ? kGradWaves : 1;
+    const int64_t most = short_row(H) ? 512 : (1 << 17) / (int64_t)row_threads(H, H <= 8192 ? 1 : H <= 16384 ? 2 : 4);
+    return std::min((N + rows - 1) / rows, most);
 }
 
 template <int T>
@@ -275,8 +384,14 @@ static sp24_status run_norm_grad(const NormGradArgs& a, hipStream_t st)
 {
     const unsigned grid = (unsigned)norm_grad_groups(a.N, a.H);
     if (grid > 0) {
-        if (a.H <= 8192) k_norm_grad<T, 1><<<grid, row_threads(a.H, 1), 0, st>>>(a);
-        else k_norm_grad<T, 4><<<grid, row_threads(a.H, 4), 0, st>>>(a);
+        auto run = [&](auto kernel, int C) { kernel<<<grid, row_threads(a.H, C), 0, st>>>(a); };
+        auto run_short = [&](auto kernel) { kernel<<<grid, 64 * kGradWaves, 0, st>>>(a); };
+        if (short_row(a.H) && a.H <= 512) run_short(k_norm_grad_short<T, 1>);
+        else if (short_row(a.H)) run_short(k_norm_grad_short<T, 2>);
+        else if (a.H > 16384) run(k_norm_grad<T, 4, false, 1024>, 4);
+        else if (a.H > 8192) run(k_norm_grad<T, 2, false, 1024>, 2);
+        else if (a.H % 8 != 0) run(k_norm_grad<T, 1, false, 1024>, 1);
+        else run(k_norm_grad<T, 1, true, 1024>, 1);
         if (hipGetLastError() != hipSuccess) return SP24_ERR_LAUNCH;
     }
     return launch_column_sums(a.partial, grid, a.H, nullptr, 1, 1, a.dweight, st);
@@ -292,7 +407,7 @@ sp24_status launch_norm_grad(const NormGradArgs& a, hipStream_t st)
 sp24_status launch_column_sums(const float* partial, int64_t rows, int64_t columns, const int32_t* offsets, int segments, int unit, float* out,
                                hipStream_t st)
 {
-    k_column_sums<<<dim3((unsigned)((columns + 63) / 64), (unsigned)segments), 1024, 0, st>>>(partial, rows, columns, offsets, unit, out);
+    k_column_sums<<<dim3((unsigned)((columns + 31) / 32), (unsigned)segments), 1024, 0, st>>>(partial, rows, columns, offsets, unit, out);
     return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
 }
 
