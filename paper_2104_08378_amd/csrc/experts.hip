@@ -7,8 +7,8 @@ namespace sp24 {
 
 // ---------------------------------------------------------------------------
 // The sort is a counting sort that keeps the order of equal keys: the number of choices of every expert before a wavefront's part, then the
-// place of each of its 64 at a time among the 64 (ballots over the bits of the expert's number).  Whole numbers throughout, so the
-// result is one.  Up to kSortPart choices one workgroup does all of it; more are cut into parts that count, a scan over parts and
+// place of each of its 64 at a time among the 64 (ballots over the bits of the expert's number; counters that lanes add to would be one
+// word for a popular expert: 4096 x 2 choices of eight took 11.8 us).  Whole numbers throughout, so the result is one.  Up to kSortPart choices one workgroup does all of it; more are cut into parts that count, a scan over parts and
 // experts, and parts that place.
 // ---------------------------------------------------------------------------
 constexpr int kSortWaves = 16, kSortExperts = 1024;
@@ -31,37 +31,56 @@ __device__ __forceinline__ uint64_t same_key(int key, bool live, int bits)
 
 __device__ __forceinline__ int sort_bits(int experts) { return 32 - __clz(max(experts - 1, 1)); }
 
-// how many of ids[first .. last) each expert has, per wavefront; the wavefronts take equal runs of whole 64s
-__device__ __forceinline__ void sort_count(SortLds& s, const SortArgs& a, int64_t first, int64_t last)
+constexpr int kSortRuns = kSortPart / kSortWaves / 64;       // of 64 choices, to a wavefront
+
+// A lane's choices: the expert, or -1, and how many of the wavefront's earlier ones name the same.
+struct SortRun {
+    int expert[kSortRuns], before[kSortRuns];
+};
+
+// ids[first .. last): the wavefronts take equal runs of whole 64s and leave in s.count how many of theirs each expert has
+__device__ __forceinline__ void sort_count(SortLds& s, const SortArgs& a, int64_t first, int64_t last, SortRun& run, int64_t& from, int64_t& to)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, bits = sort_bits(a.experts);
+    const int64_t length = ((last - first + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
+    from = min(first + wave * length, last);
+    to = min(from + length, last);
+#pragma unroll
+    for (int u = 0; u < kSortRuns; ++u) {
+        const int64_t i = from + u * 64 + lane;
+        run.expert[u] = i < to ? a.ids[i] : -1;
+    }
     for (int e = lane; e < a.experts; e += 64) s.count[wave][e] = 0;
-    const int64_t run = ((last - first + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
-    const int64_t from = min(first + wave * run, last), to = min(from + run, last);
-    for (int64_t i = from + lane; i < to; i += 64) {
-        const int e = a.ids[i];
-        if ((unsigned)e < (unsigned)a.experts) atomicAdd(&s.count[wave][e], 1);       // (a wavefront's own words, and sums of whole numbers)
+#pragma unroll
+    for (int u = 0; u < kSortRuns; ++u) {
+        if (from + u * 64 >= to) continue;
+        const int e = run.expert[u];
+        const bool live = (unsigned)e < (unsigned)a.experts;
+        const uint64_t same = same_key(e, live, bits);
+        if (!live) {
+            run.expert[u] = -1;
+            continue;
+        }
+        const int before = s.count[wave][e];
+        run.before[u] = before + __popcll(same & (((uint64_t)1 << lane) - 1));
+        if (__ffsll((unsigned long long)same) - 1 == lane) s.count[wave][e] = before + __popcll(same);
     }
 }
 
-// the rows of ids[first .. last), from the next rows in s.count on
-__device__ __forceinline__ void sort_place(SortLds& s, const SortArgs& a, int64_t first, int64_t last)
+// their rows, s.count holding the first row that the wavefront has of each expert
+__device__ __forceinline__ void sort_place(const SortLds& s, const SortArgs& a, const SortRun& run, int64_t from, int64_t to)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, bits = sort_bits(a.experts);
-    const int64_t run = ((last - first + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
-    const int64_t from = min(first + wave * run, last), to = min(from + run, last);
-    for (int64_t i0 = from; i0 < to; i0 += 64) {
-        const int64_t i = i0 + lane;
-        const int e = i < to ? a.ids[i] : -1;
-        const bool live = (unsigned)e < (unsigned)a.experts;
-        const uint64_t same = same_key(e, live, bits);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int u = 0; u < kSortRuns; ++u) {
+        const int64_t i = from + u * 64 + lane;
+        if (i >= to) continue;
         int row = -1;
-        if (live) {
-            row = s.count[wave][e] + __popcll(same & (((uint64_t)1 << lane) - 1));
+        if (run.expert[u] >= 0) {
+            row = s.count[wave][run.expert[u]] + run.before[u];
             a.rows[row] = (int32_t)i;
         }
-        if (i < to) a.slots[i] = row;
-        if (live && __ffsll((unsigned long long)same) - 1 == lane) s.count[wave][e] += __popcll(same);
+        a.slots[i] = row;
     }
 }
 
@@ -104,7 +123,9 @@ __device__ __forceinline__ void sort_finish(const SortArgs& a, int first, int to
 __global__ __launch_bounds__(1024) void k_sort_one(SortArgs a)
 {
     __shared__ SortLds s;
-    sort_count(s, a, 0, a.T);
+    SortRun run;
+    int64_t from, to;
+    sort_count(s, a, 0, a.T, run, from, to);
     __syncthreads();
     const int e = threadIdx.x;
     int total = 0;
@@ -122,14 +143,16 @@ __global__ __launch_bounds__(1024) void k_sort_one(SortArgs a)
     }
     sort_finish(a, first, total, end);
     __syncthreads();
-    sort_place(s, a, 0, a.T);
+    sort_place(s, a, run, from, to);
 }
 
 __global__ __launch_bounds__(1024) void k_sort_count(SortArgs a)
 {
     __shared__ SortLds s;
     const int64_t first = (int64_t)blockIdx.x * kSortPart;
-    sort_count(s, a, first, min(first + kSortPart, a.T));
+    SortRun run;
+    int64_t from, to;
+    sort_count(s, a, first, min(first + kSortPart, a.T), run, from, to);
     __syncthreads();
     for (int e = threadIdx.x; e < a.experts; e += blockDim.x) {
         int total = 0;
@@ -166,7 +189,9 @@ __global__ __launch_bounds__(1024) void k_sort_place(SortArgs a)
 {
     __shared__ SortLds s;
     const int64_t first = (int64_t)blockIdx.x * kSortPart, last = min(first + kSortPart, a.T);
-    sort_count(s, a, first, last);
+    SortRun run;
+    int64_t from, to;
+    sort_count(s, a, first, last, run, from, to);
     __syncthreads();
     for (int e = threadIdx.x; e < a.experts; e += blockDim.x) {
         int next = a.workspace[(int64_t)blockIdx.x * a.experts + e];
@@ -177,7 +202,7 @@ __global__ __launch_bounds__(1024) void k_sort_place(SortArgs a)
         }
     }
     __syncthreads();
-    sort_place(s, a, first, last);
+    sort_place(s, a, run, from, to);
 }
 
 sp24_status launch_moe_sort(const SortArgs& a, hipStream_t st)
