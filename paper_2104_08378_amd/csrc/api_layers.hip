@@ -277,7 +277,7 @@ int64_t sp24_moe_rows(int64_t choices, int experts)
 
 size_t sp24_moe_sort_workspace_bytes(int64_t choices, int experts)
 {
-    if (choices <= kSortPart || choices > kMostRows / 16 || experts < 1 || experts > SP24_MOST_EXPERTS) return 0;
+    if (choices <= kSortAtOnce || choices > kMostRows / 16 || experts < 1 || experts > SP24_MOST_EXPERTS) return 0;
     return (size_t)((choices + kSortPart - 1) / kSortPart) * experts * 4;
 }
 

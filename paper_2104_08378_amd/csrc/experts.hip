@@ -6,10 +6,13 @@
 namespace sp24 {
 
 // ---------------------------------------------------------------------------
-// The sort is a counting sort that keeps the order of equal keys: the number of choices of every expert before a wavefront's part, then the
-// place of each of its 64 at a time among the 64 (ballots over the bits of the expert's number; counters that lanes add to would be one
-// word for a popular expert: 4096 x 2 choices of eight took 11.8 us).  Whole numbers throughout, so the result is one.  Up to kSortPart choices one workgroup does all of it; more are cut into parts that count, a scan over parts and
-// experts, and parts that place.
+// The sort is a counting sort that keeps the order of equal keys: how many choices every expert has in all and before a wavefront's 64, and
+// the place of each among the 64 (ballots over the bits of the expert's number).  Whole numbers throughout, so the result is one.
+//
+// Placing takes some 85 instructions to 64 choices, which one compute unit issues at 0.5 us a thousand (4096 x 2 choices of eight 8.7 us on one
+// workgroup), counting a few: every workgroup counts all choices, from the L2, and places a thousand, one launch and nothing to wait for (5.7 us; 4096 x 4
+// of 64 16.7 -> 6.2).
+// Past kSortAtOnce choices that counting is the longer part: parts of kSortPart count, a scan over parts and experts, and parts place.
 // ---------------------------------------------------------------------------
 constexpr int kSortWaves = 16, kSortExperts = 1024;
 
@@ -19,74 +22,70 @@ struct SortLds {
 };
 
 // lanes with the same key as this one, among those with `live`
-__device__ __forceinline__ uint64_t same_key(int key, bool live, int bits)
+template <int BITS>
+__device__ __forceinline__ uint64_t same_key(int key, bool live)
 {
     uint64_t same = __ballot(live);
-    for (int b = 0; b < bits; ++b) {
+#pragma unroll
+    for (int b = 0; b < BITS; ++b) {
         const uint64_t set = __ballot((key >> b) & 1);
         same &= (key >> b) & 1 ? set : ~set;
     }
     return same;
 }
 
-__device__ __forceinline__ int sort_bits(int experts) { return 32 - __clz(max(experts - 1, 1)); }
-
-constexpr int kSortRuns = kSortPart / kSortWaves / 64;       // of 64 choices, to a wavefront
-
-// A lane's choices: the expert, or -1, and how many of the wavefront's earlier ones name the same.
+// A lane's RUNS choices: the expert, or -1, and how many of the wavefront's earlier ones name the same.
+template <int RUNS>
 struct SortRun {
-    int expert[kSortRuns], before[kSortRuns];
+    int expert[RUNS], before[RUNS];
 };
 
-// ids[first .. last): the wavefronts take equal runs of whole 64s and leave in s.count how many of theirs each expert has
-__device__ __forceinline__ void sort_count(SortLds& s, const SortArgs& a, int64_t first, int64_t last, SortRun& run, int64_t& from, int64_t& to)
+// The wavefront's n choices from `ids` on, at most 64 RUNS: leaves in count[] how many of them each expert has.
+template <int BITS, int RUNS>
+__device__ __forceinline__ void sort_count(int* count, const int32_t* ids, int n, int experts, SortRun<RUNS>& run)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, bits = sort_bits(a.experts);
-    const int64_t length = ((last - first + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
-    from = min(first + wave * length, last);
-    to = min(from + length, last);
+    const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int u = 0; u < kSortRuns; ++u) {
-        const int64_t i = from + u * 64 + lane;
-        run.expert[u] = i < to ? a.ids[i] : -1;
-    }
-    for (int e = lane; e < a.experts; e += 64) s.count[wave][e] = 0;
+    for (int u = 0; u < RUNS; ++u) run.expert[u] = u * 64 + lane < n ? ids[u * 64 + lane] : -1;
+    for (int e = lane; e < experts; e += 64) count[e] = 0;
 #pragma unroll
-    for (int u = 0; u < kSortRuns; ++u) {
-        if (from + u * 64 >= to) continue;
+    for (int u = 0; u < RUNS; ++u) {
+        if (u * 64 >= n) continue;
         const int e = run.expert[u];
-        const bool live = (unsigned)e < (unsigned)a.experts;
-        const uint64_t same = same_key(e, live, bits);
+        const bool live = (unsigned)e < (unsigned)experts;
+        const uint64_t same = same_key<BITS>(e, live);
         if (!live) {
             run.expert[u] = -1;
             continue;
         }
-        const int before = s.count[wave][e];
+        const int before = count[e];
         run.before[u] = before + __popcll(same & (((uint64_t)1 << lane) - 1));
-        if (__ffsll((unsigned long long)same) - 1 == lane) s.count[wave][e] = before + __popcll(same);
+        if (__ffsll((unsigned long long)same) - 1 == lane) count[e] = before + __popcll(same);
     }
 }
 
-// their rows, s.count holding the first row that the wavefront has of each expert
-__device__ __forceinline__ void sort_place(const SortLds& s, const SortArgs& a, const SortRun& run, int64_t from, int64_t to)
+// Their rows, count[] holding the first row that the wavefront has of each expert; `number` is that of the first choice.
+template <int RUNS>
+__device__ __forceinline__ void sort_place(const int* count, const SortArgs& a, const SortRun<RUNS>& run, int64_t number, int n)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63;
+    int32_t* const slots = a.slots + number;
 #pragma unroll
-    for (int u = 0; u < kSortRuns; ++u) {
-        const int64_t i = from + u * 64 + lane;
-        if (i >= to) continue;
+    for (int u = 0; u < RUNS; ++u) {
+        const int i = u * 64 + lane;
+        if (i >= n) continue;
         int row = -1;
         if (run.expert[u] >= 0) {
-            row = s.count[wave][run.expert[u]] + run.before[u];
-            a.rows[row] = (int32_t)i;
+            row = count[run.expert[u]] + run.before[u];
+            a.rows[row] = (int32_t)number + i;
         }
-        a.slots[i] = row;
+        slots[i] = row;
     }
 }
 
 // Segments from the experts' totals (thread e holds that of expert e): whole sixteens one behind the other.  Returns the segment's first row;
 // *end: the end of the last.
-__device__ __forceinline__ int sort_segments(SortLds& s, int total, int* end)
+__device__ __forceinline__ int sort_segments(int* scan, int total, int* end)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int padded = (total + 15) & ~15;
@@ -96,13 +95,13 @@ __device__ __forceinline__ int sort_segments(SortLds& s, int total, int* end)
         const int t = __shfl_up(upto, d);
         if (lane >= d) upto += t;
     }
-    if (lane == 63) s.scan[wave] = upto;
+    if (lane == 63) scan[wave] = upto;
     __syncthreads();
     int before = 0, all = 0;
 #pragma unroll
     for (int w = 0; w < kSortWaves; ++w) {
-        if (w < wave) before += s.scan[w];
-        all += s.scan[w];
+        if (w < wave) before += scan[w];
+        all += scan[w];
     }
     *end = all;
     return before + upto - padded;
@@ -120,39 +119,88 @@ __device__ __forceinline__ void sort_finish(const SortArgs& a, int first, int to
     for (int64_t i = end + threadIdx.x; i < a.R; i += blockDim.x) a.rows[i] = -1;
 }
 
-__global__ __launch_bounds__(1024) void k_sort_one(SortArgs a)
+// from an expert's first row, thread e: that of every wavefront
+__device__ __forceinline__ void sort_first_rows(SortLds& s, int e, int next)
 {
-    __shared__ SortLds s;
-    SortRun run;
-    int64_t from, to;
-    sort_count(s, a, 0, a.T, run, from, to);
-    __syncthreads();
-    const int e = threadIdx.x;
-    int total = 0;
-    if (e < a.experts)
-        for (int w = 0; w < kSortWaves; ++w) total += s.count[w][e];
-    int end;
-    const int first = sort_segments(s, total, &end);
-    if (e < a.experts) {
-        int next = first;
-        for (int w = 0; w < kSortWaves; ++w) {
-            const int n = s.count[w][e];
-            s.count[w][e] = next;
-            next += n;
-        }
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+        const int n = s.count[w][e];
+        s.count[w][e] = next;
+        next += n;
     }
-    sort_finish(a, first, total, end);
-    __syncthreads();
-    sort_place(s, a, run, from, to);
 }
 
+// All of the sort, workgroup p placing choices 1024 p .. 1024 p + 1023.  (Up to eight experts counted in fields of a register, and those
+// added over the wavefront, took 0.9 us longer than the additions in LDS, 64 to eight words though they are.)
+template <int BITS>
+__global__ __launch_bounds__(1024) void k_sort_at_once(SortArgs a)
+{
+    __shared__ SortLds s;
+    __shared__ int before[kSortExperts], after[kSortExperts];   // choices of each expert in the parts before this one; in the others
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int part = blockIdx.x, T = (int)a.T, parts = (T + 1023) / 1024;
+    if (parts > 1) {                                            // (else the wavefronts' counts below say it all)
+        before[tid] = after[tid] = 0;
+        __syncthreads();
+        for (int p0 = 0; p0 < parts; p0 += 8) {                  // eight loads on their way
+            int expert[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int i = (p0 + u) * 1024 + tid;
+                expert[u] = i < T ? a.ids[i] : -1;
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int e = expert[u];
+                const bool live = (unsigned)e < (unsigned)a.experts, earlier = p0 + u < part;
+                // (a run of one expert is one addition, not 64 to one word)
+                int* const sum = earlier ? before : after;
+                if (__ballot(e == __builtin_amdgcn_readfirstlane(e)) == ~(uint64_t)0) {
+                    if (lane == 0 && live) atomicAdd(&sum[e], 64);
+                } else if (live) atomicAdd(&sum[e], 1);
+            }
+        }
+    }
+    const int number = part * 1024 + wave * 64, n = min(max(T - number, 0), 64);
+    SortRun<1> run;
+    sort_count<BITS>(s.count[wave], a.ids + number, n, a.experts, run);
+    __syncthreads();
+    int mine = 0, total = 0;
+    if (tid < a.experts && parts > 1) {
+        mine = before[tid];
+        total = mine + after[tid];
+    } else if (tid < a.experts) {
+#pragma unroll
+        for (int w = 0; w < kSortWaves; ++w) total += s.count[w][tid];
+    }
+    int end;
+    const int first = sort_segments(s.scan, total, &end);
+    if (tid < a.experts) sort_first_rows(s, tid, first + mine);
+    if (part == 0) sort_finish(a, first, total, end);
+    __syncthreads();
+    sort_place(s.count[wave], a, run, number, n);
+}
+
+constexpr int kSortRuns = kSortPart / kSortWaves / 64;          // of 64 choices, to a wavefront of a part
+
+// a wavefront's choices of part blockIdx.x: equal runs of whole 64s
+__device__ __forceinline__ void sort_share(const SortArgs& a, int64_t& number, int& n)
+{
+    const int64_t first = (int64_t)blockIdx.x * kSortPart;
+    const int in_part = (int)min((int64_t)kSortPart, a.T - first), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    number = first + wave * 64 * kSortRuns;
+    n = min(max(in_part - wave * 64 * kSortRuns, 0), 64 * kSortRuns);
+}
+
+template <int BITS>
 __global__ __launch_bounds__(1024) void k_sort_count(SortArgs a)
 {
     __shared__ SortLds s;
-    const int64_t first = (int64_t)blockIdx.x * kSortPart;
-    SortRun run;
-    int64_t from, to;
-    sort_count(s, a, first, min(first + kSortPart, a.T), run, from, to);
+    SortRun<kSortRuns> run;
+    int64_t number;
+    int n;
+    sort_share(a, number, n);
+    sort_count<BITS>(s.count[threadIdx.x >> 6], a.ids + number, n, a.experts, run);
     __syncthreads();
     for (int e = threadIdx.x; e < a.experts; e += blockDim.x) {
         int total = 0;
@@ -164,7 +212,7 @@ __global__ __launch_bounds__(1024) void k_sort_count(SortArgs a)
 // counts of the parts -> the first row that each part gives out
 __global__ __launch_bounds__(1024) void k_sort_scan(SortArgs a, int parts)
 {
-    __shared__ SortLds s;
+    __shared__ int scan[kSortWaves];
     const int e = threadIdx.x;
     int total = 0;
     if (e < a.experts) {
@@ -172,7 +220,7 @@ __global__ __launch_bounds__(1024) void k_sort_scan(SortArgs a, int parts)
         for (int p = 0; p < parts; ++p) total += a.workspace[(int64_t)p * a.experts + e];
     }
     int end;
-    const int first = sort_segments(s, total, &end);
+    const int first = sort_segments(scan, total, &end);
     if (e < a.experts) {
         int next = first;
 #pragma unroll 8
@@ -185,35 +233,40 @@ __global__ __launch_bounds__(1024) void k_sort_scan(SortArgs a, int parts)
     sort_finish(a, first, total, end);
 }
 
+template <int BITS>
 __global__ __launch_bounds__(1024) void k_sort_place(SortArgs a)
 {
     __shared__ SortLds s;
-    const int64_t first = (int64_t)blockIdx.x * kSortPart, last = min(first + kSortPart, a.T);
-    SortRun run;
-    int64_t from, to;
-    sort_count(s, a, first, last, run, from, to);
+    SortRun<kSortRuns> run;
+    int64_t number;
+    int n;
+    sort_share(a, number, n);
+    sort_count<BITS>(s.count[threadIdx.x >> 6], a.ids + number, n, a.experts, run);
     __syncthreads();
-    for (int e = threadIdx.x; e < a.experts; e += blockDim.x) {
-        int next = a.workspace[(int64_t)blockIdx.x * a.experts + e];
-        for (int w = 0; w < kSortWaves; ++w) {
-            const int n = s.count[w][e];
-            s.count[w][e] = next;
-            next += n;
-        }
+    for (int e = threadIdx.x; e < a.experts; e += blockDim.x) sort_first_rows(s, e, a.workspace[(int64_t)blockIdx.x * a.experts + e]);
+    __syncthreads();
+    sort_place(s.count[threadIdx.x >> 6], a, run, number, n);
+}
+
+template <int BITS>
+static void run_sort(const SortArgs& a, hipStream_t st)
+{
+    if (a.T <= kSortAtOnce) {
+        const unsigned parts = a.T > 1024 ? (unsigned)((a.T + 1023) / 1024) : 1u;
+        k_sort_at_once<BITS><<<parts, 1024, 0, st>>>(a);
+        return;
     }
-    __syncthreads();
-    sort_place(s, a, run, from, to);
+    const int parts = (int)((a.T + kSortPart - 1) / kSortPart);
+    k_sort_count<BITS><<<parts, 1024, 0, st>>>(a);
+    k_sort_scan<<<1, 1024, 0, st>>>(a, parts);
+    k_sort_place<BITS><<<parts, 1024, 0, st>>>(a);
 }
 
 sp24_status launch_moe_sort(const SortArgs& a, hipStream_t st)
 {
-    const int parts = (int)((a.T + kSortPart - 1) / kSortPart);
-    if (parts <= 1) k_sort_one<<<1, 1024, 0, st>>>(a);
-    else {
-        k_sort_count<<<parts, 1024, 0, st>>>(a);
-        k_sort_scan<<<1, 1024, 0, st>>>(a, parts);
-        k_sort_place<<<parts, 1024, 0, st>>>(a);
-    }
+    if (a.experts <= 8) run_sort<3>(a, st);
+    else if (a.experts <= 64) run_sort<6>(a, st);
+    else run_sort<10>(a, st);
     return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
 }
 

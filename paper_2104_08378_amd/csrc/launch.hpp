@@ -130,7 +130,8 @@ struct LinearGradArgs {
 };
 sp24_status launch_linear_grad(const LinearGradArgs& a, hipStream_t st);
 
-constexpr int kSortPart = 16384;          // choices that one workgroup sorts
+constexpr int kSortAtOnce = 1 << 17;      // choices that one launch sorts; of more, parts of kSortPart
+constexpr int kSortPart = 16384;
 struct SortArgs {
     const int32_t* ids;                   // T choices
     int32_t *offsets, *slots, *rows, *workspace;      // workspace: experts words for every part where there are several

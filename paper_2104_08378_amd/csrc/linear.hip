@@ -97,6 +97,7 @@ constexpr LayerCost kLayerCosts[] = {
     {LayerTile::t64x32, 64, 32, false, 3.8, 0.12, 0.092, 0.74, 4.1, 0.10, 0.17, 0.48},
     {LayerTile::t128x64, 128, 64, false, 4.5, 0.16, 0.24, 2.2, 5.1, 0.19, 0.47, 1.5},
     {LayerTile::t128x128, 128, 128, false, 4.8, 0.26, 0.43, 2.4, 5.4, 0.35, 0.74, 1.0},
+    {LayerTile::t128x128_one, 128, 128, true, 6.2, 0.25, 0.29, 5.3, 6.8, 0.36, 0.45, 5.7},
     {LayerTile::t256x128, 256, 128, true, 7.3, 0.32, 0.80, 1.0, 7.4, 0.57, 1.25, 1.0},
 };
 
@@ -109,7 +110,7 @@ static LayerTile cheapest(const MmArgs& a, int stream_width, bool grouped, F&& w
     LayerTile best = LayerTile::t64x32;
     for (const LayerCost& c : kLayerCosts) {
         if (c.tile == LayerTile::stream && c.columns != stream_width) continue;
-        if (c.tile == LayerTile::t256x128 && grouped) continue;
+        if (grouped && (c.tile == LayerTile::t256x128 || c.tile == LayerTile::t128x128_one)) continue;
         const bool canonical = a.layout == SP24_LAYOUT_CANONICAL;
         double units = workgroups(c) / 256;
         if (c.whole_rounds && units > 1) units = std::ceil(units);

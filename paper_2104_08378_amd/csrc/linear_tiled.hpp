@@ -23,9 +23,12 @@ sp24_status layer_tiled(const ARGS& a, LayerTile tile, hipStream_t st)
     case LayerTile::t64x32: return run_layer<DT, 2, 1, 1, 1, 4>(a, st);
     case LayerTile::t128x64: return run_layer<DT, 4, 1, 1, 2, 4>(a, st);
     case LayerTile::t128x128: return run_layer<DT, 4, 2, 1, 2, 3>(a, st);
+    case LayerTile::t128x128_one:
+        if constexpr (!std::is_same<ARGS, GroupedArgs>::value) return run_layer<DT, 2, 2, 2, 2, 6>(a, st);
+        return SP24_ERR_LAUNCH;
     case LayerTile::t256x128:
         if constexpr (!std::is_same<ARGS, GroupedArgs>::value) return run_layer<DT, 4, 2, 2, 2, 4>(a, st);
-        return SP24_ERR_LAUNCH;                                  // (not a choice for experts' rows)
+        return SP24_ERR_LAUNCH;                                  // (neither is a choice for experts' rows)
     default: return run_layer<DT, 4, 2, 2, 4, 3>(a, st);
     }
 }

@@ -333,6 +333,7 @@ static sp24_status run_norm(const RowsArgs& a, hipStream_t st)
         kernel<<<(unsigned)(a.N < most ? a.N : most), threads, 0, st>>>(a);
         return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
     };
+    if (!whole && many && a.H > 512 && a.H <= 4096) return run(k_norm_rows<T, OUT, 2, NORM, false, 256>, row_threads(a.H, 2));
     if (whole && many && a.H > 512 && a.H <= 4096) return run(k_norm_rows<T, OUT, 2, NORM, true, 256>, row_threads(a.H, 2));
     if (whole && many && a.H > 4096 && a.H <= 8192) return run(k_norm_rows<T, OUT, 4, NORM, true, 256>, row_threads(a.H, 4));
     if (a.H <= 8192) {

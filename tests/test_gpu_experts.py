@@ -22,6 +22,7 @@ def choices(g, N, topk, E, dropped):
 @pytest.mark.parametrize("N,topk,E,dropped", [
     (0, 2, 4, 0), (1, 1, 1, 0), (1, 2, 8, 0), (16, 2, 8, 0), (63, 1, 3, 0), (64, 1, 64, 0.3), (65, 1, 65, 0), (100, 4, 1024, 0.1), (700, 3, 7, 0.2),
     (1024, 1, 1, 0), (4096, 2, 8, 0), (4096, 4, 64, 0.05), (5461, 3, 128, 0), (16384, 1, 5, 0), (16385, 1, 1000, 0.1), (20000, 4, 33, 0), (30, 2, 4, 1.0),
+    (65536, 2, 8, 0.1), (65536, 2, 9, 0), (131073, 1, 3, 0), (70001, 2, 700, 0.05),
 ])
 def test_sort(N, topk, E, dropped):
     g = torch.Generator().manual_seed(N + E)
@@ -35,10 +36,11 @@ def test_sort(N, topk, E, dropped):
 def test_sort_of_one_expert_only():
     """All choices on one expert, at either end; long runs of one key cross every wavefront and part."""
     for E, which in ((8, 0), (8, 7), (1024, 1023)):
-        ids = torch.full((20000, 2), which, dtype=torch.int32, device="cuda")
-        offsets, slots, rows = sp24.sp24_moe_sort(ids, E)
-        assert torch.equal(slots.reshape(-1), torch.arange(40000, dtype=torch.int32, device="cuda")) and torch.equal(rows[:40000], slots.reshape(-1))
-        assert bool((rows[40000:] == -1).all()) and offsets.cpu().tolist() == [0] * (which + 1) + [40000] * (E - which)
+        for N in (20000, 80000):
+            ids = torch.full((N, 2), which, dtype=torch.int32, device="cuda")
+            offsets, slots, rows = sp24.sp24_moe_sort(ids, E)
+            assert torch.equal(slots.reshape(-1), torch.arange(2 * N, dtype=torch.int32, device="cuda")) and torch.equal(rows[:2 * N], slots.reshape(-1))
+            assert bool((rows[2 * N:] == -1).all()) and offsets.cpu().tolist() == [0] * (which + 1) + [2 * N] * (E - which)
 
 
 SHAPES = [(1, 1, 1, 8, 0, 0), (5, 2, 4, 7, 0, 0), (16, 2, 8, 64, 0.3, 0), (33, 3, 5, 1000, 0.2, 3), (300, 2, 8, 72, 0, 8), (64, 8, 16, 2056, 0.1, 0), (9, 1, 64, 4097, 0, 1),
@@ -148,5 +150,5 @@ def test_refusals():
         sp24.sp24_moe_gather(x, rows, 0)
     assert e.value.status == 2
     with pytest.raises(sp24.Sp24Error) as e:
-        sp24.sp24_moe_sort(torch.zeros(16385, 1, dtype=torch.int32, device="cuda"), 64, workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))
+        sp24.sp24_moe_sort(torch.zeros((1 << 17) + 1, 1, dtype=torch.int32, device="cuda"), 64, workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))
     assert e.value.status == 2

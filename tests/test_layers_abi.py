@@ -82,12 +82,12 @@ def test_sort_gather_and_combine():
     L = sp24.lib()
     assert [sp24.sp24_moe_rows(t, e) for t, e in ((0, 8), (1, 8), (16, 1), (17, 1), (32, 8), (100, 1024))] == [0, 16, 16 + 0 * 1, 32, 144, 1600]
     assert sp24.sp24_moe_rows(-1, 8) == 0 and sp24.sp24_moe_rows(8, 0) == 0 and sp24.sp24_moe_rows(8, 1025) == 0
-    assert L.sp24_moe_sort_workspace_bytes(16384, 8) == 0 and L.sp24_moe_sort_workspace_bytes(16385, 8) == 2 * 8 * 4
+    assert L.sp24_moe_sort_workspace_bytes(1 << 17, 8) == 0 and L.sp24_moe_sort_workspace_bytes((1 << 17) + 1, 8) == 9 * 8 * 4
 
     def sort(ids=A, of=B, sl=C, ro=D, T=100, n=8, R=220, ws=0, bytes=0):
         return L.sp24_moe_sort(ids, of, sl, ro, T, n, R, ws, bytes, None)
     assert sort(ids=0) == NULL and sort(of=0) == NULL and sort(sl=0) == NULL and sort(ro=0) == NULL and sort(R=200) == SHAPE and sort(n=0) == SHAPE and sort(T=-1) == SHAPE
-    assert sort(ids=A + 2) == ALIGN and sort(sl=A) == SHAPE and sort(ro=B) == SHAPE and sort(T=20000, R=21000) == NULL and sort(T=20000, R=21000, ws=E, bytes=32) == SHAPE
+    assert sort(ids=A + 2) == ALIGN and sort(sl=A) == SHAPE and sort(ro=B) == SHAPE and sort(T=200000, R=201000) == NULL and sort(T=200000, R=201000, ws=E, bytes=32) == SHAPE
 
     def gather(X=A, sc=0, ro=B, Xs=C, so=0, N=8, R=32, k=2, H=64, ldx=64, ldxs=64, t=sp24.I8):
         return L.sp24_moe_gather(X, sc, ro, Xs, so, N, R, k, H, ldx, ldxs, t, None)
