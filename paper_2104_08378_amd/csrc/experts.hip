@@ -1,5 +1,7 @@
 // Tokens in order of their expert and back: the sort of the router's choices, the rows gathered, the weighted sum of what comes back, and
 // that sum's gradients.
+#include <algorithm>
+
 #include "launch.hpp"
 #include "rowops.hpp"
 
@@ -412,7 +414,7 @@ __global__ __launch_bounds__(256) void k_moe_combine_grad(CombineGradArgs a)
 
 sp24_status launch_moe_combine_grad(const CombineGradArgs& a, hipStream_t st)
 {
-    const unsigned grid = (unsigned)((a.R + 3) / 4);
+    const unsigned grid = (unsigned)std::max<int64_t>((a.R + 3) / 4, 1);       // (choices without rows have gradients to write)
     if (a.t == SP24_F32) k_moe_combine_grad<SP24_F32><<<grid, 256, 0, st>>>(a);
     else if (a.t == SP24_F16) k_moe_combine_grad<SP24_F16><<<grid, 256, 0, st>>>(a);
     else k_moe_combine_grad<SP24_BF16><<<grid, 256, 0, st>>>(a);

@@ -131,6 +131,17 @@ def test_combine_gradients_against_differences():
     assert float((ref.d(xs) * VY).sum()) == pytest.approx(float((ref.d(sp24.sp24_moe_combine(vy, slots)) * x.double()).sum()), rel=1e-5)
 
 
+def test_nothing_has_a_row():
+    slots, none = torch.full((5, 2), -1, dtype=torch.int32, device="cuda"), torch.empty(0, 64, dtype=BF16, device="cuda")
+    x, w = torch.ones(5, 64, dtype=BF16, device="cuda"), torch.ones(5, 2, device="cuda")
+    rows = torch.empty(0, dtype=torch.int32, device="cuda")
+    assert bool((sp24.sp24_moe_combine(none, slots, w) == 0).all()) and torch.equal(sp24.sp24_moe_combine(none, slots, w, residual=x), x)
+    dy, dw = sp24.sp24_moe_combine_backward(x, none, slots, rows, w)
+    assert tuple(dy.shape) == (0, 64) and bool((dw == 0).all())
+    xs, scales = sp24.sp24_moe_gather(torch.empty(0, 64, dtype=I8, device="cuda"), torch.full((16,), -1, dtype=torch.int32, device="cuda"), 2, scale=torch.empty(0, device="cuda"))
+    assert bool((xs == 0).all()) and bool((scales == 0).all())
+
+
 def test_refusals():
     ids = torch.zeros(4, 2, dtype=torch.int32, device="cuda")
     offsets, slots, rows = sp24.sp24_moe_sort(ids, 4)

@@ -147,6 +147,31 @@ def test_norm_gradients_against_differences():
         assert abs(float(got - slope)) <= 1e-4 * float((ref.d(dx) * vx).abs().sum()) / H ** 0.5
 
 
+@pytest.mark.parametrize("N,H,out", [(9000, 4096, F8), (8300, 1032, BF16), (33000, 72, I8), (9001, 1024, F16)])
+def test_more_rows_than_workgroups(N, H, out):
+    """Workgroups that take several rows: the last ones and some others."""
+    g = torch.Generator().manual_seed(N)
+    x, w = torch.randn(N, H, generator=g).to(BF16).cuda(), (1 + 0.2 * torch.randn(H, generator=g)).cuda()
+    n = sp24.sp24_rmsnorm(x, w, EPS, residual=x, out_dtype=out, want_rstd=True)
+    at = torch.cat([torch.arange(N - 40, N), torch.arange(0, N, 997), torch.arange(8180, 8200)]).cuda()
+    h, rstd, want = ref.norm(x[at], w, EPS, x[at])
+    ref.close(n.rstd[at], rstd, rel(H) * rstd, "rstd")
+    ref.close(n.hidden[at], h, h.abs() * 2.0 ** -24, "h")
+    if out in (I8, F8):
+        s, q, top = ref.d(n.scale[at])[:, None], ref.d(n.y[at]), want.abs().amax(1)[:, None]
+        ref.close(n.scale[at], top[:, 0] / ref.TOP[out], (rel(H) + 2.0 ** -21) * top[:, 0] / ref.TOP[out], "scale")
+        step = 0.5 * s if out == I8 else torch.maximum(want.abs() * 2.0 ** -4, s * 2.0 ** -10)
+        assert bool(((q * s - want).abs() <= step * (1 + 1e-5) + 2 * (rel(H) + 2.0 ** -21) * top).all())
+    else:
+        ref.close(n.y[at], want, rel(H) * want.abs() + 2.0 ** -24 * ref.d(w).abs() * rstd[:, None], "y")
+    # and the gradients, whose workgroups take several rows each
+    dx, dw = sp24.sp24_rmsnorm_backward(x, n.hidden, w, n.rstd)
+    want_dx, _ = ref.norm_grad(x[at], n.hidden[at], w, n.rstd[at])
+    ref.close(dx[at], want_dx, 2.0 ** -17 * want_dx.abs().amax(1, keepdim=True), "dx")
+    dy, hh, v = (t.double() for t in (x, n.hidden, n.rstd[:, None]))
+    ref.close(dw, (dy * hh * v).sum(0).cpu(), ((dy * hh * v).abs().sum(0) * (N + 4) * 2.0 ** -24).cpu(), "dw")
+
+
 def test_no_rows():
     w = torch.ones(64, device="cuda")
     none = torch.empty(0, 64, dtype=BF16, device="cuda")
