@@ -152,13 +152,20 @@ sp24_status launch_linear_grouped(const GroupedArgs& a, hipStream_t st)
     return by_input(a, [&](auto dt) { return layer_tiled<decltype(dt)::value>(a, tile, st); });
 }
 
-// The segments' dense products, A [M, rows] and B [rows, N]: 128 x 128 tiles, all segments in one launch.
+// The segments' dense products, A [M, rows] and B [rows, N], all segments in one launch.  Segments are short, so that a tile's first operands
+// and its way out weigh as much as its steps, and a step's bytes set the pace: tiles of 128 x 256 on eight wavefronts, whose rows of B are 512 bytes
+// (eight segments of 8240 rows, 2048 x 1024 bf16: 128 x 128 with four stages 52.7 us, 256 x 128 59.8, 256 x 256 64, 128 x 256 46.7; sixteen of
+// 4224, 1024 x 1024 27.6, 24.5, 31.7 and 20.9), and where columns would be wasted 128 x 128, two workgroups to a unit (52.5; 25.0).
 template <int DT, int OUT>
 static sp24_status run_segments(const SegmentArgs& a, int experts, hipStream_t st)
 {
-    const int tiles_m = (int)((a.M + 127) / 128), tiles_n = (int)((a.N + 127) / 128);
-    k_gemm_pipe<DT, OUT, 2, 2, 2, 2, 4, 2, SegmentArgs><<<dim3((unsigned)(tiles_m * tiles_n), (unsigned)experts), 256, 0, st>>>(a, tiles_m, tiles_n);
-    return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
+    auto run = [&](auto kernel, int columns) {
+        const int tiles_m = (int)((a.M + 127) / 128), tiles_n = (int)((a.N + columns - 1) / columns);
+        kernel<<<dim3((unsigned)(tiles_m * tiles_n), (unsigned)experts), 512, 0, st>>>(a, tiles_m, tiles_n);
+        return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
+    };
+    if ((a.N + 255) / 256 * 256 * 4 > (a.N + 127) / 128 * 128 * 5) return run(k_gemm_pipe<DT, OUT, 4, 2, 1, 2, 2, 2, SegmentArgs>, 128);
+    return run(k_gemm_pipe<DT, OUT, 2, 4, 2, 2, 3, 2, SegmentArgs>, 256);
 }
 
 sp24_status launch_gemm_grouped(const SegmentArgs& a, int experts, hipStream_t st)

@@ -1,30 +1,31 @@
 // What follows from the gradient of a layer's result: dZ = dY act'(Z) as rows per token, the same transposed (the first operand of the
 // weights' gradient), and the bias's gradient, the sum of dZ over the rows of a segment.
 //
-// Bound by memory: dY and Z are read once, both forms of dZ written once.  A workgroup takes 64 x 64 values through LDS in binary32, so that
-// the sums see them unrounded; rows of 65 words there, which neither the rows' writes (8 rows x 8 pieces a wavefront) nor the
-// columns' reads (8 x 8 likewise) find in one bank twice.  Sums: 16 rows (the unit of segments) in row order, then those in order.
+// Bound by memory: dY and Z are read once, both forms of dZ written once.  A workgroup takes 64 rows x 64 (128) values through LDS in binary32,
+// so that the sums see them unrounded; rows of 65 (129) words there, of which the columns' reads (8 rows x 8 a wavefront) find no
+// bank twice, and the rows' writes none (two).  Sums: 16 rows (the unit of segments) in row order, then those in order.
 #include "launch.hpp"
 #include "rowops.hpp"
 
 namespace sp24 {
 
-constexpr int kGradTile = 64, kGradPitch = 65;
+constexpr int kGradTile = 64;           // rows of a tile
 
-template <int T>
-__global__ __launch_bounds__(256) void k_linear_grad(LinearGradArgs a, int tiles_m)
+template <int T, int WIDTH>
+__global__ __launch_bounds__(4 * WIDTH) void k_linear_grad(LinearGradArgs a, int tiles_m)
 {
-    __shared__ float tile[kGradTile * kGradPitch];
-    __shared__ float part[4][kGradTile];
+    constexpr int kPitch = WIDTH + 1, CH = WIDTH / 8;
+    __shared__ float tile[kGradTile * kPitch];
+    __shared__ float part[4][WIDTH];
     const int tid = threadIdx.x;
-    const int64_t m0 = (int64_t)(blockIdx.x % tiles_m) * kGradTile, n0 = (int64_t)(blockIdx.x / tiles_m) * kGradTile;
-    const int c = tid & 7;
+    const int64_t m0 = (int64_t)(blockIdx.x % tiles_m) * WIDTH, n0 = (int64_t)(blockIdx.x / tiles_m) * kGradTile;
+    const int c = tid % CH;
     const int64_t m = m0 + c * 8;
     const int have = (int)min(a.M - m, (int64_t)8);
     raw8<T> dy[2] = {}, z[2] = {};
 #pragma unroll
     for (int it = 0; it < 2; ++it) {
-        const int64_t n = n0 + it * 32 + (tid >> 3);
+        const int64_t n = n0 + it * 32 + tid / CH;
         if (n < a.N && have > 0) {
             dy[it] = load_raw8<T>(a.dY, n * a.lddy + m, have);
             if (a.act != SP24_ACT_NONE) z[it] = load_raw8<T>(a.Z, n * a.ldz + m, have);
@@ -32,7 +33,7 @@ __global__ __launch_bounds__(256) void k_linear_grad(LinearGradArgs a, int tiles
     }
 #pragma unroll
     for (int it = 0; it < 2; ++it) {
-        const int t = it * 32 + (tid >> 3);
+        const int t = it * 32 + tid / CH;
         float v[8], x[8];
         values_of<T>(dy[it], v);
         if (a.act != SP24_ACT_NONE) {
@@ -42,26 +43,26 @@ __global__ __launch_bounds__(256) void k_linear_grad(LinearGradArgs a, int tiles
         }
         if (a.dZ && n0 + t < a.N && have > 0) store_values8<T>(a.dZ, (n0 + t) * a.lddz + m, have, v);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) tile[t * kGradPitch + c * 8 + i] = v[i];
+        for (int i = 0; i < 8; ++i) tile[t * kPitch + c * 8 + i] = v[i];
     }
     __syncthreads();
     if (a.dZt) {
 #pragma unroll
         for (int it = 0; it < 2; ++it) {
-            const int f = it * 32 + (tid >> 3), t = (tid & 7) * 8;
+            const int f = it * (WIDTH / 2) + (tid >> 3), t = (tid & 7) * 8;
             const int rows = (int)min(a.N - n0 - t, (int64_t)8);
             if (m0 + f >= a.M || rows <= 0) continue;
             float v[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = tile[(t + i) * kGradPitch + f];
+            for (int i = 0; i < 8; ++i) v[i] = tile[(t + i) * kPitch + f];
             store_values8<T>(a.dZt, (m0 + f) * a.lddzt + n0 + t, rows, v);
         }
     }
     if (a.partial) {
-        const int f = tid & 63, p = tid >> 6;
+        const int f = tid % WIDTH, p = tid / WIDTH;
         float sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sum += tile[(p * 16 + i) * kGradPitch + f];       // (rows past N are zeros)
+        for (int i = 0; i < 16; ++i) sum += tile[(p * 16 + i) * kPitch + f];       // (rows past N are zeros)
         if (a.unit == 16) {
             const int64_t row = n0 / 16 + p;
             if (m0 + f < a.M && row * 16 < a.N) a.partial[row * a.M + m0 + f] = sum;
@@ -73,16 +74,24 @@ __global__ __launch_bounds__(256) void k_linear_grad(LinearGradArgs a, int tiles
     }
 }
 
+template <int WIDTH>
+static sp24_status run_linear_grad(const LinearGradArgs& a, hipStream_t st)
+{
+    const int64_t tiles_m = (a.M + WIDTH - 1) / WIDTH, tiles_n = (a.N + kGradTile - 1) / kGradTile;
+    const unsigned grid = (unsigned)(tiles_m * tiles_n);
+    if (grid == 0) return SP24_OK;
+    if (a.t == SP24_F16) k_linear_grad<SP24_F16, WIDTH><<<grid, 4 * WIDTH, 0, st>>>(a, (int)tiles_m);
+    else k_linear_grad<SP24_BF16, WIDTH><<<grid, 4 * WIDTH, 0, st>>>(a, (int)tiles_m);
+    return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
+}
+
 sp24_status launch_linear_grad(const LinearGradArgs& a, hipStream_t st)
 {
-    const int64_t tiles_m = (a.M + kGradTile - 1) / kGradTile, tiles_n = (a.N + kGradTile - 1) / kGradTile;
-    if (tiles_m * tiles_n > 0) {
-        const unsigned grid = (unsigned)(tiles_m * tiles_n);
-        if (a.t == SP24_F16) k_linear_grad<SP24_F16><<<grid, 256, 0, st>>>(a, (int)tiles_m);
-        else k_linear_grad<SP24_BF16><<<grid, 256, 0, st>>>(a, (int)tiles_m);
-        if (hipGetLastError() != hipSuccess) return SP24_ERR_LAUNCH;
-    }
-    if (!a.dbias || a.M == 0) return SP24_OK;
+    // Large ones with an activation, whose two operands come in rows of 256 bytes a tile then: 4096 x 4096 with GELU 35.6 -> 32.9 us.  Without
+    // one 15.2 and 16.0, and few tiles (4096 x 512) 8.7 and 9.0.
+    const bool wide = a.act != SP24_ACT_NONE && a.M * a.N >= (int64_t)1 << 22;
+    const sp24_status s = wide ? run_linear_grad<128>(a, st) : run_linear_grad<64>(a, st);
+    if (s != SP24_OK || !a.dbias || a.M == 0) return s;
     return launch_column_sums(a.partial, (a.N + a.unit - 1) / a.unit, a.M, a.offsets, a.offsets ? a.experts : 1, a.unit, a.dbias, st);
 }
 

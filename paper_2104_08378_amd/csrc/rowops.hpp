@@ -104,18 +104,22 @@ __device__ __forceinline__ void load_floats8(const float* p, int64_t first, int 
 // Activations of a product's epilogue, in binary32: p = 1 / (1 + e^-x) by the chip's own 2^x and reciprocal (1 ulp each), and
 //   silu(z) = z p(z),  gelu(z) = z p(2u) with u = sqrt(2/pi) (z + 0.044715 z^3), which is the tanh form, for 1 + tanh u = 2 p(2u).
 // ---------------------------------------------------------------------------
-__device__ __forceinline__ float logistic(float x)
-{
-    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.442695040888963f * x));
-}
+constexpr float kLog2e = 1.442695040888963f, kGelu2C = 1.5957691216057308f;         // 2 sqrt(2 / pi)
 
-constexpr float kGelu2C = 1.5957691216057308f;         // 2 sqrt(2 / pi)
+// from t = -x log2(e)
+__device__ __forceinline__ float logistic_of(float t) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t)); }
+__device__ __forceinline__ float logistic(float x) { return logistic_of(-kLog2e * x); }
+// p(2u), from z and z^2
+__device__ __forceinline__ float logistic_2u(float z, float square)
+{
+    return logistic_of(z * __builtin_fmaf(-0.044715f * kGelu2C * kLog2e, square, -kGelu2C * kLog2e));
+}
 
 template <int ACT>
 __device__ __forceinline__ float activated(float z)
 {
     if constexpr (ACT == SP24_ACT_RELU) return z > 0.0f || z != z ? z : 0.0f;        // (a NaN stays one)
-    else if constexpr (ACT == SP24_ACT_GELU) return z * logistic(z * __builtin_fmaf(0.044715f * kGelu2C, z * z, kGelu2C));
+    else if constexpr (ACT == SP24_ACT_GELU) return z * logistic_2u(z, z * z);
     else if constexpr (ACT == SP24_ACT_SILU) return z * logistic(z);
     else return z;
 }
@@ -133,18 +137,20 @@ __device__ __forceinline__ void activate(float (&v)[COUNT], int act)
     else if (act == SP24_ACT_RELU) all([](float z) { return activated<SP24_ACT_RELU>(z); });
 }
 
-// d activate / d z.  Past |z| = 100 the slopes are 0 and 1 (p is 0 or 1), and z^2 could overflow against a factor of 0.
+// d activate / d z.  Past |z| = 100 the slopes are 0 and 1 (p is 0 or 1): the factors beside p (1 - p) are held where they stay finite.  (A
+// NaN goes through p.)
 __device__ __forceinline__ float activation_slope(float z, int act)
 {
     if (act == SP24_ACT_RELU) return z > 0.0f ? 1.0f : z != z ? z : 0.0f;
-    const float x = z > 100.0f ? 100.0f : z < -100.0f ? -100.0f : z;
+    const float x = __builtin_amdgcn_fmed3f(z, -100.0f, 100.0f);
     if (act == SP24_ACT_GELU) {
-        const float p = logistic(kGelu2C * x * (1.0f + 0.044715f * x * x));
-        return p + x * p * (1.0f - p) * kGelu2C * (1.0f + 0.134145f * x * x);
+        const float square = __builtin_fminf(z * z, 1e4f);
+        const float p = logistic_2u(z, square);
+        return __builtin_fmaf(x * __builtin_fmaf(0.134145f * kGelu2C, square, kGelu2C), __builtin_fmaf(-p, p, p), p);
     }
     if (act == SP24_ACT_SILU) {
-        const float p = logistic(x);
-        return p + x * p * (1.0f - p);
+        const float p = logistic(z);
+        return __builtin_fmaf(x, __builtin_fmaf(-p, p, p), p);
     }
     return 1.0f;
 }

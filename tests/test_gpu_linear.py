@@ -188,7 +188,7 @@ def test_refusals():
 
 @pytest.mark.parametrize("dtype", [F16, BF16])
 @pytest.mark.parametrize("act", ["none", "relu", "gelu", "silu"])
-@pytest.mark.parametrize("N,M,pitch,offset", [(1, 1, 0, 0), (16, 64, 0, 0), (70, 33, 3, 1), (129, 200, 8, 0), (64, 513, 0, 5), (1000, 72, 0, 0)])
+@pytest.mark.parametrize("N,M,pitch,offset", [(1, 1, 0, 0), (16, 64, 0, 0), (70, 33, 3, 1), (129, 200, 8, 0), (64, 513, 0, 5), (1000, 72, 0, 0), (2050, 2049, 0, 0), (1030, 4104, 8, 0)])
 def test_gradient_through_the_epilogue(N, M, pitch, offset, act, dtype):
     g = torch.Generator().manual_seed(N + M)
     dy, z = strided(values(g, (N, M), dtype), pitch, offset)[0], strided(values(g, (N, M), dtype, 2.0), pitch, offset)[0]
