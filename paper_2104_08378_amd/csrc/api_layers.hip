@@ -10,7 +10,7 @@ using namespace sp24;
 
 namespace {
 
-constexpr int64_t kMostRows = ((int64_t)1 << 31) - 64, kMostNorm = 32768, kMostQuantised = 65536;
+constexpr int64_t kMostRows = ((int64_t)1 << 31) - 64, kMostMm = (int64_t)1 << 30, kMostNorm = 32768, kMostQuantised = 65536;
 
 bool is_float16(sp24_dtype t) { return t == SP24_F16 || t == SP24_BF16; }
 bool is_float(sp24_dtype t) { return is_float16(t) || t == SP24_F32; }
@@ -143,7 +143,7 @@ static sp24_status check_linear(const LinearArgs& a, int64_t rows, int64_t weigh
     if (!is_input_type(a.in) || !is_float(a.out)) return SP24_ERR_DTYPE;
     if (!is_act((sp24_act)a.act)) return SP24_ERR_DTYPE;
     if (!is_layout(a.layout)) return SP24_ERR_LAYOUT;
-    if (a.M < 0 || rows < 0 || rows > kMostRows || a.M > kMostRows || weight_rows > ((int64_t)1 << 40) || !k_legal(a.K, a.in)) return SP24_ERR_SHAPE;
+    if (a.M < 0 || rows < 0 || rows > kMostMm || a.M > kMostMm || a.K > kMostMm || !k_legal(a.K, a.in)) return SP24_ERR_SHAPE;
     if (!layout_fits(a.M, a.K, a.layout)) return SP24_ERR_LAYOUT;
     if (!is_code(a.in) && (a.epi.w_scale || a.x_scale)) return SP24_ERR_DTYPE;
     if (a.M == 0 || rows == 0) return SP24_OK;

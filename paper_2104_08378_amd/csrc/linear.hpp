@@ -320,10 +320,11 @@ __device__ __forceinline__ void LinearArgs::store_wave(typename acc_of<DT>::type
     });
 }
 
-// ---- host side: the tiled and the streaming kernels, compiled per input type ----
+// ---- host side: the tiled, the staged and the streaming kernels, compiled per input type ----
 // (t128x128_one: six stages, one workgroup to a unit; t128x128: three stages, two)
 enum class LayerTile { stream, t64x32, t128x64, t128x128, t128x128_one, t256x128, t256x256 };
 template <int DT, class ARGS> sp24_status layer_tiled(const ARGS& a, LayerTile tile, hipStream_t st);
+template <int DT, class ARGS> sp24_status layer_staged(const ARGS& a, hipStream_t st);
 sp24_status launch_linear_stream(const LinearArgs& a, hipStream_t st);
 sp24_status launch_grouped_stream(const GroupedArgs& a, hipStream_t st);
 

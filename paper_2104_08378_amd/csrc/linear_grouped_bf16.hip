@@ -1,8 +1,9 @@
-// Rows of experts on the tiled kernels, bf16 inputs.
+// Rows of experts on the tiled and the staged kernels, bf16 inputs.
 #include "linear_tiled.hpp"
 
 namespace sp24 {
 
 template sp24_status layer_tiled<SP24_BF16>(const GroupedArgs& a, LayerTile tile, hipStream_t st);
+template sp24_status layer_staged<SP24_BF16>(const GroupedArgs& a, hipStream_t st);
 
 } // namespace sp24

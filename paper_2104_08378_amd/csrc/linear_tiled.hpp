@@ -1,6 +1,7 @@
-// Layers on the tiled kernels, compiled per input type.
+// Layers on the tiled kernels, and on those that stage X through registers, compiled per input type.
 #pragma once
 #include "linear.hpp"
+#include "mm_staged.hpp"
 
 namespace sp24 {
 
@@ -31,6 +32,23 @@ sp24_status layer_tiled(const ARGS& a, LayerTile tile, hipStream_t st)
         return SP24_ERR_LAUNCH;                                  // (neither is a choice for experts' rows)
     default: return run_layer<DT, 4, 2, 2, 4, 3>(a, st);
     }
+}
+
+// Rows of X at any address, any legal K.  The tiles are those of the plain product there (its lines in run_staged_from).
+template <int DT, class ARGS>
+sp24_status layer_staged(const ARGS& a, hipStream_t st)
+{
+    auto run = [&](auto kernel, int bm, int bn) {
+        const int64_t tiles_m = (a.M + bm - 1) / bm;
+        int64_t tiles_n;
+        if constexpr (std::is_same<ARGS, GroupedArgs>::value) tiles_n = grouped_tiles(a.N, a.experts, bn);
+        else tiles_n = (a.N + bn - 1) / bn;
+        kernel<<<(unsigned)(tiles_m * tiles_n), 256, 0, st>>>(a, (int)tiles_m, (int)tiles_n);
+        return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
+    };
+    if (((a.M + 63) / 64) * ((a.N + 63) / 64) <= 256) return run(k_spmm_staged<DT, 0, 2, 2, 1, 1, ARGS>, 64, 64);
+    if (a.M <= 64 || ((a.M + 127) / 128) * ((a.N + 127) / 128) < 256) return run(k_spmm_staged<DT, 0, 2, 2, 1, 2, ARGS>, 64, 128);
+    return run(k_spmm_staged<DT, 0, 2, 2, 2, 2, ARGS>, 128, 128);
 }
 
 } // namespace sp24

@@ -124,27 +124,31 @@ struct staged_b<DT, 2, BN> : nmajor_pieces<BN, is8<DT> ? 1 : 2, is8<DT> ? 128 : 
 // every LDS access of this wavefront is done, then the workgroup's barrier; loads stay in flight
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-template <int DT, int BSRC, int WM, int WN, int TM, int TN>
-__global__ __launch_bounds__(256, 2) void k_spmm_staged(MmArgs a, int tiles_m, int tiles_n)
+template <int DT, int BSRC, int WM, int WN, int TM, int TN, class ARGS = MmArgs>
+__global__ __launch_bounds__(256, 2) void k_spmm_staged(ARGS a, int tiles_m, int tiles_n)
 {
     static_assert(WM * WN == 4, "four wavefronts");
     constexpr int T64 = is8<DT> ? 2 : 1;                      // 64-column tiles of A per step
     constexpr int BN = 32 * TN * WN;
     constexpr int kImage = BN * kRowBytes;
     constexpr int kOutWide = DT == SP24_I8 ? SP24_I32 : SP24_F32;
-    constexpr int kEpi = 4 * epilogue_geometry<kOutWide, TN>::kWaveBytes;
+    constexpr int BM = 32 * TM * WM, kEpi = 4 * store_bytes<ARGS, kOutWide, TM, TN>();
     constexpr int kLds = 2 * kImage > kEpi ? 2 * kImage : kEpi;
     using acc_t = typename acc_of<DT>::type;
     using b_t = staged_b<DT, BSRC, BN>;
     using a_t = compressed_rows<DT, TM>;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[kLds];
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[kLds + vector_bytes<ARGS, DT, BM>()];
 
     int tm, tn;
     tile_of_workgroup(tiles_m, tiles_n, tm, tn);
+    if constexpr (!is_plain<ARGS>) {
+        if (!a.template enter<BM, BN>(tm, tn)) return;
+    }
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave % WN;
     const int r = lane & 31, q = lane >> 5;
+    if constexpr (ARGS::kOwnStore) a.template fetch_vectors<DT, BM, 4>(lds + kLds, (int64_t)tm * BM, wave, lane);
     const int nsteps = (int)((a.K + 64 * T64 - 1) / (64 * T64));
 
     b_t b;
@@ -249,12 +253,19 @@ __global__ __launch_bounds__(256, 2) void k_spmm_staged(MmArgs a, int tiles_m, i
     }
 
     const int64_t row_base = ((int64_t)tm * WM + wm) * TM * 32, col_base = (int64_t)tn * BN + wn * TN * 32;
+    if constexpr (ARGS::kOwnStore) {
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));            // the vectors, which the compiler does not know of
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        a.template store_wave<DT, TM, TN>(acc, lds + wave * store_bytes<ARGS, kOutWide, TM, TN>(), lds + kLds, BM, wm * TM * 32, row_base, col_base, lane);
+    }
     auto put = [&](auto out_c) {
         constexpr int OUT = decltype(out_c)::value;
         store_wave_tile<DT, OUT, TM, TN>(a, acc, lds + wave * epilogue_geometry<OUT, TN>::kWaveBytes, row_base, col_base, lane);
     };
     using std::integral_constant;
-    if constexpr (DT == SP24_I8) {
+    if constexpr (ARGS::kOwnStore) return;
+    else if constexpr (DT == SP24_I8) {
         if (a.out == SP24_I32) put(integral_constant<int, SP24_I32>{});
         else if (a.out == SP24_I8) put(integral_constant<int, SP24_I8>{});
         else if (a.out == SP24_F32) put(integral_constant<int, SP24_F32>{});

@@ -87,37 +87,42 @@ __global__ __launch_bounds__(MOST) void k_norm_rows(RowsArgs a)
                 for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(h[c][i], h[c][i], sum);
             }
         }
+        float rstd = 1.0f;
         if constexpr (NORM) {
             const float square = __uint_as_float(over_workgroup<add_f>(__float_as_uint(sum), cells[parity]));
             parity ^= 1;
-            const float rstd = 1.0f / __builtin_sqrtf(square / (float)H + a.eps);
+            rstd = 1.0f / __builtin_sqrtf(square / (float)H + a.eps);
             if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
 #pragma unroll
             for (int c = 0; c < C; ++c)
                 if (n[c] > 0) {
                     if (!KEEP) load_floats8<WHOLE>(a.weight, (c * blockDim.x + threadIdx.x) * 8, n[c], w[0]);
+                    const float common = is8<OUT> ? 1.0f : rstd;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) h[c][i] = h[c][i] * rstd * w[KEEP ? c : 0][i];
+                    for (int i = 0; i < 8; ++i) h[c][i] = h[c][i] * common * w[KEEP ? c : 0][i];
                 }
         }
         if constexpr (is8<OUT>) {
-            // magnitudes through their bit patterns, in which a NaN is the largest: it reaches the scale, and no row hides one.
+            // Codes are a row's values over their largest, in which rstd cancels: two roundings less on the way to each.
+            // Magnitudes go by their bit patterns, in which a NaN is the largest: it reaches the scale, and no row hides one.
             // (Values past the row's end are zeros.)
             uint32_t most = 0;
 #pragma unroll
             for (int c = 0; c < C; ++c)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) most = max(most, (WHOLE ? n[c] > 0 : i < n[c]) ? __float_as_uint(h[c][i]) & 0x7FFFFFFFu : 0u);
-            float top = __uint_as_float(over_workgroup<max_u>(most, cells[2]));
+            const float largest = __uint_as_float(over_workgroup<max_u>(most, cells[2])), top = largest * rstd;
             if (!NORM) __syncthreads();                          // (the norm's sum has a barrier between two uses of the cells)
-            top = top < kLeastMagnitude ? kLeastMagnitude : top;
-            if (threadIdx.x == 0) a.scale[row] = top / top_code<OUT>();
-            const float inv = top_code<OUT>() / top;
+            if (threadIdx.x == 0) a.scale[row] = (top < kLeastMagnitude ? kLeastMagnitude : top) / top_code<OUT>();
+            // (a row so small that its reciprocal overflows, whatever rstd brings it to, goes the long way)
+            const bool tiny = largest < kLeastMagnitude;
+            const float first = tiny ? rstd : 1.0f, to_codes = top_code<OUT>() / (top < kLeastMagnitude ? kLeastMagnitude : tiny ? top : largest);
+            const float inv = top < kLeastMagnitude && !tiny ? rstd * to_codes : to_codes;
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 if (n[c] <= 0) continue;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) h[c][i] *= inv;
+                for (int i = 0; i < 8; ++i) h[c][i] = h[c][i] * first * inv;
                 store_codes8<OUT, WHOLE>(a.Y, row * a.ldy + (c * blockDim.x + threadIdx.x) * 8, n[c], h[c]);
             }
         } else {

@@ -70,6 +70,8 @@ CASES = [
     (37, 5, 64, "canonical", 0, 0), (1, 1, 32, "canonical", 0, 0), (45, 64, 352, "canonical", 0, 0),     # rows that no tile divides
     (64, 7, 128, "tiled", 5, 3), (33, 70, 96, "canonical", 1, 1), (100, 40, 160, "canonical", 16, 1),    # rows of X at any address
     (256, 17, 2048, "tiled", 0, 0), (512, 100, 1024, "tiled", 16, 0), (8, 300, 64, "canonical", 0, 0),
+    (100, 20, 48, "canonical", 0, 0), (700, 333, 1072, "canonical", 0, 0), (2100, 3000, 144, "canonical", 0, 0), (1030, 90, 400, "canonical", 3, 1),   # X through registers
+    (5000, 1100, 176, "canonical", 0, 0), (60, 5000, 80, "canonical", 0, 0), (4128, 1040, 320, "tiled", 1, 1),
     (2560, 300, 256, "tiled", 0, 0), (3000, 130, 192, "canonical", 0, 0), (4096, 70, 128, "tiled", 0, 0),      # tiles of 64 to 128
     (4100, 1030, 128, "canonical", 0, 0), (4096, 2100, 320, "tiled", 0, 0), (8224, 1100, 64, "tiled", 0, 0), (11072, 20, 128, "tiled", 0, 0),
 ]
@@ -79,6 +81,7 @@ CASES = [
 @pytest.mark.parametrize("case", range(len(CASES)))
 def test_linear(case, dtype):
     M, N, K, layout, pitch, offset = CASES[case]
+    K = -(-K // 32) * 32 if dtype in (I8, F8) else K
     g = torch.Generator().manual_seed(case)
     V, meta, W = weights(g, M, K, dtype, layout)
     x, keep = strided(values(g, (N, K), dtype), pitch, offset)
@@ -237,7 +240,7 @@ GROUPS = [
     # lengths in sixteens, rows behind the last, M, K, layout
     ([1], 0, 32, 64, "tiled"), ([1, 0, 2, 1], 1, 64, 128, "tiled"), ([0, 0, 0], 2, 64, 64, "tiled"), ([3, 5, 0, 9], 0, 100, 96, "canonical"),
     ([1] * 70, 3, 32, 64, "tiled"), ([0] * 40 + [4] + [0] * 90 + [1, 7], 0, 96, 192, "canonical"), ([20, 33, 7], 2, 512, 256, "tiled"),
-    ([70, 1, 130], 1, 1024, 128, "tiled"), ([2, 1, 0, 3, 1, 1, 2, 1], 4, 2048, 512, "tiled"), ([40] * 8, 0, 256, 64, "canonical"), ([64, 60], 0, 4096, 128, "tiled"),
+    ([70, 1, 130], 1, 1024, 128, "tiled"), ([3, 0, 40, 9], 2, 70, 80, "canonical"), ([20, 50, 1, 100], 1, 1030, 144, "canonical"), ([1, 2], 1, 33, 16, "canonical"), ([2, 1, 0, 3, 1, 1, 2, 1], 4, 2048, 512, "tiled"), ([40] * 8, 0, 256, 64, "canonical"), ([64, 60], 0, 4096, 128, "tiled"),
 ]
 
 
@@ -245,6 +248,7 @@ GROUPS = [
 @pytest.mark.parametrize("case", range(len(GROUPS)))
 def test_experts_rows(case, dtype):
     lengths, extra, M, K, layout = GROUPS[case]
+    K = -(-K // 32) * 32 if dtype in (I8, F8) else K
     g = torch.Generator().manual_seed(case)
     offsets, o, R = segments(lengths, extra)
     E = len(lengths)

@@ -99,6 +99,22 @@ def test_rows_that_are_zero_tiny_or_not_numbers():
     assert bool((y[0] == 0).all()) and bool(torch.isnan(y[2]).all()) and bool(torch.isfinite(y[4:]).all())
 
 
+@pytest.mark.parametrize("size,eps", [(2.0 ** -120, 1e-36), (2.0 ** -110, 1e-30), (2.0 ** -90, 1e30), (2.0 ** -60, 1e-6), (2.0 ** 60, 1e-6)])
+def test_small_and_large_rows_of_8_bits(size, eps):
+    """Rows far from 1 and what eps makes of them; their squares may be nothing in binary32, as eps alone then says."""
+    x = (torch.tensor([[1.0, -0.5, 0.25, 0.0, 0.75, -1.0, 0.125, 0.5]]) * size).cuda()
+    w = torch.ones(8, device="cuda")
+    y = sp24.sp24_rmsnorm(x, w, eps, out_dtype=F32).y
+    for out in (I8, F8):
+        n = sp24.sp24_rmsnorm(x, w, eps, out_dtype=out)
+        want = ref.d(y)
+        top = max(float(want.abs().max()), 2.0 ** -100)
+        assert float(n.scale[0]) == pytest.approx(top / ref.TOP[out], rel=1e-6)
+        exact = want / (top / ref.TOP[out])
+        room = 0.5 if out == I8 else torch.maximum(exact.abs() * 2.0 ** -4, torch.tensor(2.0 ** -10))
+        assert bool(((ref.d(n.y) - exact).abs() <= room + 1e-4).all()), (size, eps, n.y)
+
+
 @pytest.mark.parametrize("dtype", [F16, BF16, F32])
 def test_norm_in_place_on_the_residual(dtype):
     g = torch.Generator().manual_seed(5)
