@@ -268,7 +268,8 @@ __device__ __forceinline__ void count_up(F&& f)
 
 // A wavefront's tile on its way out, 32 tokens at a time: the sums go to LDS in binary32 as rows of 32 TM features and come back eight
 // neighbouring ones to a lane, so that every global access is 16 bytes and covers whole lines of a token's row.  Rows are 16 bytes
-// longer than their values: 16 lanes that write 16 bytes of 16 rows, or read 16 of 2 rows, meet every bank once.
+// longer than their values: 16 lanes that write 16 bytes of 16 rows, or read 16 of 2 rows, meet every bank once.  4096 x 8192 x 1024
+// bf16 with bias: 46.7 us without an activation, 54 to 56 with GELU.
 template <int TM> constexpr int LinearArgs::wave_bytes() { return 32 * (TM * 128 + 16); }
 
 template <int DT, int TM, int TN>

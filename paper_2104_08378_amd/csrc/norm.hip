@@ -5,7 +5,9 @@
 //   g = w dy,  dx = rstd (g - h rstd^2 mean(g h)) + dh,  dw = sum over the rows of dy h rstd
 //
 // Bound by memory: a row is read once, stays in registers (eight values a lane and chunk, in binary32 as all sums are) and is written
-// once.  A workgroup takes a row after the other and keeps its weights.
+// once.  A workgroup takes a row after the other and keeps its weights.  8192 x 4096 bf16 with residual to 8-bit floats: 49 us, 235 MB at 4.8 TB/s
+// (a large copy reaches 5.4); to bf16 54 (5.0); 4000 rows of 4095, at odd addresses, 44 (3.0); 16 rows of 8192 3.5 us, little but the launch.
+// Gradients with the column sums: 4096 x 1024 11.7 us, 16000 x 1024 30 (4.4 TB/s).
 #include <algorithm>
 
 #include "launch.hpp"
