@@ -17,7 +17,7 @@ namespace sp24 {
 
 // the value that 8-bit codes reach at the largest magnitude of their row
 template <int OUT> constexpr float top_code() { return OUT == SP24_I8 ? 127.0f : 448.0f; }
-constexpr float kLeastMagnitude = 7.888609052210118e-31f;       // 2^-100: below it a row's codes are taken against it (and are zeros)
+constexpr float kLeastMagnitude = 7.888609052210118e-31f;       // 2^-100: a row below it has its codes taken against it
 
 template <int OUT, bool WHOLE>
 __device__ __forceinline__ void store_codes8(void* p, int64_t first, int n, const float (&v)[8])
@@ -89,23 +89,28 @@ __global__ __launch_bounds__(MOST) void k_norm_rows(RowsArgs a)
                 for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(h[c][i], h[c][i], sum);
             }
         }
-        float rstd = 1.0f;
+        float rstd = 1.0f, power = 1.0f, rest = 1.0f;            // rstd = power * rest, a power of two and a factor of 1 to 2
         if constexpr (NORM) {
             const float square = __uint_as_float(over_workgroup<add_f>(__float_as_uint(sum), cells[parity]));
             parity ^= 1;
             rstd = 1.0f / __builtin_sqrtf(square / (float)H + a.eps);
             if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
+            if constexpr (is8<OUT>) {
+                power = __uint_as_float(__float_as_uint(rstd) & 0x7F800000u);
+                rest = __uint_as_float((__float_as_uint(rstd) & 0x007FFFFFu) | 0x3F800000u);
+            }
 #pragma unroll
             for (int c = 0; c < C; ++c)
                 if (n[c] > 0) {
                     if (!KEEP) load_floats8<WHOLE>(a.weight, (c * blockDim.x + threadIdx.x) * 8, n[c], w[0]);
-                    const float common = is8<OUT> ? 1.0f : rstd;
+                    const float common = is8<OUT> ? power : rstd;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) h[c][i] = h[c][i] * common * w[KEEP ? c : 0][i];
                 }
         }
         if constexpr (is8<OUT>) {
-            // Codes are a row's values over their largest, in which rstd cancels: two roundings less on the way to each.
+            // Codes are a row's values over their largest, in which rstd cancels: two roundings less on the way to each.  Its power of two
+            // rounds nothing and stays, so that h w passes no end of binary32 that y itself keeps within.
             // Magnitudes go by their bit patterns, in which a NaN is the largest: it reaches the scale, and no row hides one.
             // (Values past the row's end are zeros.)
             uint32_t most = 0;
@@ -113,18 +118,15 @@ __global__ __launch_bounds__(MOST) void k_norm_rows(RowsArgs a)
             for (int c = 0; c < C; ++c)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) most = max(most, (WHOLE ? n[c] > 0 : i < n[c]) ? __float_as_uint(h[c][i]) & 0x7FFFFFFFu : 0u);
-            const float largest = __uint_as_float(over_workgroup<max_u>(most, cells[2])), top = largest * rstd;
+            const float largest = __uint_as_float(over_workgroup<max_u>(most, cells[2])), top = largest * rest;
             if (!NORM) __syncthreads();                          // (the norm's sum has a barrier between two uses of the cells)
             if (threadIdx.x == 0) a.scale[row] = (top < kLeastMagnitude ? kLeastMagnitude : top) / top_code<OUT>();
-            // (a row so small that its reciprocal overflows, whatever rstd brings it to, goes the long way)
-            const bool tiny = largest < kLeastMagnitude;
-            const float first = tiny ? rstd : 1.0f, to_codes = top_code<OUT>() / (top < kLeastMagnitude ? kLeastMagnitude : tiny ? top : largest);
-            const float inv = top < kLeastMagnitude && !tiny ? rstd * to_codes : to_codes;
+            const float inv = top < kLeastMagnitude ? rest * (top_code<OUT>() / kLeastMagnitude) : top_code<OUT>() / largest;
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 if (n[c] <= 0) continue;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) h[c][i] = h[c][i] * first * inv;
+                for (int i = 0; i < 8; ++i) h[c][i] *= inv;
                 store_codes8<OUT, WHOLE>(a.Y, row * a.ldy + (c * blockDim.x + threadIdx.x) * 8, n[c], h[c]);
             }
         } else {
