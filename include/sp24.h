@@ -46,7 +46,7 @@
  *     additions, unless a function's comment says more.
  *   - K must be a multiple of 16 for 16-bit types and of 32 for the 8-bit types
  *     (the dimension rule of Sec. 3.2 / Sec. 4.2, applied to the inner
- *     dimension), else SP24_ERR_SHAPE.  M and N may be any positive value; a
+ *     dimension; sp24_gemm_dense names an exception), else SP24_ERR_SHAPE.  M and N may be any positive value; a
  *     zero M or N is accepted and does nothing.
  *   - Selection rule where the paper is silent: magnitudes are compared
  *     exactly; on equal magnitude the lower column is kept; every NaN counts
@@ -302,6 +302,9 @@ sp24_status sp24_spmm(const void* V, const void* meta, const void* B, void* D, i
  * The same-shape dense product D = A x B on the dense matrix cores, with the
  * same types, accumulation and layouts as sp24_spmm: the denominator of the
  * sparse-vs-dense speedup (Sec. 3.2, Fig. 3).  A: device, M x K, row stride lda.
+ * 16-bit types with an N-major B (the gradient of a layer's weights, whose K is a number of tokens) take any K, 0 included, which
+ * gives zeros.  What lies between K and the next 16-byte boundary of a row of A may be read (it shares 16 bytes with the row's last
+ * elements) and is not used.
  */
 sp24_status sp24_gemm_dense(const void* A, const void* B, void* D, int64_t M, int64_t N, int64_t K,
                             int64_t lda, int64_t ldb, int64_t ldd, sp24_dtype in, sp24_dtype out,
@@ -512,7 +515,7 @@ sp24_status sp24_linear(const void* V, const void* meta, const void* X, void* Y,
  * What follows from the gradient of a layer's result:  dZ = dY * act'(Z),  dbias[m] = sum_n dZ[n][m].
  * dY, Z, dZ: N x M of type t (SP24_F16 or SP24_BF16); Z may be NULL for SP24_ACT_NONE.  dZ (may be NULL) may be dY or Z in place.
  * dZt (may be NULL): M x N, dZ transposed, the first operand of the weights' gradient: dW = sp24_gemm_dense(dZt, X as an N-major
- * operand) and sp24_mask_apply; dX = sp24_linear of dZ with the compressed transpose of W.  dbias (may be NULL): M floats.
+ * operand, K = N) and sp24_mask_apply, for which its rows must be 16-byte aligned: lddzt a multiple of 8, whatever N is; dX = sp24_linear of dZ with the compressed transpose of W.  dbias (may be NULL): M floats.
  * With offsets (below; N a multiple of 16) dbias holds M floats for each of the experts, summed over its segment alone.
  * workspace (dbias given): device, 16-byte aligned, sp24_linear_backward_workspace_bytes(M, N, offsets != NULL) bytes.
  */

@@ -234,13 +234,15 @@ sp24_status sp24_permute_search_workspace(const void* A, int32_t* perm, int64_t 
 }
 
 // Argument checks of every product entry point.  *empty: nothing to compute (M or N is 0).
-// x_bytes: extent of the NHWC input when a.conv.on (a.B then points at it), else unused
-static sp24_status mm_validate(const MmArgs& a, size_t x_bytes, bool* empty)
+// x_bytes: extent of the NHWC input when a.conv.on (a.B then points at it), else unused.  any_k: K of any length where the product is one
+// that adds up over tokens (dense, 16-bit, B N-major)
+static sp24_status mm_validate(const MmArgs& a, size_t x_bytes, bool any_k, bool* empty)
 {
     *empty = false;
     if (!is_input_type(a.in) || !out_legal(a.in, a.out, a.epi.on != 0)) return SP24_ERR_DTYPE;
     if (a.bo != SP24_B_KMAJOR && a.bo != SP24_B_NMAJOR) return SP24_ERR_LAYOUT;
-    if (a.M < 0 || a.N < 0 || !k_legal(a.K, a.in)) return SP24_ERR_SHAPE;
+    const bool over_tokens = any_k && !a.sparse && !a.conv.on && a.bo == SP24_B_NMAJOR && esize_of(a.in) == 2;
+    if (a.M < 0 || a.N < 0 || !(over_tokens ? a.K >= 0 : k_legal(a.K, a.in))) return SP24_ERR_SHAPE;
     if (a.sparse) {
         if (!is_layout(a.layout)) return SP24_ERR_LAYOUT;
         if (!layout_fits(a.M, a.K, a.layout)) return SP24_ERR_LAYOUT;
@@ -258,7 +260,7 @@ static sp24_status mm_validate(const MmArgs& a, size_t x_bytes, bool* empty)
     if (a.sparse) {
         if (!a.A || !a.meta) return SP24_ERR_NULL;
         if (!aligned16(a.A) || !aligned16(a.meta)) return SP24_ERR_ALIGN;
-    } else {
+    } else if (a.K > 0) {
         s = check_matrix(a.A, a.M, a.K, a.lda, es);
         if (s != SP24_OK) return s;
     }
@@ -271,6 +273,7 @@ static sp24_status mm_validate(const MmArgs& a, size_t x_bytes, bool* empty)
     }
     s = check_matrix(a.D, a.M, a.N, a.ldd, os, false);
     if (s != SP24_OK) return s;
+    if (a.K == 0) return SP24_OK;                          // (no operands to overlap)
     size_t nd = ((size_t)(a.M - 1) * a.ldd + a.N) * os;
     size_t nb = a.conv.on ? x_bytes
                           : (a.bo == SP24_B_KMAJOR) ? ((size_t)(a.N - 1) * a.ldb + a.K) * es : ((size_t)(a.K - 1) * a.ldb + a.N) * es;
@@ -398,10 +401,10 @@ static sp24_status mm_dispatch(const MmArgs& a, hipStream_t st)
     return launch_mm_simple(a, st);
 }
 
-static sp24_status mm_common(const MmArgs& a, hipStream_t st, size_t x_bytes = 0)
+static sp24_status mm_common(const MmArgs& a, hipStream_t st, size_t x_bytes = 0, bool any_k = false)
 {
     bool empty;
-    const sp24_status s = mm_validate(a, x_bytes, &empty);
+    const sp24_status s = mm_validate(a, x_bytes, any_k, &empty);
     if (s != SP24_OK || empty) return s;
     return mm_dispatch(a, st);
 }
@@ -493,7 +496,7 @@ static sp24_status static_scratch(void** out)
 static sp24_status mm_splitk(const MmArgs& a, void* workspace, size_t workspace_bytes, hipStream_t st, bool use_static = false)
 {
     bool empty;
-    sp24_status s = mm_validate(a, 0, &empty);
+    sp24_status s = mm_validate(a, 0, false, &empty);
     if (s != SP24_OK || empty) return s;
     const SplitPlan plan = split_plan(a.M, a.N, a.K, a.in);
     if (plan.slices <= 1) return mm_dispatch(a, st);
@@ -623,7 +626,7 @@ sp24_status sp24_gemm_dense(const void* A, const void* B, void* D, int64_t M, in
                             int64_t ldd, sp24_dtype in, sp24_dtype out, sp24_border bo, void* stream)
 {
     MmArgs a{A, nullptr, B, D, M, N, K, lda, ldb, ldd, in, out, bo, SP24_LAYOUT_CANONICAL, false};
-    return mm_common(a, static_cast<hipStream_t>(stream));
+    return mm_common(a, static_cast<hipStream_t>(stream), 0, true);
 }
 
 sp24_status sp24_spmm_i8_scaled(const void* V, const void* meta, const void* B, void* D, int64_t M, int64_t N, int64_t K,

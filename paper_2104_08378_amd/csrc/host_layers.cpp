@@ -284,14 +284,16 @@ PyObject* linear_backward(PyObject* self, PyObject* const* args, Py_ssize_t)
     const sp24_dtype t = type_of(type, c.ok);
     Scratch ws(c, 4, sp24_linear_backward_workspace_bytes(M, N, grouped), *dY);
     if (!c.ok) return not_handled();
-    at::Tensor dZ, dZt = make({M, N}, type, *dY), db = grouped ? make({experts, M}, at::kFloat, *dY) : make({M}, at::kFloat, *dY);
+    const int64_t pitch = (N + 7) / 8 * 8;                     // 16-byte rows, which the weights' gradient asks for
+    at::Tensor dZ, dZt = make({M, pitch}, type, *dY), db = grouped ? make({experts, M}, at::kFloat, *dY) : make({M}, at::kFloat, *dY);
+    if (pitch != N) dZt = dZt.narrow(1, 0, N);
     if (copy) dZ = make({N, M}, type, *dY);
     const void* pd = dY->data_ptr();
     void *pz = copy ? dZ.data_ptr() : nullptr, *pt = dZt.data_ptr(), *st = stream();
     float* pb = static_cast<float*>(db.data_ptr());
     const int64_t lddy = ld(*dY);
     const sp24_status s = without_gil([&] {
-        return sp24_linear_backward(pd, copy ? z.p : nullptr, pz, pt, pb, M, N, lddy, z.ld_, M, N, act, po, (int)experts, t, ws.p, ws.bytes, st);
+        return sp24_linear_backward(pd, copy ? z.p : nullptr, pz, pt, pb, M, N, lddy, z.ld_, M, pitch, act, po, (int)experts, t, ws.p, ws.bytes, st);
     });
     if (s != SP24_OK) return refused(self, s, "sp24_linear_backward");
     return tuple(copy ? wrap(dZ) : again(args[0]), wrap(dZt), wrap(db));

@@ -45,8 +45,7 @@ struct dense_rows {
         for (int i = 0; i < TM; ++i)
             src[i] = reinterpret_cast<const uint8_t*>(a.A) + min((block0 + i) * 32 + (lane & 31), a.M - 1) * a.lda * ES + 16 * q;
     }
-    __device__ __forceinline__ void load_whole(int64_t kb, int4v (&v)[TM][NA], uint32_t (&code)[TM]) const { load_edge(kb, v, code); }
-    __device__ __forceinline__ void load_edge(int64_t kb, int4v (&v)[TM][NA], uint32_t (&code)[TM]) const
+    __device__ __forceinline__ void load_whole(int64_t kb, int4v (&v)[TM][NA], uint32_t (&code)[TM]) const
     {
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
@@ -56,6 +55,24 @@ struct dense_rows {
                 v[i][s] = __builtin_bit_cast(int4v, load16_aligned(at + 16 * q < row_bytes ? src[i] + at : k_zero_row));
             }
             code[i] = 0;
+        }
+    }
+    // (16-bit types: K may end inside a piece, and what lies there behind K is not the matrix's: a NaN would outlast B's zeros)
+    __device__ __forceinline__ void load_edge(int64_t kb, int4v (&v)[TM][NA], uint32_t (&code)[TM]) const
+    {
+        load_whole(kb, v, code);
+        if constexpr (!is8<DT>) {
+#pragma unroll
+            for (int s = 0; s < NA; ++s) {
+                const int64_t left = row_bytes - (kb * (64 * ES) + 32 * s + 16 * q);
+                if (left <= 0 || left >= 16) continue;
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                    const uint32_t keep = 4 * d + 4 <= left ? ~0u : 4 * d + 2 <= left ? 0xFFFFu : 0u;
+#pragma unroll
+                    for (int i = 0; i < TM; ++i) v[i][s][d] &= (int)keep;
+                }
+            }
         }
     }
 };
@@ -210,6 +227,7 @@ sp24_status launch_mm_ksplit(const MmArgs& a, hipStream_t st, bool* handled)
 {
     *handled = false;
     if (a.conv.on || a.bo != SP24_B_NMAJOR || a.k_slices > 1 || a.K > ((int64_t)1 << 30)) return SP24_OK;
+    if (a.K < 16) return SP24_OK;                           // (of a dense product; its B may end before the 16 bytes of a piece)
     if (a.M > ((int64_t)1 << 30) || a.N > ((int64_t)1 << 30) || ((a.M + 31) / 32) * ((a.N + 63) / 64) >= ((int64_t)1 << 30)) return SP24_OK;
     *handled = true;
     if (a.in == SP24_I8) return run_ksplit<SP24_I8>(a, st);

@@ -32,8 +32,8 @@ sp24_status launch_mm_tiled(const MmArgs& a, hipStream_t st, bool* handled)
               (a.ldb * es) % 16 == 0 && a.N >= 1 && a.M >= 1 && a.M <= ((int64_t)1 << 30) && a.N <= ((int64_t)1 << 30) &&
               a.ldb * es < ((int64_t)1 << 22) && ((a.M + 127) / 128) * ((a.N + 127) / 128) < ((int64_t)1 << 30);
     if (!a.conv.on && a.bo == SP24_B_NMAJOR) {
-        // N-major B: whole 16-byte chunks of columns, rows 16-byte aligned, 32-bit row offsets within a step
-        ok = (a.K * es) % 32 == 0 && (reinterpret_cast<uintptr_t>(a.B) & 15u) == 0 && (a.ldb * es) % 16 == 0 &&
+        // N-major B: whole 16-byte chunks of columns, rows 16-byte aligned, 32-bit row offsets within a step; a dense product's K of any length
+        ok = (!a.sparse || (a.K * es) % 32 == 0) && (reinterpret_cast<uintptr_t>(a.B) & 15u) == 0 && (a.ldb * es) % 16 == 0 &&
              (a.N * es) % 16 == 0 && a.N >= 1 && a.M >= 1 && a.M <= ((int64_t)1 << 30) && a.N <= ((int64_t)1 << 30) &&
              a.ldb * es < ((int64_t)1 << 22) && ((a.M + 127) / 128) * ((a.N + 127) / 128) < ((int64_t)1 << 30);
     }

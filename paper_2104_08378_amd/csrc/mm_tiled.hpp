@@ -1047,6 +1047,16 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_gemm_pipe(ARGS a, int tiles
         __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
+        if constexpr (NMAJ && !is8<DT>) {
+            // K ends inside a 16-byte piece of A's rows: what lies there behind K is not the matrix's, and a NaN would outlast B's zeros
+            if (tail % 16 != 0) {
+                for (int row = tid; row < BM; row += 64 * NW) {
+                    uint16_t* const piece = reinterpret_cast<uint16_t*>(lds_all + row * kRowBytes + (((tail >> 4) ^ ((row >> 1) & 7)) << 4));
+                    for (int i = tail % 16 / 2; i < 8; ++i) piece[i] = 0;
+                }
+                __syncthreads();
+            }
+        }
         compute(0);
         __builtin_amdgcn_s_barrier();                // every wavefront has read stage 0 before it becomes store scratch
         __builtin_amdgcn_sched_barrier(0);

@@ -420,7 +420,7 @@ def sp24_spmm(V, meta, B, out_dtype, b_order="k", layout="canonical", out=None):
 
 
 def sp24_gemm_dense(A, B, out_dtype, b_order="k", out=None):
-    """D [M, N] = A @ B on the dense matrix cores (speedup denominator)."""
+    """D [M, N] = A @ B on the dense matrix cores (speedup denominator).  K of any length for 16-bit types and b_order "n"."""
     done = (_host or _load_host()).sp24_gemm_dense(A, B, out_dtype, b_order, out)
     if done is not None:
         return done
@@ -761,7 +761,8 @@ def sp24_linear(V, meta, X, out_dtype, w_scale=None, x_scale=None, bias=None, ac
 def sp24_linear_backward(dY, preact, act, offsets=None, workspace=None):
     """(dZ [N, M], its transpose [M, N], dbias) of a layer's result: dZ = dY * act'(preact), which is dY itself without an activation; dbias
     [M] in float32, with ``offsets`` (of sp24_moe_sort) [experts, M].  Input's gradient: sp24_linear of dZ with the compressed transposed
-    weights; weights' gradient: sp24_gemm_dense(transpose, X, ..., b_order="n"), masked."""
+    weights; weights' gradient: sp24_gemm_dense(transpose, X, ..., b_order="n"), masked.  (The rows of the transpose are 16-byte aligned,
+    as that product asks for: a view of a wider tensor where N is no multiple of 8.)"""
     done = (_host or _load_host()).sp24_linear_backward(dY, preact, act, offsets, workspace)
     if done is not None:
         return done
@@ -771,10 +772,11 @@ def sp24_linear_backward(dY, preact, act, offsets=None, workspace=None):
     z, ldz = (None, 0) if code == NO_ACT else _matrix_like(preact, (N, M), dY.dtype, "preact")
     experts = 0 if offsets is None else offsets.numel() - 1
     dZ = torch.empty((N, M), dtype=dY.dtype, device=dY.device) if code != NO_ACT else None
-    dZt = torch.empty((M, N), dtype=dY.dtype, device=dY.device)
+    pitch = -(-N // 8) * 8
+    dZt = torch.empty((M, pitch), dtype=dY.dtype, device=dY.device)[:, :N]
     dbias = torch.empty((M,) if offsets is None else (experts, M), dtype=torch.float32, device=dY.device)
     ws, ws_bytes = _scratch(workspace, lib().sp24_linear_backward_workspace_bytes(M, N, int(offsets is not None)), dY.device)
-    _check(lib().sp24_linear_backward(dY.data_ptr(), z, _ptr(dZ), dZt.data_ptr(), dbias.data_ptr(), M, N, _ld(dY), ldz, M, N, code,
+    _check(lib().sp24_linear_backward(dY.data_ptr(), z, _ptr(dZ), dZt.data_ptr(), dbias.data_ptr(), M, N, _ld(dY), ldz, M, pitch, code,
                                       _vector(offsets, experts + 1, "offsets", torch.int32), experts, _DT[dY.dtype], _ptr(ws), ws_bytes, _stream()),
            "sp24_linear_backward")
     return dY if dZ is None else dZ, dZt, dbias
