@@ -296,10 +296,11 @@ __device__ __forceinline__ void store_bytes(uint8_t* p, int64_t n, const uint4v&
         if (i < n) p[i] = (uint8_t)(v[i / 4] >> (8 * (i % 4)));
 }
 
-__global__ __launch_bounds__(256) void k_moe_gather(GatherArgs a, int blocks_a_row)
+__global__ __launch_bounds__(256) void k_moe_gather(GatherArgs a, int blocks_a_row, unsigned from)
 {
-    const int64_t row = blockIdx.x / blocks_a_row;
-    const int64_t at = ((int64_t)(blockIdx.x % blocks_a_row) * blockDim.x + threadIdx.x) * 16;
+    const unsigned group = from + blockIdx.x;
+    const int64_t row = group / blocks_a_row;
+    const int64_t at = ((int64_t)(group % blocks_a_row) * blockDim.x + threadIdx.x) * 16;
     const int64_t choice = a.rows[row], token = choice < 0 ? -1 : choice / a.topk;
     const bool live = token >= 0 && token < a.N;
     if (a.scale_out && at == 0) a.scale_out[row] = live ? a.scale[token] : 0.0f;
@@ -322,8 +323,7 @@ sp24_status launch_moe_gather(const GatherArgs& a, hipStream_t st)
     unsigned threads;
     int blocks;
     row_launch(a.row_bytes, 16, threads, blocks);
-    k_moe_gather<<<(unsigned)(a.R * blocks), threads, 0, st>>>(a, blocks);
-    return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
+    return launch_in_parts(a.R * blocks, threads, [&](unsigned from, unsigned grid) { k_moe_gather<<<grid, threads, 0, st>>>(a, blocks, from); });
 }
 
 // ---------------------------------------------------------------------------
@@ -331,10 +331,11 @@ sp24_status launch_moe_gather(const GatherArgs& a, hipStream_t st)
 // values a thread.  4096 tokens of 4096 bf16 from two experts each, with residual: 22.0 us, 134 MB at 6.1 TB/s.
 // ---------------------------------------------------------------------------
 template <int T>
-__global__ __launch_bounds__(256) void k_moe_combine(CombineArgs a, int blocks_a_row)
+__global__ __launch_bounds__(256) void k_moe_combine(CombineArgs a, int blocks_a_row, unsigned from)
 {
-    const int64_t n = blockIdx.x / blocks_a_row;
-    const int64_t at = ((int64_t)(blockIdx.x % blocks_a_row) * blockDim.x + threadIdx.x) * 8;
+    const unsigned group = from + blockIdx.x;
+    const int64_t n = group / blocks_a_row;
+    const int64_t at = ((int64_t)(group % blocks_a_row) * blockDim.x + threadIdx.x) * 8;
     if (at >= a.H) return;
     const int have = (int)min(a.H - at, (int64_t)8);
     float sum[8] = {};
@@ -373,11 +374,11 @@ sp24_status launch_moe_combine(const CombineArgs& a, hipStream_t st)
     unsigned threads;
     int blocks;
     row_launch(a.H, 8, threads, blocks);
-    const unsigned grid = (unsigned)(a.N * blocks);
-    if (a.t == SP24_F32) k_moe_combine<SP24_F32><<<grid, threads, 0, st>>>(a, blocks);
-    else if (a.t == SP24_F16) k_moe_combine<SP24_F16><<<grid, threads, 0, st>>>(a, blocks);
-    else k_moe_combine<SP24_BF16><<<grid, threads, 0, st>>>(a, blocks);
-    return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
+    return launch_in_parts(a.N * blocks, threads, [&](unsigned from, unsigned grid) {
+        if (a.t == SP24_F32) k_moe_combine<SP24_F32><<<grid, threads, 0, st>>>(a, blocks, from);
+        else if (a.t == SP24_F16) k_moe_combine<SP24_F16><<<grid, threads, 0, st>>>(a, blocks, from);
+        else k_moe_combine<SP24_BF16><<<grid, threads, 0, st>>>(a, blocks, from);
+    });
 }
 
 // ---------------------------------------------------------------------------
@@ -386,12 +387,12 @@ sp24_status launch_moe_combine(const CombineArgs& a, hipStream_t st)
 // 1024 bf16 on four experts each, one choice in 20 without a row: 17.6 us, 72 MB at 4.1 TB/s.
 // ---------------------------------------------------------------------------
 template <int T>
-__global__ __launch_bounds__(256) void k_moe_combine_grad(CombineGradArgs a)
+__global__ __launch_bounds__(256) void k_moe_combine_grad(CombineGradArgs a, unsigned from)
 {
     const int lane = threadIdx.x & 63;
-    for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < a.N * a.topk; t += (int64_t)gridDim.x * 256)
+    for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < a.N * a.topk; t += (int64_t)gridDim.x * 256)      // (in each part again)
         if (a.slots[t] < 0 || a.slots[t] >= a.R) a.dweights[t] = 0.0f;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t row = ((int64_t)from + blockIdx.x) * 4 + (threadIdx.x >> 6);
     if (row >= a.R) return;
     const int64_t choice = a.rows[row], token = choice < 0 ? -1 : choice / a.topk;
     const bool live = token >= 0 && token < a.N;
@@ -417,11 +418,12 @@ __global__ __launch_bounds__(256) void k_moe_combine_grad(CombineGradArgs a)
 
 sp24_status launch_moe_combine_grad(const CombineGradArgs& a, hipStream_t st)
 {
-    const unsigned grid = (unsigned)std::max<int64_t>((a.R + 3) / 4, 1);       // (choices without rows have gradients to write)
-    if (a.t == SP24_F32) k_moe_combine_grad<SP24_F32><<<grid, 256, 0, st>>>(a);
-    else if (a.t == SP24_F16) k_moe_combine_grad<SP24_F16><<<grid, 256, 0, st>>>(a);
-    else k_moe_combine_grad<SP24_BF16><<<grid, 256, 0, st>>>(a);
-    return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
+    const int64_t groups = std::max<int64_t>((a.R + 3) / 4, 1);                // (choices without rows have gradients to write)
+    return launch_in_parts(groups, 256, [&](unsigned from, unsigned grid) {
+        if (a.t == SP24_F32) k_moe_combine_grad<SP24_F32><<<grid, 256, 0, st>>>(a, from);
+        else if (a.t == SP24_F16) k_moe_combine_grad<SP24_F16><<<grid, 256, 0, st>>>(a, from);
+        else k_moe_combine_grad<SP24_BF16><<<grid, 256, 0, st>>>(a, from);
+    });
 }
 
 } // namespace sp24

@@ -2,6 +2,8 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "../../include/sp24.h"
 #include "common.hpp"
 
@@ -90,6 +92,18 @@ sp24_status launch_mm_tiled(const MmArgs& a, hipStream_t st, bool* handled);
 // each, images M * ldw values apart).
 sp24_status launch_splitk_reduce(const void* partial, int slices, int64_t M, int64_t N, int64_t ldw, void* D, int64_t ldd, bool integer,
                                  sp24_dtype out, hipStream_t st);
+
+// A launch has fewer than 2^32 threads along x (the runtime does not refuse more: it runs what the low 32 bits say).
+inline int64_t most_groups(int threads) { return (((int64_t)1 << 32) - 1) / threads; }
+// launch(first, grid) for as many launches as `groups` workgroups take, workgroup b of one being number first + b
+template <class F>
+sp24_status launch_in_parts(int64_t groups, int threads, F&& launch)
+{
+    if (groups == 0) return SP24_OK;
+    const int64_t most = most_groups(threads);
+    for (int64_t first = 0; first < groups; first += most) launch((unsigned)first, (unsigned)std::min(groups - first, most));
+    return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
+}
 
 // ---- the operators around the products (N rows of H values unless said otherwise; ld* in elements) ----
 struct RowsArgs {

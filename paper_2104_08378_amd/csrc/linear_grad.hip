@@ -13,13 +13,14 @@ namespace sp24 {
 constexpr int kGradTile = 64;           // rows of a tile
 
 template <int T, int WIDTH>
-__global__ __launch_bounds__(4 * WIDTH) void k_linear_grad(LinearGradArgs a, int tiles_m)
+__global__ __launch_bounds__(4 * WIDTH) void k_linear_grad(LinearGradArgs a, int tiles_m, unsigned from)
 {
     constexpr int kPitch = WIDTH + 1, CH = WIDTH / 8;
     __shared__ float tile[kGradTile * kPitch];
     __shared__ float part[4][WIDTH];
     const int tid = threadIdx.x;
-    const int64_t m0 = (int64_t)(blockIdx.x % tiles_m) * WIDTH, n0 = (int64_t)(blockIdx.x / tiles_m) * kGradTile;
+    const unsigned at = from + blockIdx.x;
+    const int64_t m0 = (int64_t)(at % tiles_m) * WIDTH, n0 = (int64_t)(at / tiles_m) * kGradTile;
     const int c = tid % CH;
     const int64_t m = m0 + c * 8;
     const int have = (int)min(a.M - m, (int64_t)8);
@@ -79,11 +80,10 @@ template <int WIDTH>
 static sp24_status run_linear_grad(const LinearGradArgs& a, hipStream_t st)
 {
     const int64_t tiles_m = (a.M + WIDTH - 1) / WIDTH, tiles_n = (a.N + kGradTile - 1) / kGradTile;
-    const unsigned grid = (unsigned)(tiles_m * tiles_n);
-    if (grid == 0) return SP24_OK;
-    if (a.t == SP24_F16) k_linear_grad<SP24_F16, WIDTH><<<grid, 4 * WIDTH, 0, st>>>(a, (int)tiles_m);
-    else k_linear_grad<SP24_BF16, WIDTH><<<grid, 4 * WIDTH, 0, st>>>(a, (int)tiles_m);
-    return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
+    return launch_in_parts(tiles_m * tiles_n, 4 * WIDTH, [&](unsigned from, unsigned grid) {
+        if (a.t == SP24_F16) k_linear_grad<SP24_F16, WIDTH><<<grid, 4 * WIDTH, 0, st>>>(a, (int)tiles_m, from);
+        else k_linear_grad<SP24_BF16, WIDTH><<<grid, 4 * WIDTH, 0, st>>>(a, (int)tiles_m, from);
+    });
 }
 
 sp24_status launch_linear_grad(const LinearGradArgs& a, hipStream_t st)

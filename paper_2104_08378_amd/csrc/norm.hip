@@ -296,11 +296,11 @@ __global__ __launch_bounds__(64 * kGradWaves) void k_norm_grad_short(NormGradArg
 // out[e][c] = the sum of rows first .. last - 1 of `partial` (columns wide), in a fixed order: 32 interleaved sums, then those.
 // Without offsets all rows; with them those of segment e, `unit` rows of the offsets to one of partial.
 __global__ __launch_bounds__(1024) void k_column_sums(const float* partial, int64_t rows, int64_t columns, const int32_t* offsets, int unit,
-                                                      float* out)
+                                                      float* out, unsigned from)
 {
     __shared__ float part[32][33];
     const int at = threadIdx.x & 31, stream = threadIdx.x >> 5;
-    const int64_t c = (int64_t)blockIdx.x * 32 + at;
+    const int64_t c = ((int64_t)from + blockIdx.x) * 32 + at;
     int64_t first = 0, last = rows;
     if (offsets) {
         first = min(max((int64_t)offsets[blockIdx.y] / unit, (int64_t)0), rows);
@@ -417,8 +417,9 @@ sp24_status launch_norm_grad(const NormGradArgs& a, hipStream_t st)
 sp24_status launch_column_sums(const float* partial, int64_t rows, int64_t columns, const int32_t* offsets, int segments, int unit, float* out,
                                hipStream_t st)
 {
-    k_column_sums<<<dim3((unsigned)((columns + 31) / 32), (unsigned)segments), 1024, 0, st>>>(partial, rows, columns, offsets, unit, out);
-    return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
+    return launch_in_parts((columns + 31) / 32, 1024, [&](unsigned from, unsigned grid) {
+        k_column_sums<<<dim3(grid, (unsigned)segments), 1024, 0, st>>>(partial, rows, columns, offsets, unit, out, from);
+    });
 }
 
 } // namespace sp24
