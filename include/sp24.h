@@ -504,7 +504,8 @@ typedef enum {
  * x_scale (N floats): 8-bit inputs only (else SP24_ERR_DTYPE); NULL means 1.  bias (M floats), residual (N x M of type out): NULL means none.
  * Z (NULL or N x M of type out) receives z, which sp24_linear_backward takes.  Y may be residual in place.
  * V, meta, layouts and K as for sp24_spmm; as there, a removed position takes no part in the sum whatever X holds.  Rows of X
- * that are not 16-byte aligned, and a K of no whole 32 columns, take a slower kernel.
+ * that are not 16-byte aligned, and a K of no whole 32 columns, take a slower kernel.  More tiles than a launch has workgroups
+ * (2^28 features, 2^29 tokens or 2^36 results at least) are SP24_ERR_SHAPE, here and in the experts' calls below.
  */
 sp24_status sp24_linear(const void* V, const void* meta, const void* X, void* Y, int64_t M, int64_t N, int64_t K, int64_t ldx,
                         int64_t ldy, const float* w_scale, const float* x_scale, const float* bias, sp24_act act,

@@ -95,6 +95,14 @@ sp24_status launch_splitk_reduce(const void* partial, int slices, int64_t M, int
 
 // A launch has fewer than 2^32 threads along x (the runtime does not refuse more: it runs what the low 32 bits say).
 inline int64_t most_groups(int threads) { return (((int64_t)1 << 32) - 1) / threads; }
+// `groups` workgroups for each of `images`, one to a tile that a kernel finds from its number: SP24_ERR_SHAPE, and no launch, where it holds fewer
+template <class F>
+sp24_status launch_tiles(int64_t groups, int images, int threads, F&& launch)
+{
+    if (groups > most_groups(threads)) return SP24_ERR_SHAPE;
+    launch(dim3((unsigned)groups, (unsigned)images), dim3((unsigned)threads));
+    return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
+}
 // launch(first, grid) for as many launches as `groups` workgroups take, workgroup b of one being number first + b
 template <class F>
 sp24_status launch_in_parts(int64_t groups, int threads, F&& launch)

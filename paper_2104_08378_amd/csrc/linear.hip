@@ -98,9 +98,8 @@ template <int DT, int OUT>
 static sp24_status run_segments(const SegmentArgs& a, int experts, hipStream_t st)
 {
     auto run = [&](auto kernel, int columns) {
-        const int tiles_m = (int)((a.M + 127) / 128), tiles_n = (int)((a.N + columns - 1) / columns);
-        kernel<<<dim3((unsigned)(tiles_m * tiles_n), (unsigned)experts), 512, 0, st>>>(a, tiles_m, tiles_n);
-        return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
+        const int64_t tiles_m = (a.M + 127) / 128, tiles_n = (a.N + columns - 1) / columns;
+        return launch_tiles(tiles_m * tiles_n, experts, 512, [&](dim3 grid, dim3 block) { kernel<<<grid, block, 0, st>>>(a, (int)tiles_m, (int)tiles_n); });
     };
     if ((a.N + 255) / 256 * 256 * 4 > (a.N + 127) / 128 * 128 * 5) return run(k_gemm_pipe<DT, OUT, 4, 2, 1, 2, 2, 2, SegmentArgs>, 128);
     return run(k_gemm_pipe<DT, OUT, 2, 4, 2, 2, 3, 2, SegmentArgs>, 256);

@@ -11,8 +11,9 @@ static sp24_status run_layer_stream(const ARGS& a, hipStream_t st)
     int64_t tiles_n;
     if constexpr (std::is_same<ARGS, GroupedArgs>::value) tiles_n = grouped_tiles(a.N, a.experts, BR);
     else tiles_n = (a.N + BR - 1) / BR;
-    k_spmm_stream<DT, BR, NW, NS, false, ARGS><<<(unsigned)(tiles_m * tiles_n), 64 * NW, 0, st>>>(a, (int)tiles_m, (int)tiles_n);
-    return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
+    return launch_tiles(tiles_m * tiles_n, 1, 64 * NW, [&](dim3 grid, dim3 block) {
+        k_spmm_stream<DT, BR, NW, NS, false, ARGS><<<grid, block, 0, st>>>(a, (int)tiles_m, (int)tiles_n);
+    });
 }
 
 sp24_status launch_linear_stream(const LinearArgs& a, hipStream_t st)

@@ -13,8 +13,9 @@ static sp24_status run_layer(const ARGS& a, hipStream_t st)
     int64_t tiles_n;
     if constexpr (std::is_same<ARGS, GroupedArgs>::value) tiles_n = grouped_tiles(a.N, a.experts, BN);
     else tiles_n = (a.N + BN - 1) / BN;
-    k_spmm_pipe<DT, SP24_F32, WM, WN, TM, TN, NS, 0, ARGS><<<(unsigned)(tiles_m * tiles_n), 64 * WM * WN, 0, st>>>(a, (int)tiles_m, (int)tiles_n);
-    return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
+    return launch_tiles(tiles_m * tiles_n, 1, 64 * WM * WN, [&](dim3 grid, dim3 block) {
+        k_spmm_pipe<DT, SP24_F32, WM, WN, TM, TN, NS, 0, ARGS><<<grid, block, 0, st>>>(a, (int)tiles_m, (int)tiles_n);
+    });
 }
 
 template <int DT, class ARGS>
@@ -43,8 +44,7 @@ sp24_status layer_staged(const ARGS& a, hipStream_t st)
         int64_t tiles_n;
         if constexpr (std::is_same<ARGS, GroupedArgs>::value) tiles_n = grouped_tiles(a.N, a.experts, bn);
         else tiles_n = (a.N + bn - 1) / bn;
-        kernel<<<(unsigned)(tiles_m * tiles_n), 256, 0, st>>>(a, (int)tiles_m, (int)tiles_n);
-        return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
+        return launch_tiles(tiles_m * tiles_n, 1, 256, [&](dim3 grid, dim3 block) { kernel<<<grid, block, 0, st>>>(a, (int)tiles_m, (int)tiles_n); });
     };
     if (((a.M + 63) / 64) * ((a.N + 63) / 64) <= 256) return run(k_spmm_staged<DT, 0, 2, 2, 1, 1, ARGS>, 64, 64);
     if (a.M <= 64 || ((a.M + 127) / 128) * ((a.N + 127) / 128) < 256) return run(k_spmm_staged<DT, 0, 2, 2, 1, 2, ARGS>, 64, 128);
