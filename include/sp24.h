@@ -450,9 +450,9 @@ sp24_status sp24_conv2d_dense_i8_scaled(const void* A, const void* X, void* D, i
  * 32-bit integers are contiguous.  Sums, statistics and every intermediate value
  * are binary32; a result is rounded once, to nearest even.  The general
  * conventions above hold: no allocation, no synchronisation, errors before any
- * launch.  Buffers that a call writes may not overlap its others, except in place
- * (the same address and row stride) where said.  Results are the same from call
- * to call.
+ * launch.  Buffers that a call writes may not overlap its others (ranges of bytes from a
+ * matrix's first element to its last), except in place (the same address and row
+ * stride) where said.  Results are the same from call to call.
  * ---------------------------------------------------------------------------
  */
 

@@ -29,7 +29,7 @@ Span matrix(const void* p, int64_t rows, int64_t cols, int64_t ld, int es)
 }
 Span vec(const void* p, int64_t n, int es) { return {p, p && n > 0 ? (size_t)n * es : 0}; }
 
-// does `out` share bytes with one of `others`, those at its own address excepted where `same_ok` (an operation in place)?
+// does `out` share bytes with one of `others`?  (Ranges from the first element's byte to the last's: rows that lie between another buffer's rows count)
 bool overlaps(Span out, std::initializer_list<Span> others)
 {
     for (const Span& o : others)

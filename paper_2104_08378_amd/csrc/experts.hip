@@ -14,7 +14,10 @@ namespace sp24 {
 // Placing takes some 85 instructions to 64 choices, which one compute unit issues at 0.5 us a thousand (4096 x 2 choices of eight 8.7 us on one
 // workgroup), counting a few: every workgroup counts all choices, from the L2, and places a thousand, one launch and nothing to wait for (5.7 us; 4096 x 4
 // of 64 16.7 -> 6.2).
-// Past kSortAtOnce choices that counting is the longer part: parts of kSortPart count, a scan over parts and experts, and parts place.
+// Past kSortAtOnce choices parts of kSortPart count, a scan over parts and experts, and parts place: three launches whose time hardly grows, where
+// counting everything in every workgroup grows with the square.  One launch / parts, us, uniform choices: of 8 experts 2^13 6.1 / 15.1, 2^16
+// 18.1 / 21.3, 2^17 32 / 21.3, 2^18 60 / 22.4, 2^20 800 / 28; of 64 2^13 5.6 / 17.8, 2^16 12.4 / 27.2, 2^17 20.4 / 27.2, 2^18 38 / 28.4; of 1024 2^13 9.9 /
+// 27.4, 2^17 25.1 / 42.4, 2^18 44.1 / 43.6.  2^17 is between the experts' numbers: right for 64, past the crossing for 8 (about 2^16), before it for 1024.
 // ---------------------------------------------------------------------------
 constexpr int kSortWaves = 16, kSortExperts = 1024;
 
@@ -274,7 +277,7 @@ sp24_status launch_moe_sort(const SortArgs& a, hipStream_t st)
 
 // ---------------------------------------------------------------------------
 // Rows by expert: row i is the token of choice rows[i], zeros where there is none.  Bound by memory, 16 bytes a thread.
-// 4096 tokens of 4096 bf16 to two experts each: 21.2 us, 101 MB at 4.7 TB/s where a token is counted once.
+// 4096 tokens of 4096 bf16 to two experts each: 21.2 us, 101 MB at 4.7 TB/s where a token is counted once; int8 with scales 12.1 (4.2), 16 tokens 2.6.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ uint4v load_bytes(const uint8_t* p, int64_t n)
 {
@@ -328,7 +331,8 @@ sp24_status launch_moe_gather(const GatherArgs& a, hipStream_t st)
 
 // ---------------------------------------------------------------------------
 // out[n] = residual[n] + sum over j, in that order, of weights[n][j] Y[slots[n][j]], in binary32, rounded once.  Bound by memory, eight
-// values a thread.  4096 tokens of 4096 bf16 from two experts each, with residual: 22.0 us, 134 MB at 6.1 TB/s.
+// values a thread.  4096 tokens of 4096 bf16 from two experts each, with residual: 22.0 us, 134 MB at 6.1 TB/s.  (Y, residual and out have one type:
+// the experts' results come rounded to it, and out is; a float32 stream takes float32 results.)
 // ---------------------------------------------------------------------------
 template <int T>
 __global__ __launch_bounds__(256) void k_moe_combine(CombineArgs a, int blocks_a_row, unsigned from)

@@ -152,7 +152,7 @@ struct LinearGradArgs {
 };
 sp24_status launch_linear_grad(const LinearGradArgs& a, hipStream_t st);
 
-constexpr int kSortAtOnce = 1 << 17;      // choices that one launch sorts; of more, parts of kSortPart
+constexpr int kSortAtOnce = 1 << 17;      // choices that one launch sorts (both sides measured in experts.hip); of more, parts of kSortPart
 constexpr int kSortPart = 16384;
 struct SortArgs {
     const int32_t* ids;                   // T choices
