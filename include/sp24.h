@@ -582,6 +582,85 @@ sp24_status sp24_linear_grouped(const void* V, const void* meta, const void* X, 
 sp24_status sp24_gemm_dense_grouped(const void* A, const void* B, void* D, const int32_t* offsets, int experts, int64_t M, int64_t N,
                                     int64_t rows, int64_t lda, int64_t ldb, int64_t ldd, sp24_dtype in, sp24_dtype out, void* stream);
 
+typedef enum { SP24_SCORE_SOFTMAX = 0, SP24_SCORE_SIGMOID = 1 } sp24_score;
+
+/*
+ * The experts of every token and their weights, from the router's logits, N x experts of type t = SP24_F32, SP24_F16 or SP24_BF16:
+ *   s[n][e] = softmax of row n, or 1 / (1 + exp(-logits[n][e]));  c[n][e] = s[n][e] + bias[e]            (bias NULL: 0)
+ *   ids[n][0 .. topk-1] = the experts of the largest c, descending, the lower expert on a tie
+ *   weights[n][j] = scale * s[n][ids[n][j]], renormalise != 0: divided by their sum over j (0 where that is 0)
+ * groups > 1: the experts are `groups` runs of experts / groups (a whole number), a group's value the sum of its group_best (1 or 2) largest
+ * c, and only experts of the groups_kept groups of largest value (the lower group on a tie) can be chosen.
+ * All of it is binary64, each result rounded once: the choice does not hang on a rounding of binary32.
+ * An expert with a logit or c of -inf is never chosen (its score is 0 where the logit is -inf); where fewer than topk are left, the last ids are -1, which
+ * sp24_moe_sort gives no row, and their weights 0.  A group of one such expert less counts what it has.  NaN is larger than every number: it is chosen, and its
+ * weight (renormalised: every one of the row) is NaN.
+ * scores (NULL: not wanted): N x experts floats, contiguous, receives s.  load (NULL: not wanted): experts entries, receives how many of the N x
+ * topk choices are each expert's, what a bias for balance is led by.
+ * experts <= SP24_MOST_EXPERTS, topk <= SP24_MOST_CHOICES and <= groups_kept * (experts / groups); scale finite.
+ */
+#define SP24_MOST_CHOICES 64
+sp24_status sp24_moe_route(const void* logits, const float* bias, int32_t* ids, float* weights, float* scores, int32_t* load, int64_t N,
+                           int experts, int topk, int groups, int groups_kept, int group_best, sp24_score score, int renormalise, float scale,
+                           int64_t ldl, sp24_dtype t, void* stream);
+
+/*
+ * Its gradient: dlogits (N x experts of type t, may be logits in place) from dweights (N x topk) and dscores (N x experts floats, contiguous; NULL: none),
+ * the choice being held.  ids as sp24_moe_route wrote them; an entry outside 0 .. experts - 1 has no part, one that is there twice has both.
+ *   g[e] = dscores[e] + sum over j of [ids[j] = e] h[j],  h = scale * dweights, renormalised scale * (dweights - sum(dweights s) / W) / W,  W = sum s (0: h = 0)
+ *   softmax: dlogits = s (g - sum g s);  sigmoid: dlogits = s (1 - s) g;  0 where the logit is -inf
+ */
+sp24_status sp24_moe_route_backward(const void* logits, const int32_t* ids, const float* dweights, const float* dscores, void* dlogits, int64_t N,
+                                    int experts, int topk, sp24_score score, int renormalise, float scale, int64_t ldl, int64_t lddl, sp24_dtype t,
+                                    void* stream);
+
+/*
+ * Rows kept in 8 bits for the backward pass (a checkpoint of activations): codes with a scale for every SP24_CHECKPOINT_BLOCK
+ * neighbouring values of a row, so that a channel far larger than the others takes the precision of its own block alone.
+ *   m = max(max |x| of the block, 2^-100), scale = m / 127 (SP24_I8) or m / 448 (SP24_F8), code = x * (127 or 448) / m, the quotient rounded to
+ *   binary32 and that to the nearest code (ties to even)
+ * A block that holds an infinity or a NaN has the scale NaN, and stands for NaN throughout.
+ * X: N x H of type t = SP24_F32, SP24_F16 or SP24_BF16.  codes: N x H of type `code`, row stride ldc.  scale: N x ceil(H / block) floats, contiguous.
+ */
+#define SP24_CHECKPOINT_BLOCK 128
+sp24_status sp24_checkpoint_rows(const void* X, void* codes, float* scale, int64_t N, int64_t H, int64_t ldx, int64_t ldc, sp24_dtype t,
+                                 sp24_dtype code, void* stream);
+
+/*
+ * out[r][i] = act(codes[n][i] * scale[n][i / block]), n = r, or (rows, of sp24_moe_sort) n = rows[r] / topk: the rows of sorted choices from the
+ * tokens' kept ones, zeros where rows[r] is -1 (or names no token).  codes, scale: N rows as sp24_checkpoint_rows wrote them.  out: R x H of type t = SP24_F32,
+ * SP24_F16 or SP24_BF16; without `rows` R == N.
+ */
+sp24_status sp24_restore_rows(const void* codes, const float* scale, const int32_t* rows, void* out, int64_t N, int64_t R, int topk, int64_t H,
+                              int64_t ldc, int64_t ldo, sp24_act act, sp24_dtype code, sp24_dtype t, void* stream);
+
+/*
+ * sp24_linear_backward with Z kept in 8 bits: zcodes (N x M of type `code`, row stride ldz) and zscale (N x ceil(M / block)); both may be NULL for
+ * SP24_ACT_NONE.  Everything else as there.  dZ may be dY in place.
+ */
+sp24_status sp24_linear_backward_checkpoint(const void* dY, const void* zcodes, const float* zscale, void* dZ, void* dZt, float* dbias, int64_t M,
+                                            int64_t N, int64_t lddy, int64_t ldz, int64_t lddz, int64_t lddzt, sp24_act act, const int32_t* offsets,
+                                            int experts, sp24_dtype code, sp24_dtype t, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The weights' gradient from rows kept in 8 bits: D = A x B, A: M x K of type in = SP24_F16 or SP24_BF16 (the dZt of the layer's gradient, K its tokens),
+ * B: the K x N values that `codes` and `scale` stand for, each rounded to `in`, the matrix instructions' operand (codes times scale has at most 2^-8 of a
+ * block's largest value of precision: this is no more than half of that for the largest, less for all others).  Binary32 sums.  D: M x N of type
+ * `in` or SP24_F32.  K may be any number, 0 included, which gives zeros.  Rows of A must be 16-byte aligned; what lies between K and the next 16-byte
+ * boundary of a row may be read and is not used.
+ */
+sp24_status sp24_gemm_dense_checkpoint(const void* A, const void* codes, const float* scale, void* D, int64_t M, int64_t N, int64_t K, int64_t lda,
+                                       int64_t ldc, int64_t ldd, sp24_dtype in, sp24_dtype code, sp24_dtype out, void* stream);
+
+/*
+ * sp24_gemm_dense_grouped with its second operand kept in 8 bits: D_e = A[:, segment e] x B[segment e, :].  `rows` NULL: row r of B is row r of
+ * `codes`, which has `row_count` rows then (tokens == row_count).  Else row r of B is row rows[r] / topk of the `tokens` rows of codes, the rows of sorted choices from the tokens' kept
+ * ones, and zeros where rows[r] is -1 (or names no token).  offsets and the limits as there, with any N.
+ */
+sp24_status sp24_gemm_dense_grouped_checkpoint(const void* A, const void* codes, const float* scale, const int32_t* rows, void* D, const int32_t* offsets,
+                                               int experts, int64_t M, int64_t N, int64_t row_count, int64_t tokens, int topk, int64_t lda, int64_t ldc,
+                                               int64_t ldd, sp24_dtype in, sp24_dtype code, sp24_dtype out, void* stream);
+
 /* Static, NUL-terminated description of a status code. */
 const char* sp24_status_string(sp24_status s);
 

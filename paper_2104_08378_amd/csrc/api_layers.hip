@@ -239,17 +239,21 @@ size_t sp24_linear_backward_workspace_bytes(int64_t M, int64_t N, int grouped)
     return (size_t)((N + unit - 1) / unit) * M * 4;
 }
 
-sp24_status sp24_linear_backward(const void* dY, const void* Z, void* dZ, void* dZt, float* dbias, int64_t M, int64_t N, int64_t lddy, int64_t ldz,
-                                 int64_t lddz, int64_t lddzt, sp24_act act, const int32_t* offsets, int experts, sp24_dtype t, void* workspace,
-                                 size_t workspace_bytes, void* stream)
+// Z: values of type t (zcode == t), or codes of type zcode with their scales
+static sp24_status linear_backward(const void* dY, const void* Z, const float* zscale, void* dZ, void* dZt, float* dbias, int64_t M, int64_t N, int64_t lddy,
+                                   int64_t ldz, int64_t lddz, int64_t lddzt, sp24_act act, const int32_t* offsets, int experts, sp24_dtype zcode,
+                                   sp24_dtype t, void* workspace, size_t workspace_bytes, void* stream)
 {
+    const int zs = esize_of(zcode);
+    const bool kept = zcode != t;
     if (!is_float16(t) || !is_act(act)) return SP24_ERR_DTYPE;
     if (M < 0 || N < 0 || M > kMostRows || N > kMostRows || ((M + 63) / 64) * ((N + 63) / 64) >= ((int64_t)1 << 31)) return SP24_ERR_SHAPE;
     if (offsets && (experts < 1 || experts > SP24_MOST_EXPERTS || N % kSegmentRows != 0)) return SP24_ERR_SHAPE;
     if (offsets && misaligned(offsets, 4)) return SP24_ERR_ALIGN;
     if (M == 0) return SP24_OK;
     SP24_TRY(check_matrix(dY, N, M, lddy, 2, false));
-    if (act != SP24_ACT_NONE) SP24_TRY(check_matrix(Z, N, M, ldz, 2, false));
+    if (act != SP24_ACT_NONE) SP24_TRY(check_matrix(Z, N, M, ldz, zs, false));
+    if (act != SP24_ACT_NONE && kept && N > 0) SP24_TRY(check_vector(zscale));
     if (dZ) SP24_TRY(check_matrix(dZ, N, M, lddz, 2, false));
     if (dZt && N > 0) SP24_TRY(check_matrix(dZt, M, N, lddzt, 2, false));
     const size_t need = dbias ? sp24_linear_backward_workspace_bytes(M, N, offsets != nullptr) : 0;
@@ -259,14 +263,32 @@ sp24_status sp24_linear_backward(const void* dY, const void* Z, void* dZ, void* 
         if (need > 0 && !aligned16(workspace)) return SP24_ERR_ALIGN;
         if (workspace_bytes < need) return SP24_ERR_SHAPE;
     }
-    const Span dy = matrix(dY, N, M, lddy, 2), z = matrix(act != SP24_ACT_NONE ? Z : nullptr, N, M, ldz, 2), dz = matrix(dZ, N, M, lddz, 2),
+    const Span dy = matrix(dY, N, M, lddy, 2), z = matrix(act != SP24_ACT_NONE ? Z : nullptr, N, M, ldz, zs),
+               zc = vec(act != SP24_ACT_NONE && kept ? zscale : nullptr, N * kept_blocks(M), 4), dz = matrix(dZ, N, M, lddz, 2),
                dzt = matrix(dZt, M, N, lddzt, 2), db = vec(dbias, (offsets ? experts : 1) * M, 4), ws = Span{workspace, need},
                of = vec(offsets, offsets ? experts + 1 : 0, 4);
-    if (overlaps(dz, {dzt, db, ws, of}) || overlaps(dzt, {dy, z, db, ws, of}) || overlaps(db, {dy, z, ws, of}) || overlaps(ws, {dy, z, of})) return SP24_ERR_SHAPE;
-    if ((overlaps(dz, {dy}) && !in_place(dz, lddz, dy, lddy, 2, 2)) || (overlaps(dz, {z}) && !in_place(dz, lddz, z, ldz, 2, 2))) return SP24_ERR_SHAPE;
-    return launch_linear_grad(LinearGradArgs{dY, Z, dZ, dZt, dbias ? static_cast<float*>(workspace) : nullptr, dbias, offsets, M, N, lddy, ldz, lddz, lddzt,
-                                             (int)act, experts, grad_unit(offsets), t},
+    if (overlaps(dz, {dzt, db, ws, of, zc}) || overlaps(dzt, {dy, z, db, ws, of, zc}) || overlaps(db, {dy, z, ws, of, zc}) || overlaps(ws, {dy, z, of, zc}))
+        return SP24_ERR_SHAPE;
+    if ((overlaps(dz, {dy}) && !in_place(dz, lddz, dy, lddy, 2, 2)) || (overlaps(dz, {z}) && !in_place(dz, lddz, z, ldz, 2, zs))) return SP24_ERR_SHAPE;
+    return launch_linear_grad(LinearGradArgs{dY, Z, zscale, dZ, dZt, dbias ? static_cast<float*>(workspace) : nullptr, dbias, offsets, M, N, lddy, ldz, lddz, lddzt,
+                                             (int)act, experts, grad_unit(offsets), t, zcode},
                               static_cast<hipStream_t>(stream));
+}
+
+sp24_status sp24_linear_backward(const void* dY, const void* Z, void* dZ, void* dZt, float* dbias, int64_t M, int64_t N, int64_t lddy, int64_t ldz,
+                                 int64_t lddz, int64_t lddzt, sp24_act act, const int32_t* offsets, int experts, sp24_dtype t, void* workspace,
+                                 size_t workspace_bytes, void* stream)
+{
+    return linear_backward(dY, Z, nullptr, dZ, dZt, dbias, M, N, lddy, ldz, lddz, lddzt, act, offsets, experts, t, t, workspace, workspace_bytes, stream);
+}
+
+sp24_status sp24_linear_backward_checkpoint(const void* dY, const void* zcodes, const float* zscale, void* dZ, void* dZt, float* dbias, int64_t M,
+                                            int64_t N, int64_t lddy, int64_t ldz, int64_t lddz, int64_t lddzt, sp24_act act, const int32_t* offsets,
+                                            int experts, sp24_dtype code, sp24_dtype t, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!is_code(code)) return SP24_ERR_DTYPE;
+    return linear_backward(dY, zcodes, zscale, dZ, dZt, dbias, M, N, lddy, ldz, lddz, lddzt, act, offsets, experts, code, t, workspace, workspace_bytes,
+                           stream);
 }
 
 int64_t sp24_moe_rows(int64_t choices, int experts)
@@ -367,6 +389,128 @@ sp24_status sp24_moe_combine_backward(const void* dOut, const void* Y, const int
     if (overlaps(dy, {y}) && !in_place(dy, lddy, y, ldy, es, es)) return SP24_ERR_SHAPE;
     return launch_moe_combine_grad(CombineGradArgs{dOut, Y, rows, slots, weights, dY, dweights, N, row_count, H, lddo, ldy, lddy, topk, t},
                                    static_cast<hipStream_t>(stream));
+}
+
+static bool is_score(sp24_score score) { return score == SP24_SCORE_SOFTMAX || score == SP24_SCORE_SIGMOID; }
+
+sp24_status sp24_moe_route(const void* logits, const float* bias, int32_t* ids, float* weights, float* scores, int32_t* load, int64_t N, int experts,
+                           int topk, int groups, int groups_kept, int group_best, sp24_score score, int renormalise, float scale, int64_t ldl, sp24_dtype t,
+                           void* stream)
+{
+    if (!is_float(t) || !is_score(score)) return SP24_ERR_DTYPE;
+    if (N < 0 || N > kMostRows || experts < 1 || experts > SP24_MOST_EXPERTS || topk < 1 || topk > SP24_MOST_CHOICES) return SP24_ERR_SHAPE;
+    if (groups < 1 || groups > experts || experts % groups != 0 || groups_kept < 1 || groups_kept > groups || (group_best != 1 && group_best != 2)) return SP24_ERR_SHAPE;
+    if (topk > groups_kept * (experts / groups) || !std::isfinite(scale)) return SP24_ERR_SHAPE;
+    if (load) SP24_TRY(check_vector(load));
+    const int es = esize_of(t);
+    if (N > 0) {
+        SP24_TRY(check_matrix(logits, N, experts, ldl, es, false));
+        if (bias) SP24_TRY(check_vector(bias));
+        SP24_TRY(check_vector(ids));
+        SP24_TRY(check_vector(weights));
+        if (scores) SP24_TRY(check_vector(scores));
+    }
+    const Span l = matrix(logits, N, experts, ldl, es), b = vec(bias, experts, 4), id = vec(ids, N * topk, 4), w = vec(weights, N * topk, 4),
+               sc = vec(scores, N * experts, 4), lo = vec(load, experts, 4);
+    if (overlaps(id, {l, b, w, sc, lo}) || overlaps(w, {l, b, sc, lo}) || overlaps(sc, {l, b, lo}) || overlaps(lo, {l, b})) return SP24_ERR_SHAPE;
+    return launch_moe_route(RouteArgs{logits, bias, ids, weights, scores, load, N, ldl, experts, topk, groups, groups_kept, group_best,
+                                      score == SP24_SCORE_SOFTMAX, renormalise != 0, scale, t},
+                            static_cast<hipStream_t>(stream));
+}
+
+sp24_status sp24_moe_route_backward(const void* logits, const int32_t* ids, const float* dweights, const float* dscores, void* dlogits, int64_t N,
+                                    int experts, int topk, sp24_score score, int renormalise, float scale, int64_t ldl, int64_t lddl, sp24_dtype t,
+                                    void* stream)
+{
+    if (!is_float(t) || !is_score(score)) return SP24_ERR_DTYPE;
+    if (N < 0 || N > kMostRows || experts < 1 || experts > SP24_MOST_EXPERTS || topk < 1 || topk > SP24_MOST_CHOICES || !std::isfinite(scale)) return SP24_ERR_SHAPE;
+    if (N == 0) return SP24_OK;
+    const int es = esize_of(t);
+    SP24_TRY(check_matrix(logits, N, experts, ldl, es, false));
+    SP24_TRY(check_matrix(dlogits, N, experts, lddl, es, false));
+    SP24_TRY(check_vector(ids));
+    SP24_TRY(check_vector(dweights));
+    if (dscores) SP24_TRY(check_vector(dscores));
+    const Span l = matrix(logits, N, experts, ldl, es), d = matrix(dlogits, N, experts, lddl, es);
+    if (overlaps(d, {vec(ids, N * topk, 4), vec(dweights, N * topk, 4), vec(dscores, N * experts, 4)})) return SP24_ERR_SHAPE;
+    if (overlaps(d, {l}) && !in_place(d, lddl, l, ldl, es, es)) return SP24_ERR_SHAPE;
+    return launch_moe_route_grad(RouteGradArgs{logits, ids, dweights, dscores, dlogits, N, ldl, lddl, experts, topk, score == SP24_SCORE_SOFTMAX,
+                                               renormalise != 0, scale, t},
+                                 static_cast<hipStream_t>(stream));
+}
+
+// the blocks of so many rows have numbers that the launches can count
+static bool blocks_fit(int64_t rows, int64_t H) { return rows <= ((int64_t)1 << 35) / kept_blocks(H); }
+
+sp24_status sp24_checkpoint_rows(const void* X, void* codes, float* scale, int64_t N, int64_t H, int64_t ldx, int64_t ldc, sp24_dtype t, sp24_dtype code,
+                                 void* stream)
+{
+    if (!is_float(t) || !is_code(code)) return SP24_ERR_DTYPE;
+    if (N < 0 || H < 1 || N > kMostRows || H > kMostRows || !blocks_fit(N, H)) return SP24_ERR_SHAPE;
+    if (N == 0) return SP24_OK;
+    const int es = esize_of(t);
+    SP24_TRY(check_matrix(X, N, H, ldx, es, false));
+    SP24_TRY(check_matrix(codes, N, H, ldc, 1, false));
+    SP24_TRY(check_vector(scale));
+    const Span x = matrix(X, N, H, ldx, es), c = matrix(codes, N, H, ldc, 1), sc = vec(scale, N * kept_blocks(H), 4);
+    if (overlaps(c, {x, sc}) || overlaps(sc, {x})) return SP24_ERR_SHAPE;
+    return launch_checkpoint_rows(KeepArgs{X, codes, scale, N, H, ldx, ldc, t, code}, static_cast<hipStream_t>(stream));
+}
+
+sp24_status sp24_restore_rows(const void* codes, const float* scale, const int32_t* rows, void* out, int64_t N, int64_t R, int topk, int64_t H, int64_t ldc,
+                              int64_t ldo, sp24_act act, sp24_dtype code, sp24_dtype t, void* stream)
+{
+    if (!is_float(t) || !is_code(code) || !is_act(act)) return SP24_ERR_DTYPE;
+    if (N < 0 || R < 0 || H < 1 || N > kMostRows || R > kMostRows || H > kMostRows || topk < 1 || !blocks_fit(R, H) || !blocks_fit(N, H)) return SP24_ERR_SHAPE;
+    if (R == 0) return SP24_OK;                                        // (an empty `rows` may have no address)
+    if (!rows && R != N) return SP24_ERR_SHAPE;
+    const int es = esize_of(t);
+    SP24_TRY(check_matrix(codes, N, H, ldc, 1, false));
+    if (N > 0) SP24_TRY(check_vector(scale));
+    SP24_TRY(check_matrix(out, R, H, ldo, es, false));
+    if (rows) SP24_TRY(check_vector(rows));
+    if (overlaps(matrix(out, R, H, ldo, es), {matrix(codes, N, H, ldc, 1), vec(scale, N * kept_blocks(H), 4), vec(rows, R, 4)})) return SP24_ERR_SHAPE;
+    return launch_restore_rows(RestoreArgs{codes, scale, rows, out, N, R, H, ldc, ldo, topk, (int)act, code, t}, static_cast<hipStream_t>(stream));
+}
+
+// What both products from kept rows check.  K: columns of A; tokens: rows of the codes
+static sp24_status gemm_kept(const KeptMmArgs& a, void* stream)
+{
+    if (!is_float16(a.in) || !is_code(a.code) || !(a.out == SP24_F32 || a.out == a.in)) return SP24_ERR_DTYPE;
+    if (a.M < 0 || a.N < 0 || a.K < 0 || a.tokens < 0 || a.M > kMostRows || a.N > kMostRows || a.K > kMostRows || a.tokens > kMostRows || a.topk < 1) return SP24_ERR_SHAPE;
+    if (a.M == 0 || a.N == 0) return SP24_OK;
+    if (!blocks_fit(a.tokens, a.N)) return SP24_ERR_SHAPE;
+    const int os = esize_of(a.out);
+    if (a.K > 0) {
+        SP24_TRY(check_matrix(a.A, a.M, a.K, a.lda, 2));
+        if (a.lda >= (int64_t)1 << 23) return SP24_ERR_SHAPE;           // 32-bit offsets inside a tile
+        if (a.tokens > 0) {
+            SP24_TRY(check_matrix(a.codes, a.tokens, a.N, a.ldc, 1, false));
+            SP24_TRY(check_vector(a.scale));
+        }
+        if (a.rows) SP24_TRY(check_vector(a.rows));
+    }
+    SP24_TRY(check_matrix(a.D, a.M * a.experts, a.N, a.ldd, os, false));
+    if (overlaps(matrix(a.D, a.M * a.experts, a.N, a.ldd, os),
+                 {matrix(a.A, a.M, a.K, a.lda, 2), matrix(a.codes, a.tokens, a.N, a.ldc, 1), vec(a.scale, a.tokens * kept_blocks(a.N), 4), vec(a.rows, a.K, 4),
+                  vec(a.offsets, a.experts + 1, 4)}))
+        return SP24_ERR_SHAPE;
+    return launch_gemm_kept(a, static_cast<hipStream_t>(stream));
+}
+
+sp24_status sp24_gemm_dense_checkpoint(const void* A, const void* codes, const float* scale, void* D, int64_t M, int64_t N, int64_t K, int64_t lda, int64_t ldc,
+                                       int64_t ldd, sp24_dtype in, sp24_dtype code, sp24_dtype out, void* stream)
+{
+    return gemm_kept(KeptMmArgs{A, codes, scale, nullptr, nullptr, D, M, N, K, K, lda, ldc, ldd, 1, 1, in, code, out}, stream);
+}
+
+sp24_status sp24_gemm_dense_grouped_checkpoint(const void* A, const void* codes, const float* scale, const int32_t* rows, void* D, const int32_t* offsets,
+                                               int experts, int64_t M, int64_t N, int64_t row_count, int64_t tokens, int topk, int64_t lda, int64_t ldc,
+                                               int64_t ldd, sp24_dtype in, sp24_dtype code, sp24_dtype out, void* stream)
+{
+    if (experts < 1 || experts > SP24_MOST_EXPERTS || row_count % kSegmentRows != 0 || (!rows && row_count > 0 && tokens != row_count)) return SP24_ERR_SHAPE;
+    if (M > 0 && N > 0) SP24_TRY(check_vector(offsets));
+    return gemm_kept(KeptMmArgs{A, codes, scale, rows, offsets, D, M, N, row_count, tokens, lda, ldc, ldd, topk, experts, in, code, out}, stream);
 }
 
 } // extern "C"

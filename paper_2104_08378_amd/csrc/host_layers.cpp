@@ -397,6 +397,288 @@ PyObject* moe_combine_backward(PyObject* self, PyObject* const* args, Py_ssize_t
     return s == SP24_OK ? tuple(dY.object(), wrap(dw)) : refused(self, s, "sp24_moe_combine_backward");
 }
 
+// what a call of the functions below reads or writes has to be on the device whose stream it goes to
+void here(Call& c, const at::Tensor* t)
+{
+    if (c.ok && t) c.require(t->device().index() == c10::hip::current_device());
+}
+template <typename T>
+T* entries_here(Call& c, int i, int64_t n, at::ScalarType type)
+{
+    T* const p = entries<T>(c, i, n, type);
+    if (c.ok && !c.none(i)) here(c, c.tensor(i));
+    return p;
+}
+
+bool softmax_score(Call& c, int i)
+{
+    if (c.text_is(i, "softmax")) return true;
+    c.require(c.text_is(i, "sigmoid"));
+    return false;
+}
+int small(Call& c, int i)
+{
+    const int64_t v = c.integer(i);
+    c.require(v >= 0 && v <= INT32_MAX);
+    return c.ok ? (int)v : 0;
+}
+bool is_float_row(at::ScalarType t) { return t == at::kFloat || t == at::kHalf || t == at::kBFloat16; }
+bool is_code_type(at::ScalarType t) { return t == at::kChar || t == at::kFloat8_e4m3fn; }
+
+// rows kept in 8 bits (argument i, a pair of codes and scales)
+struct Kept {
+    PyObject* parts[2] = {nullptr, nullptr};
+    const at::Tensor *codes = nullptr, *scale = nullptr;
+    int64_t N = 0, H = 0, ld_ = 0;
+    Kept(Call& c, int i)
+    {
+        if (!c.ok) return;
+        c.require(PyTuple_Check(c.args[i]) && PyTuple_GET_SIZE(c.args[i]) == 2);
+        if (!c.ok) return;
+        for (int k = 0; k < 2; ++k) parts[k] = PyTuple_GET_ITEM(c.args[i], k);
+        Call p{parts, true};
+        codes = p.rowmajor(0);
+        scale = p.contiguous(1);
+        c.require(p.ok);
+        if (!c.ok) return;
+        N = codes->size(0);
+        H = codes->size(1);
+        ld_ = ld(*codes);
+        c.require(is_code_type(codes->scalar_type()) && scale->scalar_type() == at::kFloat &&
+                  scale->numel() == N * ((H + SP24_CHECKPOINT_BLOCK - 1) / SP24_CHECKPOINT_BLOCK));
+        here(c, codes);
+        here(c, scale);
+    }
+    const void* data() const { return codes->data_ptr(); }
+    const float* scales() const { return static_cast<const float*>(scale->data_ptr()); }
+};
+
+// (logits, topk, score, bias, groups, groups_kept, group_best, renormalise, scale, want_scores, want_load) -> (ids, weights, scores, load)
+PyObject* moe_route(PyObject* self, PyObject* const* args, Py_ssize_t)
+{
+    Call c{args, true};
+    const at::Tensor* X = c.rowmajor(0);
+    const int topk = small(c, 1);
+    const bool softmax = softmax_score(c, 2);
+    if (!c.ok) return not_handled();
+    const int64_t N = X->size(0), E = X->size(1);
+    here(c, X);
+    c.require(is_float_row(X->scalar_type()) && topk >= 1 && topk <= SP24_MOST_CHOICES && E >= 1 && E <= SP24_MOST_EXPERTS);
+    const float* bias = entries_here<const float>(c, 3, E, at::kFloat);
+    const int groups = small(c, 4), kept = small(c, 5), best = small(c, 6), renormalise = c.truth(7);
+    const float scale = c.real(8);
+    const int want_scores = c.truth(9), want_load = c.truth(10);
+    if (!c.ok) return not_handled();
+    const sp24_dtype t = type_of(X->scalar_type(), c.ok);
+    at::Tensor ids = make({N, topk}, at::kInt, *X), weights = make({N, topk}, at::kFloat, *X), scores, load;
+    if (want_scores) scores = make({N, E}, at::kFloat, *X);
+    if (want_load) load = make({E}, at::kInt, *X);
+    const void* px = X->data_ptr();
+    int32_t *pi = static_cast<int32_t*>(ids.data_ptr()), *pl = want_load ? static_cast<int32_t*>(load.data_ptr()) : nullptr;
+    float *pw = static_cast<float*>(weights.data_ptr()), *ps = want_scores ? static_cast<float*>(scores.data_ptr()) : nullptr;
+    void* st = stream();
+    const int64_t ldx = ld(*X);
+    const sp24_status s = without_gil([&] {
+        return sp24_moe_route(px, bias, pi, pw, ps, pl, N, (int)E, topk, groups, kept, best, softmax ? SP24_SCORE_SOFTMAX : SP24_SCORE_SIGMOID, renormalise, scale,
+                              ldx, t, st);
+    });
+    return s == SP24_OK ? tuple(wrap(ids), wrap(weights), wrap(scores), wrap(load)) : refused(self, s, "sp24_moe_route");
+}
+
+// (logits, ids, dweights, score, renormalise, scale, dscores, out)
+PyObject* moe_route_backward(PyObject* self, PyObject* const* args, Py_ssize_t)
+{
+    Call c{args, true};
+    const at::Tensor *X = c.rowmajor(0), *ids = c.contiguous(1);
+    const bool softmax = softmax_score(c, 3);
+    c.require(!c.none(2));
+    if (!c.ok) return not_handled();
+    c.require(ids->dim() == 2 && ids->scalar_type() == at::kInt && is_float_row(X->scalar_type()));
+    if (!c.ok) return not_handled();
+    const int64_t N = X->size(0), E = X->size(1), topk = ids->size(1), shape[2] = {N, E};
+    here(c, X);
+    here(c, ids);
+    c.require(ids->size(0) == N && E >= 1 && E <= SP24_MOST_EXPERTS && topk >= 1 && topk <= SP24_MOST_CHOICES);
+    if (!c.ok) return not_handled();
+    const float *dw = entries_here<const float>(c, 2, N * topk, at::kFloat), *ds = entries_here<const float>(c, 6, N * E, at::kFloat);
+    const int renormalise = c.truth(4);
+    const float scale = c.real(5);
+    if (!c.ok) return not_handled();
+    const sp24_dtype t = type_of(X->scalar_type(), c.ok);
+    Result d(c, 7, shape, X->scalar_type(), X);
+    here(c, d.t);
+    if (!c.ok) return not_handled();
+    const void* px = X->data_ptr();
+    const int32_t* pi = static_cast<const int32_t*>(ids->data_ptr());
+    void *pd = d.t->data_ptr(), *st = stream();
+    const int64_t ldx = ld(*X), ldd = ld(*d.t);
+    const sp24_status s = without_gil([&] {
+        return sp24_moe_route_backward(px, pi, dw, ds, pd, N, (int)E, (int)topk, softmax ? SP24_SCORE_SOFTMAX : SP24_SCORE_SIGMOID, renormalise, scale, ldx, ldd,
+                                       t, st);
+    });
+    return s == SP24_OK ? d.object() : refused(self, s, "sp24_moe_route_backward");
+}
+
+// (X, dtype, out) -> (codes, scale)
+PyObject* checkpoint_rows(PyObject* self, PyObject* const* args, Py_ssize_t)
+{
+    Call c{args, true};
+    const at::Tensor* X = c.rowmajor(0);
+    const at::ScalarType code = c.dtype(1);
+    if (!c.ok) return not_handled();
+    here(c, X);
+    c.require(is_float_row(X->scalar_type()) && is_code_type(code));
+    const int64_t N = X->size(0), H = X->size(1), shape[2] = {N, H};
+    Result q(c, 2, shape, code, X);
+    here(c, q.t);
+    if (!c.ok) return not_handled();
+    const sp24_dtype t = type_of(X->scalar_type(), c.ok), to = type_of(code, c.ok);
+    at::Tensor scale = make({N, (H + SP24_CHECKPOINT_BLOCK - 1) / SP24_CHECKPOINT_BLOCK}, at::kFloat, *X);
+    const void* px = X->data_ptr();
+    void *pq = q.t->data_ptr(), *st = stream();
+    float* ps = static_cast<float*>(scale.data_ptr());
+    const int64_t ldx = ld(*X), ldq = ld(*q.t);
+    const sp24_status s = without_gil([&] { return sp24_checkpoint_rows(px, pq, ps, N, H, ldx, ldq, t, to, st); });
+    return s == SP24_OK ? tuple(q.object(), wrap(scale)) : refused(self, s, "sp24_checkpoint_rows");
+}
+
+// (checkpoint, out_dtype, act, rows, topk, out)
+PyObject* restore_rows(PyObject* self, PyObject* const* args, Py_ssize_t)
+{
+    Call c{args, true};
+    const Kept k(c, 0);
+    const at::ScalarType out = c.dtype(1);
+    const sp24_act act = activation(c, 2);
+    if (!c.ok) return not_handled();
+    int64_t R = k.N;
+    if (!c.none(3)) {
+        const at::Tensor* rows = c.contiguous(3);
+        if (!c.ok) return not_handled();
+        R = rows->numel();
+    }
+    const int32_t* rows = entries_here<const int32_t>(c, 3, R, at::kInt);
+    const int topk = small(c, 4);
+    c.require(is_float_row(out));
+    const int64_t shape[2] = {R, k.H}, H = k.H, N = k.N, ldk = k.ld_;
+    Result o(c, 5, shape, out, k.codes);
+    here(c, o.t);
+    if (!c.ok) return not_handled();
+    const sp24_dtype code = type_of(k.codes->scalar_type(), c.ok), t = type_of(out, c.ok);
+    const void* pc = k.data();
+    const float* ps = k.scales();
+    void *po = o.t->data_ptr(), *st = stream();
+    const int64_t ldo = ld(*o.t);
+    const sp24_status s = without_gil([&] { return sp24_restore_rows(pc, ps, rows, po, N, R, topk, H, ldk, ldo, act, code, t, st); });
+    return s == SP24_OK ? o.object() : refused(self, s, "sp24_restore_rows");
+}
+
+// (dY, preact, act, offsets, workspace) -> (dZ, dZt, dbias)
+PyObject* linear_backward_checkpoint(PyObject* self, PyObject* const* args, Py_ssize_t)
+{
+    Call c{args, true};
+    const at::Tensor* dY = c.rowmajor(0);
+    const sp24_act act = activation(c, 2);
+    if (!c.ok) return not_handled();
+    here(c, dY);
+    const int64_t N = dY->size(0), M = dY->size(1);
+    const at::ScalarType type = dY->scalar_type();
+    const bool copy = act != SP24_ACT_NONE;
+    const void* pz = nullptr;
+    const float* ps = nullptr;
+    int64_t ldz = 0;
+    sp24_dtype code = SP24_I8;
+    if (copy) {
+        const Kept k(c, 1);
+        c.require(c.ok && k.N == N && k.H == M);
+        if (!c.ok) return not_handled();
+        pz = k.data();
+        ps = k.scales();
+        ldz = k.ld_;
+        code = type_of(k.codes->scalar_type(), c.ok);
+    }
+    const bool grouped = !c.none(3);
+    int64_t experts = 0;
+    const int32_t* po = nullptr;
+    if (grouped) {
+        const at::Tensor* offsets = c.contiguous(3);
+        if (!c.ok) return not_handled();
+        here(c, offsets);
+        experts = offsets->numel() - 1;
+        c.require(offsets->scalar_type() == at::kInt && experts >= 1 && experts <= SP24_MOST_EXPERTS);
+        po = static_cast<const int32_t*>(offsets->data_ptr());
+    }
+    if (!c.ok) return not_handled();
+    const sp24_dtype t = type_of(type, c.ok);
+    Scratch ws(c, 4, sp24_linear_backward_workspace_bytes(M, N, grouped), *dY);
+    if (c.ok && !c.none(4)) here(c, c.tensor(4));
+    if (!c.ok) return not_handled();
+    const int64_t pitch = (N + 7) / 8 * 8;                     // 16-byte rows, which the weights' gradient asks for
+    at::Tensor dZ, dZt = make({M, pitch}, type, *dY), db = grouped ? make({experts, M}, at::kFloat, *dY) : make({M}, at::kFloat, *dY);
+    if (pitch != N) dZt = dZt.narrow(1, 0, N);
+    if (copy) dZ = make({N, M}, type, *dY);
+    const void* pd = dY->data_ptr();
+    void *pdz = copy ? dZ.data_ptr() : nullptr, *pt = dZt.data_ptr(), *st = stream();
+    float* pb = static_cast<float*>(db.data_ptr());
+    const int64_t lddy = ld(*dY);
+    const sp24_status s = without_gil([&] {
+        return sp24_linear_backward_checkpoint(pd, pz, ps, pdz, pt, pb, M, N, lddy, ldz, M, pitch, act, po, (int)experts, code, t, ws.p, ws.bytes, st);
+    });
+    if (s != SP24_OK) return refused(self, s, "sp24_linear_backward_checkpoint");
+    return tuple(copy ? wrap(dZ) : again(args[0]), wrap(dZt), wrap(db));
+}
+
+// (A, checkpoint, out_dtype, out)
+PyObject* gemm_dense_checkpoint(PyObject* self, PyObject* const* args, Py_ssize_t)
+{
+    Call c{args, true};
+    const at::Tensor* A = c.rowmajor(0);
+    const Kept k(c, 1);
+    const at::ScalarType out = c.dtype(2);
+    if (!c.ok) return not_handled();
+    here(c, A);
+    const int64_t M = A->size(0), K = k.N, N = k.H, ldk = k.ld_, shape[2] = {M, N};
+    c.require(A->size(1) == K);
+    const sp24_dtype ti = type_of(A->scalar_type(), c.ok), to = type_of(out, c.ok), code = type_of(k.codes->scalar_type(), c.ok);
+    Result d(c, 3, shape, out, A);
+    here(c, d.t);
+    if (!c.ok) return not_handled();
+    const void *pa = A->data_ptr(), *pc = k.data();
+    const float* ps = k.scales();
+    void *pd = d.t->data_ptr(), *st = stream();
+    const int64_t lda = ld(*A), ldd = ld(*d.t);
+    const sp24_status s = without_gil([&] { return sp24_gemm_dense_checkpoint(pa, pc, ps, pd, M, N, K, lda, ldk, ldd, ti, code, to, st); });
+    return s == SP24_OK ? d.object() : refused(self, s, "sp24_gemm_dense_checkpoint");
+}
+
+// (A, checkpoint, offsets, out_dtype, rows, topk, out): a new result only
+PyObject* gemm_dense_grouped_checkpoint(PyObject* self, PyObject* const* args, Py_ssize_t)
+{
+    Call c{args, true};
+    const at::Tensor *A = c.rowmajor(0), *offsets = c.contiguous(2);
+    const Kept k(c, 1);
+    const at::ScalarType out = c.dtype(3);
+    const int topk = small(c, 5);
+    c.require(c.none(6));
+    if (!c.ok) return not_handled();
+    here(c, A);
+    here(c, offsets);
+    const int64_t experts = offsets->numel() - 1, M = A->size(0), R = A->size(1), N = k.H, tokens = k.N, ldk = k.ld_;
+    c.require(offsets->scalar_type() == at::kInt && experts >= 1 && experts <= SP24_MOST_EXPERTS && (!c.none(4) || tokens == R));
+    const int32_t* rows = entries_here<const int32_t>(c, 4, R, at::kInt);
+    const sp24_dtype ti = type_of(A->scalar_type(), c.ok), to = type_of(out, c.ok), code = c.ok ? type_of(k.codes->scalar_type(), c.ok) : SP24_I8;
+    if (!c.ok) return not_handled();
+    at::Tensor D = make({experts, M, N}, out, *A);
+    const void *pa = A->data_ptr(), *pc = k.data();
+    const float* ps = k.scales();
+    const int32_t* po = static_cast<const int32_t*>(offsets->data_ptr());
+    void *pd = D.data_ptr(), *st = stream();
+    const int64_t lda = ld(*A);
+    const sp24_status s = without_gil([&] {
+        return sp24_gemm_dense_grouped_checkpoint(pa, pc, ps, rows, pd, po, (int)experts, M, N, R, tokens, topk, lda, ldk, N, ti, code, to, st);
+    });
+    return s == SP24_OK ? wrap(D) : refused(self, s, "sp24_gemm_dense_grouped_checkpoint");
+}
+
 } // namespace
 
 PyMethodDef sp24_layer_methods[] = {
@@ -411,4 +693,11 @@ PyMethodDef sp24_layer_methods[] = {
     SP24_METHOD("sp24_moe_gather", moe_gather),
     SP24_METHOD("sp24_moe_combine", moe_combine),
     SP24_METHOD("sp24_moe_combine_backward", moe_combine_backward),
+    SP24_METHOD("sp24_moe_route", moe_route),
+    SP24_METHOD("sp24_moe_route_backward", moe_route_backward),
+    SP24_METHOD("sp24_checkpoint_rows", checkpoint_rows),
+    SP24_METHOD("sp24_restore_rows", restore_rows),
+    SP24_METHOD("sp24_linear_backward_checkpoint", linear_backward_checkpoint),
+    SP24_METHOD("sp24_gemm_dense_checkpoint", gemm_dense_checkpoint),
+    SP24_METHOD("sp24_gemm_dense_grouped_checkpoint", gemm_dense_grouped_checkpoint),
     {nullptr, nullptr, 0, nullptr}};

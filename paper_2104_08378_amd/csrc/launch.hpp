@@ -142,13 +142,14 @@ sp24_status launch_column_sums(const float* partial, int64_t rows, int64_t colum
                                hipStream_t st);
 
 struct LinearGradArgs {
-    const void *dY, *Z;                   // N rows of M values
+    const void *dY, *Z;                   // N rows of M values; Z as codes (zcode) with their scales
+    const float* zscale;
     void *dZ, *dZt;
     float *partial, *dbias;               // partial: a row of M for every `unit` (16 or 64) rows
     const int32_t* offsets;
     int64_t M, N, lddy, ldz, lddz, lddzt;
     int act, experts, unit;
-    sp24_dtype t;
+    sp24_dtype t, zcode;                  // zcode: t, or the 8-bit type
 };
 sp24_status launch_linear_grad(const LinearGradArgs& a, hipStream_t st);
 
@@ -195,6 +196,65 @@ struct CombineGradArgs {
     sp24_dtype t;
 };
 sp24_status launch_moe_combine_grad(const CombineGradArgs& a, hipStream_t st);
+
+struct RouteArgs {
+    const void* logits;
+    const float* bias;                    // null: 0
+    int32_t* ids;
+    float *weights, *scores;              // scores, load: null where not asked for
+    int32_t* load;
+    int64_t N, ldl;
+    int experts, topk, groups, groups_kept, group_best, softmax, renormalise;
+    float scale;
+    sp24_dtype t;
+};
+sp24_status launch_moe_route(const RouteArgs& a, hipStream_t st);
+
+struct RouteGradArgs {
+    const void* logits;
+    const int32_t* ids;
+    const float *dweights, *dscores;      // dscores null: 0
+    void* dlogits;
+    int64_t N, ldl, lddl;
+    int experts, topk, softmax, renormalise;
+    float scale;
+    sp24_dtype t;
+};
+sp24_status launch_moe_route_grad(const RouteGradArgs& a, hipStream_t st);
+
+constexpr int kKeptBlock = SP24_CHECKPOINT_BLOCK;      // values of a row under one scale
+__host__ __device__ inline int64_t kept_blocks(int64_t H) { return (H + kKeptBlock - 1) / kKeptBlock; }
+struct KeepArgs {
+    const void* X;
+    void* codes;
+    float* scale;                         // N x kept_blocks(H)
+    int64_t N, H, ldx, ldc;
+    sp24_dtype t, code;
+};
+sp24_status launch_checkpoint_rows(const KeepArgs& a, hipStream_t st);
+
+struct RestoreArgs {
+    const void* codes;
+    const float* scale;
+    const int32_t* rows;                  // null: row r of the codes
+    void* out;
+    int64_t N, R, H, ldc, ldo;            // N: rows of codes, R of out
+    int topk, act;
+    sp24_dtype code, t;
+};
+sp24_status launch_restore_rows(const RestoreArgs& a, hipStream_t st);
+
+// D = A x what the codes stand for, of all rows or (offsets) segment by segment
+struct KeptMmArgs {
+    const void *A, *codes;
+    const float* scale;
+    const int32_t *rows, *offsets;        // rows null: column k of A meets row k of the codes; offsets null: one segment
+    void* D;
+    int64_t M, N, K, tokens, lda, ldc, ldd;      // K: columns of A; tokens: rows of the codes
+    int topk, experts;
+    sp24_dtype in, code, out;
+};
+sp24_status launch_gemm_kept(const KeptMmArgs& a, hipStream_t st);
 
 struct LinearArgs;                        // linear.hpp
 struct GroupedArgs;

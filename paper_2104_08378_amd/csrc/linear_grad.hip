@@ -8,14 +8,15 @@
 //
 // dZ is rounded to 16 bits, which both of its products read (the matrix instructions' operands): gradients of 4096 x 1024 weights from 4096
 // tokens are off by 0.0023 of their size in bf16, where rounding the results alone leaves 0.0017.  The bias's gradient sums unrounded values.
+#include "kept.hpp"
 #include "launch.hpp"
-#include "rowops.hpp"
 
 namespace sp24 {
 
 constexpr int kGradTile = 64;           // rows of a tile
 
-template <int T, int WIDTH>
+// ZT: what Z is held in, the values' type or codes with a scale for each block of 128
+template <int T, int ZT, int WIDTH>
 __global__ __launch_bounds__(4 * WIDTH) void k_linear_grad(LinearGradArgs a, int tiles_m, unsigned from)
 {
     constexpr int kPitch = WIDTH + 1, CH = WIDTH / 8;
@@ -28,12 +29,19 @@ __global__ __launch_bounds__(4 * WIDTH) void k_linear_grad(LinearGradArgs a, int
     const int64_t m = m0 + c * 8;
     const int have = (int)min(a.M - m, (int64_t)8);
     raw8<T> dy[2] = {}, z[2] = {};
+    uint2v codes[2] = {};
+    float scale[2] = {};
 #pragma unroll
     for (int it = 0; it < 2; ++it) {
         const int64_t n = n0 + it * 32 + tid / CH;
         if (n < a.N && have > 0) {
             dy[it] = load_raw8<T>(a.dY, n * a.lddy + m, have);
-            if (a.act != SP24_ACT_NONE) z[it] = load_raw8<T>(a.Z, n * a.ldz + m, have);
+            if (a.act != SP24_ACT_NONE) {
+                if constexpr (is8<ZT>) {
+                    codes[it] = load_codes8<false>(reinterpret_cast<const uint8_t*>(a.Z) + n * a.ldz + m, have);
+                    scale[it] = a.zscale[n * kept_blocks(a.M) + m / kKeptBlock];
+                } else z[it] = load_raw8<T>(a.Z, n * a.ldz + m, have);
+            }
         }
     }
 #pragma unroll
@@ -42,7 +50,8 @@ __global__ __launch_bounds__(4 * WIDTH) void k_linear_grad(LinearGradArgs a, int
         float v[8], x[8];
         values_of<T>(dy[it], v);
         if (a.act != SP24_ACT_NONE) {
-            values_of<T>(z[it], x);
+            if constexpr (is8<ZT>) kept_values8<ZT>(codes[it], scale[it], x);
+            else values_of<T>(z[it], x);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] *= activation_slope(x[i], a.act);
         }
@@ -84,8 +93,14 @@ static sp24_status run_linear_grad(const LinearGradArgs& a, hipStream_t st)
 {
     const int64_t tiles_m = (a.M + WIDTH - 1) / WIDTH, tiles_n = (a.N + kGradTile - 1) / kGradTile;
     return launch_in_parts(tiles_m * tiles_n, 4 * WIDTH, [&](unsigned from, unsigned grid) {
-        if (a.t == SP24_F16) k_linear_grad<SP24_F16, WIDTH><<<grid, 4 * WIDTH, 0, st>>>(a, (int)tiles_m, from);
-        else k_linear_grad<SP24_BF16, WIDTH><<<grid, 4 * WIDTH, 0, st>>>(a, (int)tiles_m, from);
+        auto run = [&](auto t) {
+            constexpr int T = decltype(t)::value;
+            if (a.zcode == SP24_I8) k_linear_grad<T, SP24_I8, WIDTH><<<grid, 4 * WIDTH, 0, st>>>(a, (int)tiles_m, from);
+            else if (a.zcode == SP24_F8) k_linear_grad<T, SP24_F8, WIDTH><<<grid, 4 * WIDTH, 0, st>>>(a, (int)tiles_m, from);
+            else k_linear_grad<T, T, WIDTH><<<grid, 4 * WIDTH, 0, st>>>(a, (int)tiles_m, from);
+        };
+        if (a.t == SP24_F16) run(std::integral_constant<int, SP24_F16>{});
+        else run(std::integral_constant<int, SP24_BF16>{});
     });
 }
 

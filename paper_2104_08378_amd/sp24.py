@@ -97,10 +97,19 @@ def lib():
         L.sp24_moe_combine_backward.argtypes = [vp] * 7 + [i64, i64, i32, i64, i64, i64, i64, i32, vp]
         L.sp24_linear_grouped.argtypes = [vp] * 5 + [i32] + [i64] * 5 + [vp, vp, vp, i32, vp, i64, i32, i32, i32, vp]
         L.sp24_gemm_dense_grouped.argtypes = [vp] * 4 + [i32] + [i64] * 6 + [i32, i32, vp]
+        L.sp24_moe_route.argtypes = [vp] * 6 + [i64] + [i32] * 7 + [f32, i64, i32, vp]
+        L.sp24_moe_route_backward.argtypes = [vp] * 5 + [i64] + [i32] * 4 + [f32, i64, i64, i32, vp]
+        L.sp24_checkpoint_rows.argtypes = [vp] * 3 + [i64] * 4 + [i32, i32, vp]
+        L.sp24_restore_rows.argtypes = [vp] * 4 + [i64, i64, i32, i64, i64, i64, i32, i32, i32, vp]
+        L.sp24_linear_backward_checkpoint.argtypes = [vp] * 6 + [i64] * 6 + [i32, vp, i32, i32, i32, vp, st, vp]
+        L.sp24_gemm_dense_checkpoint.argtypes = [vp] * 4 + [i64] * 6 + [i32, i32, i32, vp]
+        L.sp24_gemm_dense_grouped_checkpoint.argtypes = [vp] * 6 + [i32] + [i64] * 4 + [i32] + [i64] * 3 + [i32, i32, i32, vp]
         for name in ("sp24_rmsnorm_backward_workspace_bytes", "sp24_linear_backward_workspace_bytes", "sp24_moe_sort_workspace_bytes"):
             getattr(L, name).restype = st
         for name in ("sp24_rmsnorm", "sp24_quantize_rows", "sp24_rmsnorm_backward", "sp24_linear", "sp24_linear_backward", "sp24_moe_sort", "sp24_moe_gather",
-                     "sp24_moe_combine", "sp24_moe_combine_backward", "sp24_linear_grouped", "sp24_gemm_dense_grouped"):
+                     "sp24_moe_combine", "sp24_moe_combine_backward", "sp24_linear_grouped", "sp24_gemm_dense_grouped", "sp24_moe_route", "sp24_moe_route_backward",
+                     "sp24_checkpoint_rows", "sp24_restore_rows", "sp24_linear_backward_checkpoint", "sp24_gemm_dense_checkpoint",
+                     "sp24_gemm_dense_grouped_checkpoint"):
             getattr(L, name).restype = i32
         L.sp24_status_string.argtypes = [i32]
         L.sp24_status_string.restype = ctypes.c_char_p
@@ -899,4 +908,194 @@ def sp24_gemm_dense_grouped(A, B, offsets, out_dtype, out=None):
         raise ValueError("out must be a contiguous tensor [experts, M, N] of out_dtype")
     _check(lib().sp24_gemm_dense_grouped(A.data_ptr(), B.data_ptr(), D.data_ptr(), _vector(offsets, experts + 1, "offsets", torch.int32), experts, M, N, R,
                                          _ld(A), _ld(B), N, _DT[A.dtype], _DT[out_dtype], _stream()), "sp24_gemm_dense_grouped")
+    return D
+
+
+# ---- routing, and rows kept in 8 bits for the backward pass ---------------------------------------------------------
+
+SOFTMAX, SIGMOID = 0, 1
+_SCORE = {"softmax": SOFTMAX, "sigmoid": SIGMOID}
+MOST_CHOICES = 64                  # SP24_MOST_CHOICES of the header
+CHECKPOINT_BLOCK = 128             # SP24_CHECKPOINT_BLOCK
+
+#: What sp24_moe_route returns; None in the place of what was not asked for.
+Route = collections.namedtuple("Route", "ids weights scores load")
+#: Rows kept in 8 bits: codes [N, H] and a scale [N, ceil(H / CHECKPOINT_BLOCK)] for every block of neighbouring values.
+Checkpoint = collections.namedtuple("Checkpoint", "codes scale")
+
+
+def _here(*tensors):
+    """The tensors (None: not there) are on the device whose stream the call goes to."""
+    for t in tensors:
+        if t is not None and _dev(t, "argument").device.index != torch.cuda.current_device():
+            raise ValueError("tensors must be on the current device")
+
+
+def _score(score):
+    if score not in _SCORE:
+        raise ValueError("score must be 'softmax' or 'sigmoid'")
+    return _SCORE[score]
+
+
+def _float_rows(x, name):
+    _rowmajor(x, name)
+    if x.dtype not in (torch.float32, torch.float16, torch.bfloat16):
+        raise ValueError(f"{name} must be float32, float16 or bfloat16")
+    return x.shape
+
+
+def _float_type(t):
+    if t not in (torch.float32, torch.float16, torch.bfloat16):
+        raise ValueError("out_dtype must be float32, float16 or bfloat16")
+    return _DT[t]
+
+
+def _code_type(t):
+    if t not in (torch.int8, torch.float8_e4m3fn):
+        raise ValueError("codes must be int8 or float8_e4m3fn")
+    return _DT[t]
+
+
+def _kept(checkpoint, name="checkpoint"):
+    """(codes, scale, N, H) of a Checkpoint."""
+    codes, scale = checkpoint
+    _rowmajor(codes, f"{name}.codes")
+    _code_type(codes.dtype)
+    N, H = codes.shape
+    _vector(scale, N * -(-H // CHECKPOINT_BLOCK), f"{name}.scale")
+    return codes, scale, N, H
+
+
+def sp24_moe_route(logits, topk, score="softmax", bias=None, groups=1, groups_kept=1, group_best=2, renormalise=True, scale=1.0, want_scores=False,
+                   want_load=False):
+    """The ``topk`` experts of every token and their weights from the router's logits [N, experts]: Route(ids [N, topk] int32, weights [N, topk],
+    scores [N, experts], load [experts] int32).  Scores are ``score`` of the logits; ``bias`` [experts] is added for the choice alone; with ``groups`` of neighbouring
+    experts only those of the ``groups_kept`` groups whose ``group_best`` best experts are the best together.  Where fewer than topk can be chosen (logits
+    of -inf), ids -1, which sp24_moe_sort gives no row."""
+    done = (_host or _load_host()).sp24_moe_route(logits, topk, score, bias, groups, groups_kept, group_best, renormalise, scale, want_scores, want_load)
+    if done is not None:
+        return Route._make(done)
+    N, E = _float_rows(logits, "logits")
+    _here(logits, bias)
+    if not 1 <= topk <= MOST_CHOICES:
+        raise ValueError(f"topk must be 1 .. {MOST_CHOICES}")
+    new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=logits.device)  # noqa: E731
+    ids, weights = new(N, topk, dtype=torch.int32), new(N, topk)
+    scores, load = new(N, E) if want_scores else None, new(E, dtype=torch.int32) if want_load else None
+    _check(lib().sp24_moe_route(logits.data_ptr(), _vector(bias, E, "bias"), ids.data_ptr(), weights.data_ptr(), _ptr(scores), _ptr(load), N, E, topk, groups,
+                                groups_kept, group_best, _score(score), int(bool(renormalise)), float(scale), _ld(logits), _DT[logits.dtype], _stream()),
+           "sp24_moe_route")
+    return Route(ids, weights, scores, load)
+
+
+def sp24_moe_route_backward(logits, ids, dweights, score="softmax", renormalise=True, scale=1.0, dscores=None, out=None):
+    """The gradient of sp24_moe_route's logits from those of the weights [N, topk] and of the scores [N, experts] (None: zero), the choice being held.
+    ``out`` may be the logits."""
+    done = (_host or _load_host()).sp24_moe_route_backward(logits, ids, dweights, score, renormalise, scale, dscores, out)
+    if done is not None:
+        return done
+    N, E = _float_rows(logits, "logits")
+    _here(logits, ids, dweights, dscores, out)
+    if ids.dim() != 2 or ids.shape[0] != N:
+        raise ValueError("ids must be [N, topk]")
+    if dweights is None:
+        raise ValueError("dweights must be given")
+    topk = ids.shape[1]
+    d = _out(out, (N, E), logits.dtype, logits.device)
+    _check(lib().sp24_moe_route_backward(logits.data_ptr(), _vector(ids, N * topk, "ids", torch.int32), _vector(dweights, N * topk, "dweights"),
+                                         _vector(dscores, N * E, "dscores"), d.data_ptr(), N, E, topk, _score(score), int(bool(renormalise)), float(scale),
+                                         _ld(logits), _ld(d), _DT[logits.dtype], _stream()), "sp24_moe_route_backward")
+    return d
+
+
+def sp24_checkpoint_rows(X, dtype=torch.int8, out=None):
+    """Checkpoint(codes, scale): the rows of X kept in 8 bits for the backward pass, a scale for every CHECKPOINT_BLOCK neighbouring values."""
+    done = (_host or _load_host()).sp24_checkpoint_rows(X, dtype, out)
+    if done is not None:
+        return Checkpoint._make(done)
+    N, H = _float_rows(X, "X")
+    _here(X, out)
+    code = _code_type(dtype)
+    codes = _out(out, (N, H), dtype, X.device)
+    scale = torch.empty((N, -(-H // CHECKPOINT_BLOCK)), dtype=torch.float32, device=X.device)
+    _check(lib().sp24_checkpoint_rows(X.data_ptr(), codes.data_ptr(), scale.data_ptr(), N, H, _ld(X), _ld(codes), _DT[X.dtype], code, _stream()),
+           "sp24_checkpoint_rows")
+    return Checkpoint(codes, scale)
+
+
+def sp24_restore_rows(checkpoint, out_dtype, act="none", rows=None, topk=1, out=None):
+    """act of the rows of a Checkpoint, [N, H]; with ``rows`` (of sp24_moe_sort) those of its choices' tokens, [R, H], zeros where there is no choice."""
+    done = (_host or _load_host()).sp24_restore_rows(checkpoint, out_dtype, act, rows, topk, out)
+    if done is not None:
+        return done
+    codes, scale, N, H = _kept(checkpoint)
+    _here(codes, scale, rows, out)
+    R = N if rows is None else rows.numel()
+    O = _out(out, (R, H), out_dtype, codes.device)
+    _check(lib().sp24_restore_rows(codes.data_ptr(), scale.data_ptr(), _vector(rows, R, "rows", torch.int32), O.data_ptr(), N, R, topk, H, _ld(codes), _ld(O),
+                                   _act(act), _DT[codes.dtype], _float_type(out_dtype), _stream()), "sp24_restore_rows")
+    return O
+
+
+def sp24_linear_backward_checkpoint(dY, preact, act, offsets=None, workspace=None):
+    """sp24_linear_backward with ``preact`` a Checkpoint (None without an activation)."""
+    done = (_host or _load_host()).sp24_linear_backward_checkpoint(dY, preact, act, offsets, workspace)
+    if done is not None:
+        return done
+    _rowmajor(dY, "dY")
+    N, M = dY.shape
+    code, codes, scale = _act(act), None, None
+    if code != NO_ACT:
+        codes, scale, n, m = _kept(preact, "preact")
+        if (n, m) != (N, M):
+            raise ValueError("preact must have dY's shape")
+    _here(dY, codes, scale, offsets, workspace)
+    experts = 0 if offsets is None else offsets.numel() - 1
+    dZ = torch.empty((N, M), dtype=dY.dtype, device=dY.device) if code != NO_ACT else None
+    pitch = -(-N // 8) * 8
+    dZt = torch.empty((M, pitch), dtype=dY.dtype, device=dY.device)[:, :N]
+    dbias = torch.empty((M,) if offsets is None else (experts, M), dtype=torch.float32, device=dY.device)
+    ws, ws_bytes = _scratch(workspace, lib().sp24_linear_backward_workspace_bytes(M, N, int(offsets is not None)), dY.device)
+    _check(lib().sp24_linear_backward_checkpoint(dY.data_ptr(), _ptr(codes), _ptr(scale), _ptr(dZ), dZt.data_ptr(), dbias.data_ptr(), M, N, _ld(dY),
+                                                 0 if codes is None else _ld(codes), M, pitch, code, _vector(offsets, experts + 1, "offsets", torch.int32), experts,
+                                                 I8 if codes is None else _DT[codes.dtype], _DT[dY.dtype], _ptr(ws), ws_bytes, _stream()),
+           "sp24_linear_backward_checkpoint")
+    return dY if dZ is None else dZ, dZt, dbias
+
+
+def sp24_gemm_dense_checkpoint(A, checkpoint, out_dtype, out=None):
+    """A [M, K] @ what the rows of a Checkpoint [K, N] stand for: the weights' gradient from rows kept in 8 bits."""
+    done = (_host or _load_host()).sp24_gemm_dense_checkpoint(A, checkpoint, out_dtype, out)
+    if done is not None:
+        return done
+    _rowmajor(A, "A")
+    codes, scale, K, N = _kept(checkpoint)
+    _here(A, codes, scale, out)
+    M = A.shape[0]
+    if A.shape[1] != K:
+        raise ValueError("inner dimensions differ")
+    D = _out(out, (M, N), out_dtype, A.device)
+    _check(lib().sp24_gemm_dense_checkpoint(A.data_ptr(), codes.data_ptr(), scale.data_ptr(), D.data_ptr(), M, N, K, _ld(A), _ld(codes), _ld(D), _DT[A.dtype],
+                                            _DT[codes.dtype], _DT[out_dtype], _stream()), "sp24_gemm_dense_checkpoint")
+    return D
+
+
+def sp24_gemm_dense_grouped_checkpoint(A, checkpoint, offsets, out_dtype, rows=None, topk=1, out=None):
+    """D [experts, M, N]: A [M, R] @ B [R, N] over the rows of every segment, B the rows of a Checkpoint, or (``rows`` [R] of sp24_moe_sort) those of its
+    choices' tokens, zeros where there is no choice."""
+    done = (_host or _load_host()).sp24_gemm_dense_grouped_checkpoint(A, checkpoint, offsets, out_dtype, rows, topk, out)
+    if done is not None:
+        return done
+    _rowmajor(A, "A"), _dev(offsets, "offsets")
+    codes, scale, tokens, N = _kept(checkpoint)
+    _here(A, codes, scale, offsets, rows, out)
+    (M, R), experts = A.shape, offsets.numel() - 1
+    if rows is None and R != tokens:
+        raise ValueError("inner dimensions differ")
+    D = torch.empty((max(experts, 0), M, N), dtype=out_dtype, device=A.device) if out is None else out
+    if out is not None and (tuple(_dev(D, "out").shape) != (experts, M, N) or D.dtype != out_dtype or not D.is_contiguous()):
+        raise ValueError("out must be a contiguous tensor [experts, M, N] of out_dtype")
+    _check(lib().sp24_gemm_dense_grouped_checkpoint(A.data_ptr(), codes.data_ptr(), scale.data_ptr(), _vector(rows, R, "rows", torch.int32), D.data_ptr(),
+                                                    _vector(offsets, experts + 1, "offsets", torch.int32), experts, M, N, R, tokens, topk, _ld(A), _ld(codes), N,
+                                                    _DT[A.dtype], _DT[codes.dtype], _DT[out_dtype], _stream()), "sp24_gemm_dense_grouped_checkpoint")
     return D

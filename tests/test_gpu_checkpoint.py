@@ -1,0 +1,295 @@
+"""Rows kept in 8 bits for the backward pass, and what is computed from them, against 64 bits.
+
+Codes and scales are defined to the bit.  What a code stands for is one product in binary32, 2^-24 of it; an activation's slope stays below 1.13 and costs
+twelve units of 2^-24 of its argument; products round their operand once to the input type (half of its unit of the last place, as the result does)
+and a sum of K products in binary32 is off by less than (K + 4) 2^-24 of the sum of their magnitudes."""
+import pytest
+import torch
+
+import layers_ref as ref
+import routing_ref
+from paper_2104_08378_amd import sp24
+
+pytestmark = pytest.mark.gpu
+
+F16, BF16, F32, I8, F8 = torch.float16, torch.bfloat16, torch.float32, torch.int8, torch.float8_e4m3fn
+INF, NAN = float("inf"), float("nan")
+
+
+def pitched(t, spare, offset):
+    """The same matrix on the GPU in a larger buffer (of NaN; of 0x7F in 8 bits): rows `spare` elements longer, from element `offset` on."""
+    N, H = t.shape
+    narrow = t.element_size() == 1
+    raw = torch.full((offset + N * (H + spare) + 16,), 0x7F if narrow else NAN, dtype=torch.uint8 if narrow else t.dtype, device="cuda")
+    raw[offset:offset + N * (H + spare)].view(N, H + spare)[:, :H].copy_(t.view(torch.uint8) if narrow else t)
+    return raw.view(t.dtype)[offset:offset + N * (H + spare)].view(N, H + spare)[:, :H]
+
+
+def rows_of(g, N, H, dtype):
+    x = torch.randn(N, H, generator=g)
+    x = x * torch.where(torch.rand(H, generator=g) < 0.02, 30.0, 1.0)
+    return x.to(dtype)
+
+
+def kept(x, code, spare=0, offset=0):
+    """A Checkpoint of x on the GPU from the reference's codes."""
+    codes, scale = routing_ref.keep(x, code)
+    return sp24.Checkpoint(pitched(codes.to(code), spare, offset), scale.cuda())
+
+
+SIZES = [(1, 1), (1, 8), (3, 7), (2, 127), (5, 128), (4, 129), (3, 200), (7, 256), (2, 1000), (16, 4096), (9, 4100), (300, 40), (1, 65537), (1000, 136)]
+
+
+@pytest.mark.parametrize("code", [I8, F8])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("N,H", SIZES)
+def test_rows_kept(N, H, dtype, code):
+    g = torch.Generator().manual_seed(N + H)
+    x = rows_of(g, N, H, dtype)
+    codes, scale = routing_ref.keep(x, code)
+    got = sp24.sp24_checkpoint_rows(x.cuda(), code)
+    assert got.codes.dtype == code and torch.equal(got.scale.cpu(), scale)
+    assert torch.equal(got.codes.cpu().float(), codes)
+    out = pitched(torch.zeros(N, H, dtype=torch.uint8).view(code), 5, 3)
+    again = sp24.sp24_checkpoint_rows(pitched(x, 3, 1), code, out=out)
+    assert again.codes.data_ptr() == out.data_ptr() and torch.equal(again.scale, got.scale)
+    assert torch.equal(again.codes.contiguous().view(torch.uint8), got.codes.view(torch.uint8))
+    if N > 1:
+        between = torch.as_strided(out.view(torch.uint8), (N - 1, 5), (H + 5, 1), out.storage_offset() + H)
+        assert bool((between == 0x7F).all()), "written outside the rows"
+
+
+@pytest.mark.parametrize("code", [I8, F8])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_halves_the_ends_of_the_type_and_what_is_not_finite(dtype, code):
+    top = torch.finfo(dtype).max
+    g = torch.Generator().manual_seed(1)
+    x = torch.randn(14, 384, generator=g)
+    x = x.to(dtype).float()
+    # fractions of the largest value that lie in the middle between two codes
+    x[0, :128] = 3.5 * (torch.arange(128) * 2 + 1) / 254.0 if code == I8 else 448.0 * (torch.arange(128) % 16 * 2 + 17) / 32 * 2.0 ** -(torch.arange(128) // 16 * 2)
+    x[0, 127] = 3.5 if code == I8 else 448.0
+    x[1] = x[1] * 0
+    x[2, :128], x[2, 5] = 1e-30, 2.0 ** -120
+    x[3] = top
+    x[3, ::2] = -top / 2
+    x[4, 1], x[5, 200], x[6, 300] = INF, -INF, NAN
+    x[7, :128] = INF
+    x[8] = torch.finfo(dtype).tiny * torch.rand(384, generator=g)
+    x[9] = torch.finfo(dtype).smallest_normal / 8
+    x[9, 4] = top
+    x[10] = -0.0
+    x[11, :128] = torch.linspace(-1, 1, 128)
+    x[12, :128] = top * torch.linspace(-1, 1, 128)
+    x = x.to(dtype)
+    codes, scale = routing_ref.keep(x, code)
+    got = sp24.sp24_checkpoint_rows(x.cuda(), code)
+    assert torch.equal(got.scale.cpu().isnan(), scale.isnan()) and torch.equal(got.scale.cpu().nan_to_num(), scale.nan_to_num())
+    finite = torch.isfinite(scale).repeat_interleave(128, 1)
+    assert torch.equal(torch.where(finite, got.codes.cpu().float(), 0.0), torch.where(finite, codes, 0.0))
+    back = sp24.sp24_restore_rows(got, F32).cpu()
+    assert torch.equal(torch.isnan(back), ~finite)
+
+
+def test_every_quotient_of_a_16_bit_type():
+    """All positive bfloat16 numbers below a power of two, against blocks of many largest values."""
+    every = torch.arange(0, 0x3F80, dtype=torch.int16).view(BF16).float()              # 0 .. 1
+    near = every[every > 1e-4]
+    rows = []
+    for most in (1.0, 1.0078125, 1.25, 1.3359375, 1.5, 1.7578125, 1.9921875):
+        values = torch.nn.functional.pad(near, (0, -near.numel() % 127)).view(-1, 127)
+        rows.append(torch.cat([values, torch.full((values.shape[0], 1), most)], 1))
+    x = torch.cat(rows).to(BF16)
+    for code in (I8, F8):
+        codes, scale = routing_ref.keep(x, code)
+        got = sp24.sp24_checkpoint_rows(x.cuda(), code)
+        assert torch.equal(got.codes.cpu().float(), codes) and torch.equal(got.scale.cpu(), scale)
+
+
+@pytest.mark.parametrize("code", [I8, F8])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("N,H", SIZES)
+def test_rows_had_again(N, H, dtype, code):
+    g = torch.Generator().manual_seed(N + H)
+    c = kept(rows_of(g, N, H, F32), code, 3, 5)
+    x = routing_ref.stands_for(*c)
+    for act in ("none", "relu", "gelu", "silu"):
+        want, err = ref.act(x, act), x.abs() * ((1 if act in ("none", "relu") else 16) * 2.0 ** -24)
+        got = sp24.sp24_restore_rows(c, dtype, act=act)
+        ref.close(got, want, err, act)
+        out = pitched(torch.zeros(N, H, dtype=dtype), 7, 1)
+        assert torch.equal(sp24.sp24_restore_rows(c, dtype, act=act, out=out), got)
+    # the rows of sorted choices; -1 and choices of no token: zeros
+    rows = torch.randint(-2, 3 * N + 2, (2 * N + 5,), generator=g).to(torch.int32)
+    live = (rows >= 0) & (rows < 3 * N)
+    got = sp24.sp24_restore_rows(c, dtype, act="silu", rows=rows.cuda(), topk=3)
+    whole = sp24.sp24_restore_rows(c, dtype, act="silu")
+    want = torch.where(live[:, None], whole.cpu()[torch.where(live, rows // 3, 0).long()], torch.zeros((), dtype=dtype))
+    assert torch.equal(got.cpu(), want)
+
+
+def test_no_rows():
+    for code in (I8, F8):
+        c = sp24.sp24_checkpoint_rows(torch.empty(0, 200, dtype=BF16, device="cuda"), code)
+        assert c.codes.shape == (0, 200) and c.scale.shape == (0, 2)
+        assert sp24.sp24_restore_rows(c, F16).shape == (0, 200)
+        rows = torch.full((16,), -1, dtype=torch.int32, device="cuda")
+        assert bool((sp24.sp24_restore_rows(c, F16, rows=rows, topk=2) == 0).all())
+        A = torch.empty(33, 0, dtype=BF16, device="cuda")
+        out = torch.full((33, 200), NAN, device="cuda")
+        assert bool((sp24.sp24_gemm_dense_checkpoint(A, c, F32, out=out) == 0).all())
+
+
+@pytest.mark.parametrize("code", [I8, F8])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("N,M", [(1, 1), (3, 40), (64, 128), (77, 129), (130, 600), (509, 1000)])
+@pytest.mark.parametrize("act", ["relu", "gelu", "silu", "none"])
+def test_gradient_through_the_activation(N, M, act, dtype, code):
+    g = torch.Generator().manual_seed(N + M)
+    dy, c = torch.randn(N, M, generator=g).to(dtype), kept(2 * torch.randn(N, M, generator=g), code, 5, 3)
+    dz, dzt, db = sp24.sp24_linear_backward_checkpoint(pitched(dy, 3, 1), None if act == "none" else c, act)
+    z = routing_ref.stands_for(*c)
+    want = ref.d(dy) * ref.slope(z, act)
+    err = ref.d(dy).abs() * (14 * 2.0 ** -24) * (1 + z.abs())
+    ref.close(dz, want, err, "dz")
+    assert torch.equal(dzt, dz.t()) and dzt.stride(0) % 8 == 0
+    ref.close(db, want.sum(0), err.sum(0) + want.abs().sum(0) * (N + 4) * 2.0 ** -24, "db")
+    # the same numbers in 32 bits, had again and rounded to the type: nothing in 16 bits comes between here
+    if N % 16 == 0:
+        offsets = torch.tensor([0, 0, N - 16, N], dtype=torch.int32, device="cuda")
+        z2, t2, b2 = sp24.sp24_linear_backward_checkpoint(dy.cuda(), None if act == "none" else c, act, offsets=offsets)
+        assert torch.equal(z2, dz) and torch.equal(t2, dzt)
+        for e, (a, b) in enumerate(((0, 0), (0, N - 16), (N - 16, N))):
+            ref.close(b2[e], want[a:b].sum(0), err[a:b].sum(0) + want[a:b].abs().sum(0) * (N + 4) * 2.0 ** -24, "db")
+
+
+def test_gradient_through_a_large_activation():
+    """The tiles of large matrices."""
+    g = torch.Generator().manual_seed(2)
+    N, M = 2100, 2056
+    dy, c = torch.randn(N, M, generator=g).to(BF16), sp24.sp24_checkpoint_rows(torch.randn(N, M, generator=g).to(BF16).cuda(), I8)
+    dz, dzt, db = sp24.sp24_linear_backward_checkpoint(dy.cuda(), c, "gelu")
+    z = routing_ref.stands_for(*c)
+    want, err = ref.d(dy) * ref.slope(z, "gelu"), ref.d(dy).abs() * (14 * 2.0 ** -24) * (1 + z.abs())
+    ref.close(dz, want, err, "dz")
+    assert torch.equal(dzt, dz.t())
+    ref.close(db, want.sum(0), err.sum(0) + want.abs().sum(0) * (N + 4) * 2.0 ** -24, "db")
+
+
+def rounded(x, dtype):
+    """The product's operand: a value in binary32, rounded to the input type."""
+    return x.float().to(dtype).double()
+
+
+def product(M, N, K, dtype, code, out, spare=0, c_spare=0, c_offset=0):
+    g = torch.Generator().manual_seed(M + 3 * N + 7 * K)
+    a = torch.randn(M, K, generator=g).to(dtype)
+    c = kept(rows_of(g, K, N, F32), code, c_spare, c_offset)
+    pitch = -(-K // 8) * 8 + spare
+    A = torch.full((M, pitch), NAN, dtype=dtype, device="cuda")[:, :K]
+    A.copy_(a)
+    b = rounded(routing_ref.stands_for(*c), dtype)
+    D = sp24.sp24_gemm_dense_checkpoint(A, c, out)
+    ref.close(D, ref.d(a) @ b, (ref.d(a).abs() @ b.abs()) * ((K + 4) * 2.0 ** -24), str((M, N, K, dtype, code, out)))
+    target = torch.full((M, N + 3), NAN, dtype=out, device="cuda")[:, :N]
+    assert torch.equal(sp24.sp24_gemm_dense_checkpoint(A, c, out, out=target), D) and target.data_ptr()
+
+
+@pytest.mark.parametrize("code", [I8, F8])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("K", [1, 2, 7, 8, 9, 15, 16, 31, 63, 64, 65, 128, 130, 200, 509, 1021])
+def test_weights_gradient_from_any_number_of_tokens(K, dtype, code):
+    product(70, 40, K, dtype, code, F32)
+    product(200, 264, K, dtype, code, dtype, spare=16)
+
+
+@pytest.mark.parametrize("code", [I8, F8])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("M,N,c_spare,c_offset", [(1, 1, 0, 0), (33, 17, 3, 1), (70, 45, 0, 0), (64, 64, 1, 5), (300, 1411, 0, 3), (5, 8, 9, 1), (129, 127, 0, 0), (2100, 201, 7, 9),
+                                                  (260, 520, 0, 0), (1540, 1288, 0, 0), (66600, 104, 0, 0)])
+def test_weights_gradient_of_any_size(M, N, c_spare, c_offset, dtype, code):
+    for K in (3, 77, 130):
+        product(M, N, K, dtype, code, F32 if K % 2 else dtype, 0, c_spare, c_offset)
+
+
+@pytest.mark.parametrize("M,N,K", [(4096, 1024, 200), (4096, 2304, 136), (2304, 2048, 72), (1024, 8192, 330), (8192, 640, 77), (512, 512, 2000)])
+def test_weights_gradient_on_every_tile(M, N, K):
+    product(M, N, K, BF16, I8, BF16)
+    product(M, N, K, F16, F8, F32)
+
+
+def test_a_nan_behind_the_last_token_and_a_block_that_is_none():
+    """What a row of A holds behind its columns has no part; a NaN block spoils its own columns and no others."""
+    g = torch.Generator().manual_seed(3)
+    x = torch.randn(37, 300, generator=g)
+    x[5, 140] = INF
+    a = torch.randn(50, 37, generator=g).to(BF16)
+    A = torch.full((50, 48), NAN, dtype=BF16, device="cuda")[:, :37]
+    A.copy_(a)
+    D = sp24.sp24_gemm_dense_checkpoint(A, sp24.sp24_checkpoint_rows(x.cuda(), I8), F32).cpu()
+    assert bool(torch.isnan(D[:, 128:256]).all()) and not bool(torch.isnan(D[:, :128]).any()) and not bool(torch.isnan(D[:, 256:]).any())
+
+
+def segments(g, lengths, spare_rows):
+    offsets = [0]
+    for n in lengths:
+        offsets.append(offsets[-1] + n)
+    return torch.tensor(offsets, dtype=torch.int32, device="cuda"), offsets[-1] + spare_rows
+
+
+@pytest.mark.parametrize("code", [I8, F8])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("M,N,lengths,spare", [(40, 56, [16], 0), (128, 128, [0, 16, 0, 32, 0], 16), (200, 264, [48, 0, 80, 160], 0), (256, 136, [64, 128, 16], 64), (70, 45, [0, 0], 0),
+                                               (300, 520, [336, 16, 0, 208], 32), (1024, 1024, [112, 400], 0)])
+def test_experts_weights_gradient(M, N, lengths, spare, dtype, code):
+    g = torch.Generator().manual_seed(M + N)
+    offsets, R = segments(g, lengths, spare)
+    a = torch.randn(M, R, generator=g).to(dtype)
+    A = torch.full((M, R + 8), NAN, dtype=dtype, device="cuda")[:, :R]
+    A.copy_(a)
+    o = offsets.tolist()
+
+    def check(D, b, out):
+        assert D.shape == (len(lengths), M, N)
+        for e in range(len(lengths)):
+            ae, be = ref.d(a)[:, o[e]:o[e + 1]], b[o[e]:o[e + 1]]
+            ref.close(D[e], ae @ be, (ae.abs() @ be.abs()) * ((R + 4) * 2.0 ** -24), str((M, N, e, out)))
+    # a row kept for every sorted row
+    c = kept(rows_of(g, R, N, F32), code, 3, 1)
+    b = rounded(routing_ref.stands_for(*c), dtype)
+    for out in (F32, dtype):
+        check(sp24.sp24_gemm_dense_grouped_checkpoint(A, c, offsets, out), b, out)
+    # a row kept for every token; some rows without a choice, some of a choice of no token
+    tokens, topk = max(R // 3, 1), 2
+    c = kept(rows_of(g, tokens, N, F32), code)
+    rows = torch.randint(-3, 2 * tokens + 2, (R,), generator=g).to(torch.int32)
+    live = (rows >= 0) & (rows < 2 * tokens)
+    b = rounded(routing_ref.stands_for(*c), dtype)[torch.where(live, rows // 2, 0).long()] * live[:, None]
+    out = torch.full((len(lengths), M, N), NAN, dtype=dtype, device="cuda")
+    check(sp24.sp24_gemm_dense_grouped_checkpoint(A, c, offsets, dtype, rows=rows.cuda(), topk=topk, out=out), b, dtype)
+    check(sp24.sp24_gemm_dense_grouped_checkpoint(A, c, offsets, F32, rows=rows.cuda(), topk=topk), b, F32)
+
+
+def test_rows_of_no_choice_hide_what_is_not_finite():
+    """A row without a choice is zeros whatever the tokens' rows hold; so is A there, by contract."""
+    x = torch.full((4, 128), NAN)
+    c = sp24.sp24_checkpoint_rows(x.cuda(), F8)
+    rows = torch.full((32,), -1, dtype=torch.int32, device="cuda")
+    offsets = torch.tensor([0, 32], dtype=torch.int32, device="cuda")
+    D = sp24.sp24_gemm_dense_grouped_checkpoint(torch.ones(40, 32, dtype=BF16, device="cuda"), c, offsets, F32, rows=rows, topk=2)
+    assert bool((D == 0).all()) and bool((sp24.sp24_restore_rows(c, BF16, rows=rows, topk=2) == 0).all())
+
+
+def test_rows_far_into_the_codes():
+    """Codes past 2^32 bytes from the first."""
+    K, N, pitch = 40, 264, 1 << 27
+    raw = torch.empty(K * pitch, dtype=torch.uint8, device="cuda").view(I8)
+    g = torch.Generator().manual_seed(4)
+    x, a = rows_of(g, K, N, BF16).cuda(), torch.randn(70, K, generator=g).to(BF16).cuda()
+    near = sp24.sp24_checkpoint_rows(x, I8)
+    far = sp24.sp24_checkpoint_rows(x, I8, out=raw.view(K, pitch)[:, :N])
+    assert torch.equal(far.codes, near.codes) and torch.equal(sp24.sp24_restore_rows(far, BF16), sp24.sp24_restore_rows(near, BF16))
+    assert torch.equal(sp24.sp24_gemm_dense_checkpoint(a, far, F32), sp24.sp24_gemm_dense_checkpoint(a, near, F32))
+    dy = torch.randn(K, N, generator=g).to(BF16).cuda()
+    for p, q in zip(sp24.sp24_linear_backward_checkpoint(dy, far, "gelu"), sp24.sp24_linear_backward_checkpoint(dy, near, "gelu")):
+        assert torch.equal(p, q)

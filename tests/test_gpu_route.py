@@ -1,0 +1,236 @@
+"""Routing to experts and its gradient, against 64 bits.
+
+The ids have to be the reference's: both sides compare in binary64.  Weights and scores are rounded once from binary64 values that a few operations of 2^-53
+made (exponentials to an ulp, a sum of up to 1024): (E + 16) 2^-53 of them.  Gradients likewise, of the sum of the magnitudes of their terms."""
+import pytest
+import torch
+
+import layers_ref as ref
+import routing_ref
+from paper_2104_08378_amd import sp24
+
+pytestmark = pytest.mark.gpu
+
+F16, BF16, F32 = torch.float16, torch.bfloat16, torch.float32
+INF, NAN = float("inf"), float("nan")
+
+
+def pitched(t, spare, offset):
+    """The same matrix on the GPU in a buffer of NaN: rows `spare` elements longer, from element `offset` on."""
+    N, E = t.shape
+    raw = torch.full((offset + N * (E + spare) + 8,), NAN, dtype=t.dtype, device="cuda")
+    view = raw[offset:offset + N * (E + spare)].view(N, E + spare)[:, :E]
+    view.copy_(t)
+    return view
+
+
+def check(logits, topk, **how):
+    got = sp24.sp24_moe_route(logits, topk, want_scores=True, want_load=True, **how)
+    bias = how.get("bias")
+    ids, weights, scores, load = routing_ref.route(logits, topk, **dict(how, bias=bias))
+    assert torch.equal(got.ids.cpu().long(), ids.long())
+    assert got.ids.dtype == torch.int32 and torch.equal(got.load.cpu().long(), load.long())
+    tiny = (logits.shape[1] + 16) * 2.0 ** -53
+    ref.close(got.scores, scores, torch.nan_to_num(scores) * tiny, "scores")
+    ref.close(got.weights, weights, torch.nan_to_num(weights.abs()) * tiny * 2, "weights")
+    again = sp24.sp24_moe_route(logits, topk, **how)
+    assert again.scores is None and again.load is None and torch.equal(again.ids, got.ids)
+    assert torch.equal(again.weights.view(torch.int32), got.weights.view(torch.int32))
+    return got
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("N,E,topk", [(1, 1, 1), (1, 2, 2), (3, 8, 2), (33, 7, 3), (17, 9, 4), (40, 16, 16), (5, 17, 1), (9, 32, 8), (31, 33, 6), (70, 64, 4), (6, 65, 8),
+                                      (19, 100, 8), (4, 128, 8), (13, 129, 5), (21, 160, 6), (37, 256, 8), (5, 257, 64), (7, 384, 10), (3, 512, 8), (5, 513, 7), (6, 1000, 64),
+                                      (2, 1024, 32)])
+def test_route(N, E, topk, dtype, score):
+    g = torch.Generator().manual_seed(N * 1000 + E)
+    x = (torch.randn(N, E, generator=g) * 2).to(dtype)
+    b = (0.1 * torch.randn(E, generator=g)).cuda()
+    check(x.cuda(), topk, score=score)
+    check(pitched(x, 3, 1), topk, score=score, bias=b, renormalise=False, scale=2.5)
+    for groups in (2, 4, 8):
+        if E % groups == 0:
+            for kept in {1, groups // 2, groups}:
+                k = min(topk, kept * (E // groups))
+                check(x.cuda(), k, score=score, bias=b, groups=groups, groups_kept=kept, group_best=1 + kept % 2)
+
+
+@pytest.mark.parametrize("E,groups", [(6, 3), (30, 10), (96, 6), (120, 40), (256, 256), (255, 5), (1000, 125), (1024, 512)])
+def test_groups_of_any_size(E, groups):
+    g = torch.Generator().manual_seed(E)
+    x = torch.randn(9, E, generator=g)
+    x[2, ::3] = -INF
+    for kept, best in ((1, 1), (max(groups // 2, 1), 2), (groups, 2)):
+        check(x.cuda(), min(4, kept * (E // groups)), score="sigmoid", groups=groups, groups_kept=kept, group_best=best, bias=(0.3 * torch.randn(E, generator=g)).cuda())
+
+
+@pytest.mark.parametrize("E", [8, 40, 64, 256, 700])
+def test_ties_go_to_the_lower_expert(E):
+    for score in ("softmax", "sigmoid"):
+        got = check(torch.zeros(5, E, device="cuda"), 4, score=score)
+        assert got.ids.tolist() == [[0, 1, 2, 3]] * 5
+    g = torch.Generator().manual_seed(E)
+    x = torch.randint(0, 3, (30, E), generator=g).float()
+    check(x.cuda(), 5)
+    check(x.cuda(), 3, score="sigmoid", groups=4, groups_kept=2)
+    # past 17 the logistic function is 1 in 32 bits, not in 64; past 37 it is in both
+    x = torch.randint(18, 50, (30, E), generator=g).float()
+    check(x.cuda(), 6, score="sigmoid")
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E", [8, 20, 64, 256, 1024])
+def test_masked_infinite_and_nan(E, score):
+    g = torch.Generator().manual_seed(E)
+    x = torch.randn(12, E, generator=g)
+    x[0] = -INF                                       # a row with nothing left
+    x[1, 2:] = -INF                                   # fewer than topk left
+    x[2, ::2] = -INF
+    x[3, 5] = NAN
+    x[4, 1] = INF
+    x[5] = INF
+    x[6] = -3.0e38
+    x[7] = 3.0e38
+    x[8, :] = -INF
+    x[8, 3] = NAN
+    x[9] = torch.where(torch.rand(E, generator=g) < 0.9, -INF, x[9])
+    x[10] = -800.0                                    # scores of 0, or all alike
+    x[11, 4] = NAN
+    x[11, 6] = -INF
+    b = 0.1 * torch.randn(E, generator=g)
+    for renormalise in (True, False):
+        check(x.cuda(), 4, score=score, renormalise=renormalise)
+        check(x.cuda(), 4, score=score, renormalise=renormalise, groups=4, groups_kept=2)
+        c = b.clone()
+        c[1], c[3], c[6], c[7] = -INF, INF, NAN, -5.0
+        check(x.cuda(), 4, score=score, renormalise=renormalise, bias=c.cuda())
+        check(x.cuda(), 2, score=score, renormalise=renormalise, bias=c.cuda(), groups=2, groups_kept=1)
+
+
+def test_many_rows_and_their_load():
+    g = torch.Generator(device="cuda").manual_seed(1)
+    for N, E, topk in ((20011, 8, 2), (5000, 64, 6), (3001, 256, 8)):
+        x = torch.randn(N, E, device="cuda", generator=g)
+        got = sp24.sp24_moe_route(x, topk, want_load=True)
+        want = x.double().softmax(1).sort(dim=1, descending=True, stable=True)
+        assert torch.equal(got.ids.long(), want.indices[:, :topk])
+        assert torch.equal(got.load.long(), torch.bincount(want.indices[:, :topk].reshape(-1), minlength=E))
+        offsets, slots, rows = sp24.sp24_moe_sort(got.ids, E)
+        assert torch.equal((got.load + 15) // 16 * 16, offsets[1:] - offsets[:-1])
+
+
+def test_no_rows():
+    got = sp24.sp24_moe_route(torch.empty(0, 8, device="cuda"), 2, want_scores=True, want_load=True)
+    assert got.ids.shape == (0, 2) and got.scores.shape == (0, 8) and got.load.tolist() == [0] * 8
+    assert sp24.sp24_moe_route_backward(torch.empty(0, 8, device="cuda"), got.ids, got.weights).shape == (0, 8)
+
+
+def gradient(x, ids, dw, ds, score, renormalise, scale, out=None):
+    got = sp24.sp24_moe_route_backward(x, ids, dw, score=score, renormalise=renormalise, scale=scale, dscores=ds, out=out)
+    return got
+
+
+def expected(x, ids, dw, ds, score, renormalise, scale):
+    """(the gradient, the sum of its terms' magnitudes), the formula in 64 bits."""
+    l, ids, dw = ref.d(x), ids.cpu().long(), ref.d(dw)
+    s, E = routing_ref.scores(l, score), l.shape[1]
+    live = (ids >= 0) & (ids < E)
+    at = torch.where(live, ids, 0)
+    h, size = torch.where(live, dw, 0.0), torch.where(live, dw, 0.0).abs()
+    if renormalise:
+        w = torch.where(live, s.gather(1, at), 0.0)
+        W = w.sum(1, keepdim=True)
+        size = torch.where(W > 0, (size + (size * w).sum(1, keepdim=True) / W) / W, 0.0)
+        h = torch.where(W > 0, (h - (h * w).sum(1, keepdim=True) / W) / W, 0.0)
+    g, G = torch.zeros_like(s), torch.zeros_like(s)
+    for j in range(ids.shape[1]):
+        one = torch.zeros_like(s).scatter_(1, at[:, j:j + 1], 1.0) * live[:, j:j + 1]
+        g, G = g + one * scale * h[:, j:j + 1], G + one * abs(scale) * size[:, j:j + 1]
+    if ds is not None:
+        g, G = g + ref.d(ds), G + ref.d(ds).abs()
+    if score == "sigmoid":
+        d, D = s * (1 - s) * g, s * G
+    else:
+        d, D = s * (g - (g * s).sum(1, keepdim=True)), s * (G + (G * s).sum(1, keepdim=True))
+    masked = l == -INF
+    return torch.where(masked, 0.0, d), torch.where(masked, 0.0, D)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("N,E,topk", [(1, 1, 1), (3, 8, 2), (33, 7, 3), (40, 16, 16), (9, 32, 8), (31, 33, 6), (70, 64, 4), (6, 65, 8), (13, 129, 5), (37, 256, 8), (5, 300, 64),
+                                      (3, 512, 8), (6, 1000, 10), (2, 1024, 64)])
+def test_gradient(N, E, topk, dtype, score):
+    g = torch.Generator().manual_seed(N * 1000 + E)
+    x = (torch.randn(N, E, generator=g) * 2).to(dtype)
+    ids = x.float().topk(topk, dim=1).indices.to(torch.int32)
+    if N > 3:
+        ids[1, 0], ids[2] = -1, -1
+        ids[3, -1] = E                                # names nobody
+        x[0, 0] = -INF
+    dw, ds = torch.randn(N, topk, generator=g).cuda(), torch.randn(N, E, generator=g).cuda()
+    for renormalise, d, scale in ((True, None, 1.0), (False, ds, 2.5), (True, ds, 0.5), (False, None, 1.0)):
+        want, size = expected(x, ids, dw, d, score, renormalise, scale)
+        got = gradient(x.cuda(), ids.cuda(), dw, d, score, renormalise, scale)
+        # (a few thousand operations of 2^-53 and the rounding on the way to 32 bits, 2^-24 of the result)
+        ref.close(got, want, size * 4096 * 2.0 ** -53 + want.abs() * 2.0 ** -24, str((N, E, topk, dtype, score, renormalise)))
+        wide = pitched(x, 5, 3)
+        again = gradient(wide, ids.cuda(), dw, d, score, renormalise, scale, out=wide)
+        assert again.data_ptr() == wide.data_ptr() and torch.equal(again, got)
+
+
+def test_gradient_of_a_choice_that_is_there_twice():
+    g = torch.Generator().manual_seed(5)
+    x, ids = torch.randn(7, 12, generator=g), torch.randint(0, 3, (7, 4), generator=g, dtype=torch.int32)
+    dw = torch.randn(7, 4, generator=g)
+    for score in ("softmax", "sigmoid"):
+        want, size = expected(x, ids, dw, None, score, False, 1.0)
+        ref.close(gradient(x.cuda(), ids.cuda(), dw.cuda(), None, score, False, 1.0), want, size * 2.0 ** -40, score)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("renormalise", [True, False])
+def test_gradient_against_differences(score, renormalise):
+    g = torch.Generator().manual_seed(6)
+    x = torch.randn(5, 24, generator=g)
+    ids = sp24.sp24_moe_route(x.cuda(), 4, score=score).ids.cpu()
+    dw, ds = torch.randn(5, 4, generator=g), torch.randn(5, 24, generator=g)
+
+    def value(l):
+        w, s = routing_ref.weights_of(l, ids, score, renormalise, 1.5)
+        return (w * dw.double()).sum() + (s * ds.double()).sum()
+    got = ref.d(gradient(x.cuda(), ids.cuda(), dw.cuda(), ds.cuda(), score, renormalise, 1.5))
+    step = 1e-5
+    for n in range(5):
+        for e in range(24):
+            up, down = x.double(), x.double()
+            up[n, e] += step
+            down[n, e] -= step
+            # central differences: step^2 / 6 of a third derivative (a few hundred at most), 2^-53 of the value over the step, and 2^-24 of the result
+            assert abs(float((value(up) - value(down)) / (2 * step) - got[n, e])) < 1e-8 + 2.0 ** -23 * abs(float(got[n, e]))
+
+
+def test_gradient_of_masked_rows():
+    x = torch.randn(4, 16, generator=torch.Generator().manual_seed(7))
+    x[0] = -INF
+    x[1, 3:] = -INF
+    x[2] = -800.0
+    for score in ("softmax", "sigmoid"):
+        r = sp24.sp24_moe_route(x.cuda(), 4, score=score)
+        got = sp24.sp24_moe_route_backward(x.cuda(), r.ids, torch.ones(4, 4, device="cuda"), score=score, dscores=torch.ones(4, 16, device="cuda"))
+        assert bool(torch.isfinite(got).all()) and bool((got[0] == 0).all()) and bool((got[1, 3:] == 0).all())
+
+
+def test_rows_far_into_a_pitched_matrix():
+    """Logits past 2^32 bytes from the first."""
+    N, E, pitch = 3000, 64, 1 << 20
+    raw = torch.empty(N * pitch, dtype=F16, device="cuda")
+    x = raw.view(N, pitch)[:, :E]
+    x.copy_(torch.randn(N, E, generator=torch.Generator().manual_seed(8)))
+    got, want = sp24.sp24_moe_route(x, 4), sp24.sp24_moe_route(x.contiguous(), 4)
+    assert torch.equal(got.ids, want.ids) and torch.equal(got.weights, want.weights)
+    dw = torch.randn(N, 4, device="cuda")
+    d = sp24.sp24_moe_route_backward(x.contiguous(), got.ids, dw)
+    assert torch.equal(sp24.sp24_moe_route_backward(x, got.ids, dw, out=x), d)

@@ -1,0 +1,93 @@
+"""Host-only checks of routing and of rows kept in 8 bits: every refusal comes before a device is touched (the addresses are made up)."""
+import ctypes
+
+import pytest
+
+from paper_2104_08378_amd import sp24
+
+OK, NULL, SHAPE, ALIGN, DTYPE = 0, 1, 2, 3, 4
+STEP = 0x10000000
+A, B, C, D, E, F, G = (STEP * i for i in range(1, 8))          # fake, aligned, far apart
+f = ctypes.c_float
+NAN, INF = float("nan"), float("inf")
+
+
+def route(l=A, b=B, ids=C, w=D, s=E, load=F, N=8, n=64, k=4, groups=1, kept=1, best=2, score=0, renorm=1, scale=1.0, ldl=64, t=sp24.F32):
+    return sp24.lib().sp24_moe_route(l, b, ids, w, s, load, N, n, k, groups, kept, best, score, renorm, f(scale), ldl, t, None)
+
+
+@pytest.mark.parametrize("bad,want", [
+    (dict(l=0), NULL), (dict(ids=0), NULL), (dict(w=0), NULL), (dict(l=A + 2), ALIGN), (dict(b=B + 1), ALIGN), (dict(ids=C + 2), ALIGN), (dict(w=D + 3), ALIGN),
+    (dict(s=E + 2), ALIGN), (dict(load=F + 1), ALIGN), (dict(ldl=63), SHAPE), (dict(N=-1), SHAPE), (dict(n=0), SHAPE), (dict(n=1025, ldl=2000), SHAPE),
+    (dict(k=0), SHAPE), (dict(k=65), SHAPE), (dict(n=3, k=4), SHAPE), (dict(groups=0), SHAPE), (dict(groups=5), SHAPE), (dict(groups=128), SHAPE), (dict(groups=4, kept=0), SHAPE),
+    (dict(groups=4, kept=5), SHAPE), (dict(groups=32, kept=1), SHAPE), (dict(best=0), SHAPE), (dict(best=3), SHAPE), (dict(scale=NAN), SHAPE), (dict(scale=INF), SHAPE),
+    (dict(score=2), DTYPE), (dict(t=sp24.I8), DTYPE), (dict(t=sp24.I32), DTYPE), (dict(ids=A), SHAPE), (dict(w=A + 64), SHAPE), (dict(s=A), SHAPE), (dict(load=B), SHAPE),
+    (dict(ids=D), SHAPE), (dict(w=E), SHAPE), (dict(s=F), SHAPE), (dict(load=C + 16), SHAPE), (dict(N=0, load=0, l=0, ids=0, w=0), OK)])
+def test_route(bad, want):
+    assert route(**bad) == want
+
+
+def back(l=A, ids=B, dw=C, ds=D, out=E, N=8, n=64, k=4, score=0, renorm=1, scale=1.0, ldl=64, ldo=64, t=sp24.F32):
+    return sp24.lib().sp24_moe_route_backward(l, ids, dw, ds, out, N, n, k, score, renorm, f(scale), ldl, ldo, t, None)
+
+
+@pytest.mark.parametrize("bad,want", [
+    (dict(l=0), NULL), (dict(ids=0), NULL), (dict(dw=0), NULL), (dict(out=0), NULL), (dict(l=A + 1), ALIGN), (dict(ds=D + 2), ALIGN), (dict(out=E + 2), ALIGN), (dict(ldl=60), SHAPE),
+    (dict(ldo=60), SHAPE), (dict(n=0), SHAPE), (dict(n=1025, ldl=2000, ldo=2000), SHAPE), (dict(k=0), SHAPE), (dict(k=65), SHAPE), (dict(scale=INF), SHAPE), (dict(score=-1), DTYPE),
+    (dict(t=sp24.F8), DTYPE), (dict(out=A + 4), SHAPE), (dict(out=A, ldo=72), SHAPE), (dict(out=B), SHAPE), (dict(out=C), SHAPE), (dict(out=D), SHAPE), (dict(N=0, l=0), OK)])
+def test_route_backward(bad, want):
+    assert back(**bad) == want
+
+
+def keep(X=A, c=B, s=C, N=8, H=200, ldx=200, ldc=200, t=sp24.BF16, code=sp24.I8):
+    return sp24.lib().sp24_checkpoint_rows(X, c, s, N, H, ldx, ldc, t, code, None)
+
+
+def restore(c=A, s=B, rows=0, out=C, N=8, R=8, k=1, H=200, ldc=200, ldo=200, act=0, code=sp24.F8, t=sp24.F16):
+    return sp24.lib().sp24_restore_rows(c, s, rows, out, N, R, k, H, ldc, ldo, act, code, t, None)
+
+
+@pytest.mark.parametrize("bad,want", [
+    (dict(X=0), NULL), (dict(c=0), NULL), (dict(s=0), NULL), (dict(X=A + 1), ALIGN), (dict(s=C + 2), ALIGN), (dict(ldx=199), SHAPE), (dict(ldc=199), SHAPE), (dict(H=0), SHAPE),
+    (dict(N=-1), SHAPE), (dict(N=1 << 30, H=1 << 20, ldx=1 << 20, ldc=1 << 20), SHAPE), (dict(t=sp24.I8), DTYPE), (dict(code=sp24.F32), DTYPE), (dict(c=A), SHAPE), (dict(s=A + 64), SHAPE),
+    (dict(s=B + 64), SHAPE), (dict(N=0, X=0), OK)])
+def test_keep(bad, want):
+    assert keep(**bad) == want
+
+
+@pytest.mark.parametrize("bad,want", [
+    (dict(c=0), NULL), (dict(s=0), NULL), (dict(out=0), NULL), (dict(s=B + 2), ALIGN), (dict(out=C + 1), ALIGN), (dict(rows=D + 2), ALIGN), (dict(R=9), SHAPE), (dict(ldc=100), SHAPE),
+    (dict(ldo=100), SHAPE), (dict(k=0), SHAPE), (dict(H=0), SHAPE), (dict(act=4), DTYPE), (dict(code=sp24.F16), DTYPE), (dict(t=sp24.I32), DTYPE), (dict(out=A), SHAPE), (dict(out=B), SHAPE),
+    (dict(out=D, rows=D, R=4), SHAPE), (dict(N=0, R=0), OK), (dict(R=0, rows=D), OK)])
+def test_restore(bad, want):
+    assert restore(**bad) == want
+
+
+def test_linear_backward():
+    L = sp24.lib()
+    need = L.sp24_linear_backward_workspace_bytes(64, 32, 1)
+
+    def grad(dY=A, Z=B, zs=C, dZ=D, dZt=E, db=F, M=64, N=32, ld=64, ldz=64, ldt=32, act=2, of=G, n=4, code=sp24.I8, t=sp24.F16, ws=8 * STEP, bytes=need):
+        return L.sp24_linear_backward_checkpoint(dY, Z, zs, dZ, dZt, db, M, N, ld, ldz, 64, ldt, act, of, n, code, t, ws, bytes, None)
+    assert grad(dY=0) == NULL and grad(Z=0) == NULL and grad(zs=0) == NULL and grad(ws=0) == NULL and grad(bytes=need - 4) == SHAPE and grad(N=24, ldt=24) == SHAPE
+    assert grad(zs=C + 2) == ALIGN and grad(ldz=63) == SHAPE and grad(code=sp24.F16) == DTYPE and grad(t=sp24.F32) == DTYPE and grad(act=5) == DTYPE
+    assert grad(dZ=B) == SHAPE and grad(dZ=C) == SHAPE and grad(dZt=B + 64) == SHAPE and grad(db=C) == SHAPE and grad(ws=C) == SHAPE and grad(dZ=A + 2) == SHAPE
+    assert grad(n=0) == SHAPE and grad(M=0) == OK
+
+
+def test_products():
+    L = sp24.lib()
+
+    def plain(a=A, c=B, s=C, d=D, M=64, N=64, K=37, lda=40, ldc=64, ldd=64, i=sp24.BF16, code=sp24.I8, o=sp24.F32):
+        return L.sp24_gemm_dense_checkpoint(a, c, s, d, M, N, K, lda, ldc, ldd, i, code, o, None)
+    assert plain(a=0) == NULL and plain(c=0) == NULL and plain(s=0) == NULL and plain(d=0) == NULL and plain(a=A + 8) == ALIGN and plain(lda=41) == ALIGN and plain(lda=32) == SHAPE
+    assert plain(ldc=63) == SHAPE and plain(ldd=63) == SHAPE and plain(s=C + 2) == ALIGN and plain(d=D + 2) == ALIGN and plain(K=-1) == SHAPE and plain(M=-1) == SHAPE
+    assert plain(lda=1 << 23) == SHAPE and plain(i=sp24.I8) == DTYPE and plain(i=sp24.F32) == DTYPE and plain(code=sp24.BF16) == DTYPE and plain(o=sp24.F16) == DTYPE
+    assert plain(d=A) == SHAPE and plain(d=B) == SHAPE and plain(d=C) == SHAPE and plain(M=0) == OK and plain(N=0) == OK
+
+    def grouped(a=A, c=B, s=C, rows=D, d=E, of=F, n=4, M=64, N=60, R=32, tokens=20, k=2, lda=32, ldc=64, ldd=64, i=sp24.BF16, code=sp24.F8, o=sp24.F32):
+        return L.sp24_gemm_dense_grouped_checkpoint(a, c, s, rows, d, of, n, M, N, R, tokens, k, lda, ldc, ldd, i, code, o, None)
+    assert grouped(a=0) == NULL and grouped(c=0) == NULL and grouped(s=0) == NULL and grouped(d=0) == NULL and grouped(of=0) == NULL and grouped(of=F + 2) == ALIGN
+    assert grouped(rows=0) == SHAPE and grouped(rows=D + 1) == ALIGN and grouped(R=24) == SHAPE and grouped(n=0) == SHAPE and grouped(n=1025) == SHAPE and grouped(k=0) == SHAPE
+    assert grouped(tokens=-1) == SHAPE and grouped(lda=24) == SHAPE and grouped(d=D) == SHAPE and grouped(d=F) == SHAPE and grouped(d=B) == SHAPE and grouped(i=sp24.F8) == DTYPE
+    assert grouped(M=0) == OK
