@@ -6,6 +6,8 @@
 //
 // All in binary64: of 10^5 tokens' experts some pairs' scores are within a rounding of binary32 of each other, and which one is chosen must
 // not hang on the order of a sum.
+#include <algorithm>
+
 #include "launch.hpp"
 #include "rowops.hpp"
 
@@ -23,6 +25,20 @@ __device__ __forceinline__ double dpp_of(double v)
     const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), CTRL, 0xF, 0xF, true);
     return __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
 }
+// OP of both sixteens of every 32 lanes, or (WAVE) of both halves of the wavefront, in all of them: a register swapped with a copy of itself leaves the
+// lower one in both places of the one and the upper one in both of the other
+template <bool WAVE, class OP>
+__device__ __forceinline__ double over_halves(double v, OP op)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)b, hi = (uint32_t)(b >> 32);
+    auto swapped = [](uint32_t x) {
+        if constexpr (WAVE) return __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        else return __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    };
+    const auto l = swapped(lo), h = swapped(hi);
+    return op(__builtin_bit_cast(double, ((uint64_t)h[0] << 32) | l[0]), __builtin_bit_cast(double, ((uint64_t)h[1] << 32) | l[1]));
+}
 // OP over the L lanes of a row, the same in all of them and in the same order always
 template <int L, class OP>
 __device__ __forceinline__ double over_row(double v, OP op)
@@ -31,23 +47,72 @@ __device__ __forceinline__ double over_row(double v, OP op)
     if constexpr (L >= 4) v = op(v, dpp_of<0x4E>(v));            // quad_perm [2,3,0,1]
     if constexpr (L >= 8) v = op(v, dpp_of<0x141>(v));           // the other half of eight lanes, mirrored
     if constexpr (L >= 16) v = op(v, dpp_of<0x140>(v));          // the other half of sixteen
-    if constexpr (L >= 32) v = op(v, __shfl_xor(v, 16));
-    if constexpr (L >= 64) v = op(v, __shfl_xor(v, 32));
+    if constexpr (L >= 32) v = over_halves<false>(v, op);
+    if constexpr (L >= 64) v = over_halves<true>(v, op);
     return v;
 }
 struct larger_of { __device__ __forceinline__ double operator()(double a, double b) const { return __builtin_fmax(a, b); } };
 struct sum_of { __device__ __forceinline__ double operator()(double a, double b) const { return a + b; } };
 
-__device__ __forceinline__ float logit_of(const void* p, int64_t i, sp24_dtype t)
+// COUNT neighbouring values from element i on, the first `have` of them (the others: `otherwise`); 16 bytes at a time where there are that many
+template <int T, int COUNT>
+__device__ __forceinline__ void load_run(const void* p, int64_t i, int have, float otherwise, float (&v)[COUNT])
 {
-    return t == SP24_F32 ? load_value<SP24_F32>(p, i) : t == SP24_BF16 ? load_value<SP24_BF16>(p, i) : load_value<SP24_F16>(p, i);
+    constexpr int kAtOnce = T == SP24_F32 ? 4 : 8;
+    if (COUNT % kAtOnce == 0 && have >= COUNT) {
+        const uint8_t* const at = reinterpret_cast<const uint8_t*>(p) + i * value_size<T>();
+#pragma unroll
+        for (int k = 0; k < COUNT / kAtOnce; ++k) {
+            const uint4v q = load_from<uint4v>(at + k * 16);
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) {
+                if constexpr (T == SP24_F32) v[k * kAtOnce + j] = __uint_as_float(q[j]);
+                else v[k * kAtOnce + j] = value_of<T>((q[j / 2] >> (16 * (j & 1))) & 0xFFFFu);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < COUNT; ++k) v[k] = k < have ? load_value<T>(p, i + k) : otherwise;
+    }
+}
+template <int COUNT>
+__device__ __forceinline__ void load_logits(const void* p, int64_t i, int have, sp24_dtype t, float (&v)[COUNT])
+{
+    if (t == SP24_F32) load_run<SP24_F32>(p, i, have, -__builtin_inff(), v);
+    else if (t == SP24_BF16) load_run<SP24_BF16>(p, i, have, -__builtin_inff(), v);
+    else load_run<SP24_F16>(p, i, have, -__builtin_inff(), v);
+}
+
+// COUNT neighbouring results from element i on, the first `have` of them, each rounded to T
+template <int T, int COUNT>
+__device__ __forceinline__ void store_run(void* p, int64_t i, int have, const float (&v)[COUNT])
+{
+    constexpr int kAtOnce = T == SP24_F32 ? 4 : 8;
+    if (COUNT % kAtOnce == 0 && have >= COUNT) {
+        uint8_t* const at = reinterpret_cast<uint8_t*>(p) + i * value_size<T>();
+#pragma unroll
+        for (int k = 0; k < COUNT / kAtOnce; ++k) {
+            uint4v q;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (T == SP24_F32) q[j] = __float_as_uint(v[k * kAtOnce + j]);
+                else q[j] = pack_out16<T>(v[k * kAtOnce + 2 * j], v[k * kAtOnce + 2 * j + 1]);
+            }
+            store_to(at + k * 16, q);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < COUNT; ++k)
+            if (k < have) store_out<T>(p, i + k, v[k]);
+    }
 }
 
 constexpr double kNever = -__builtin_inf();
 
-// The scores of a row's experts, 0 for those whose logit is -inf.  A NaN (or, softmax, +inf) makes NaN of what it takes part in.
+// The scores of a row's experts, 0 for those whose logit is -inf, and (rest) 1 - s of a logistic one without the difference.  A NaN (or, softmax,
+// +inf) makes NaN of what it takes part in.  Exponents are 0 and less.
 template <int L, int V>
-__device__ __forceinline__ void scores_of_row(const float (&x)[V], bool softmax, double (&s)[V])
+__device__ __forceinline__ void scores_of_row(const float (&x)[V], bool softmax, double (&s)[V], double* rest = nullptr)
 {
     if (softmax) {
         float most = -__builtin_inff();
@@ -60,64 +125,124 @@ __device__ __forceinline__ void scores_of_row(const float (&x)[V], bool softmax,
             s[i] = x[i] == -__builtin_inff() ? 0.0 : exp((double)x[i] - top);
             sum += s[i];
         }
-        sum = over_row<L>(sum, sum_of{});
+        const double part = 1.0 / over_row<L>(sum, sum_of{});
 #pragma unroll
-        for (int i = 0; i < V; ++i) s[i] = x[i] == -__builtin_inff() ? 0.0 : s[i] / sum;
+        for (int i = 0; i < V; ++i) s[i] = x[i] == -__builtin_inff() ? 0.0 : s[i] * part;
     } else {
 #pragma unroll
-        for (int i = 0; i < V; ++i) s[i] = x[i] == -__builtin_inff() ? 0.0 : 1.0 / (1.0 + exp(-(double)x[i]));
+        for (int i = 0; i < V; ++i) {
+            // 1 / (1 + t) for x >= 0 and t / (1 + t) below, t = e^-|x|; the chip's reciprocal with two steps of Newton's: 1 + t is 1 to 2
+            const double t = exp(-__builtin_fabs((double)x[i])), d = 1.0 + t;
+            double q = __builtin_amdgcn_rcp(d);
+            q = __builtin_fma(__builtin_fma(-d, q, 1.0), q, q);
+            q = __builtin_fma(__builtin_fma(-d, q, 1.0), q, q);
+            s[i] = x[i] < 0.0f ? t * q : q;                      // (0 at -inf)
+            if (rest) rest[i] = x[i] < 0.0f ? q : t * q;
+        }
     }
 }
 
-template <int L, int V, bool GROUPS>
+// lane `from` of the row's L lanes, to all of them
+template <int L>
+__device__ __forceinline__ double row_lane(double v, int from)
+{
+    return __shfl(v, from, L);
+}
+
+// Where expert e's value lies in a row's image in LDS: first experts of all lanes, then second ones, so that the lanes' writes are neighbours
+template <int L, int V>
+__device__ __forceinline__ int image_place(int e)
+{
+    return e % V * L + e / V;
+}
+
+// How experts are grouped: not; runs of 2^n lanes that hold whole groups; any other way
+enum { kNoGroups, kLaneGroups, kAnyGroups };
+
+template <int L, int V, int GROUPS>
 __global__ __launch_bounds__(kRouteThreads) void k_route(RouteArgs a, unsigned from)
 {
     constexpr int kRows = kRouteThreads / L, kMost = L * V, kPicks = kMost < SP24_MOST_CHOICES ? kMost : SP24_MOST_CHOICES;
-    __shared__ double picked_s[kRows][kPicks];
-    __shared__ int picked_e[kRows][kPicks];
-    __shared__ double keys[GROUPS ? kRows : 1][GROUPS ? kMost : 1];
-    __shared__ double values[GROUPS ? kRows : 1][GROUPS ? kMost : 1];      // of the groups; then whether they stay
+    constexpr bool ANY = GROUPS == kAnyGroups;
+    __shared__ double scores[kRows][kMost];
+    __shared__ int picked[kRows][kPicks];
+    __shared__ double keys[ANY ? kRows : 1][ANY ? kMost : 1];
+    __shared__ double values[ANY ? kRows : 1][ANY ? kMost : 1];            // of the groups
     const int l = threadIdx.x % L, r = threadIdx.x / L, E = a.experts;
     const int64_t row = ((int64_t)from + blockIdx.x) * kRows + r;
     const bool live = row < a.N;
+    if (a.load && from + blockIdx.x == 0) {                      // counted by the launch behind this one
+        for (int e = threadIdx.x; e < E; e += kRouteThreads) a.load[e] = 0;
+    }
     float x[V];
     double s[V], key[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) x[i] = live && l * V + i < E ? logit_of(a.logits, row * a.ldl + l * V + i, a.t) : -__builtin_inff();
+    const int have = min(max(E - l * V, 0), V);                  // of the lane's experts
+    load_logits(a.logits, row * a.ldl + l * V, live ? have : 0, a.t, x);
+    float bias[V] = {};
+    if (a.bias) load_run<SP24_F32>(a.bias, l * V, have, 0.0f, bias);
     scores_of_row<L>(x, a.softmax, s);
     // What is compared: a NaN is the largest, +inf (of a bias) the next; an expert that cannot be chosen is -inf.
+    float rounded[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        const int e = l * V + i;
-        const double c = s[i] + (a.bias && e < E ? (double)a.bias[e] : 0.0);
+        const double c = s[i] + (double)bias[i];
         key[i] = x[i] == -__builtin_inff() ? kNever : c != c ? __builtin_inf() : __builtin_fmin(c, 1e300);
-        if (a.scores && live && e < E) a.scores[row * E + e] = (float)s[i];
+        scores[r][i * L + l] = s[i];
+        rounded[i] = (float)s[i];
     }
-    if constexpr (GROUPS) {
+    if (a.scores && live) store_run<SP24_F32>(a.scores, row * E + l * V, have, rounded);
+    if constexpr (GROUPS == kLaneGroups) {
+        // the two largest of the lane, then of the lanes of its group
+        double first = key[0], second = kNever;
+#pragma unroll
+        for (int i = 1; i < V; ++i) {
+            second = __builtin_fmax(second, __builtin_fmin(first, key[i]));
+            first = __builtin_fmax(first, key[i]);
+        }
+        const int lanes = E / a.groups / V;
+        for (int d = 1; d < lanes; d *= 2) {
+            const double other = __shfl_xor(first, d), next = __shfl_xor(second, d);
+            second = __builtin_fmax(__builtin_fmin(first, other), __builtin_fmax(second, next));
+            first = __builtin_fmax(first, other);
+        }
+        const double value = a.group_best == 1 || second == kNever ? first : first + second;
+        // the group stays if fewer than groups_kept are ahead of it
+        const int mine = l / lanes;
+        int ahead = 0;
+        for (int h = 0; h < a.groups; ++h) {
+            const double v = row_lane<L>(value, h * lanes);
+            ahead += v > value || (v == value && h < mine);
+        }
+        if (ahead >= a.groups_kept) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) key[i] = kNever;
+        }
+    }
+    if constexpr (ANY) {
         const int size = E / a.groups;
 #pragma unroll
-        for (int i = 0; i < V; ++i) keys[r][l * V + i] = key[i];
+        for (int i = 0; i < V; ++i) keys[r][i * L + l] = key[i];
         __syncthreads();
         for (int g = l; g < a.groups; g += L) {
             double first = kNever, second = kNever;
             for (int i = 0; i < size; ++i) {
-                const double k = keys[r][g * size + i];
+                const double k = keys[r][image_place<L, V>(g * size + i)];
                 second = __builtin_fmax(second, __builtin_fmin(first, k));
                 first = __builtin_fmax(first, k);
             }
             values[r][g] = a.group_best == 1 || second == kNever ? first : first + second;
         }
         __syncthreads();
-        // a group stays if fewer than groups_kept are ahead of it
-        for (int i = 0; i < V; ++i) {
-            const int g = l * V + i < E ? (l * V + i) / size : 0;
+        for (int g = l; g < a.groups; g += L) {
             const double mine = values[r][g];
             int ahead = 0;
             for (int h = 0; h < a.groups; ++h) ahead += values[r][h] > mine || (values[r][h] == mine && h < g);
-            if (ahead >= a.groups_kept) keys[r][l * V + i] = kNever;
+            if (ahead >= a.groups_kept)
+                for (int i = 0; i < size; ++i) keys[r][image_place<L, V>(g * size + i)] = kNever;
         }
+        __syncthreads();
 #pragma unroll
-        for (int i = 0; i < V; ++i) key[i] = keys[r][l * V + i];
+        for (int i = 0; i < V; ++i) key[i] = keys[r][i * L + l];
     }
     for (int j = 0; j < a.topk; ++j) {
         double best = key[0];
@@ -125,38 +250,51 @@ __global__ __launch_bounds__(kRouteThreads) void k_route(RouteArgs a, unsigned f
         for (int i = 1; i < V; ++i) best = __builtin_fmax(best, key[i]);
         const double most = over_row<L>(best, larger_of{});
         const uint64_t have = __ballot(best == most) >> ((threadIdx.x & 63) / L * L);
-        const bool none = most == kNever;
         if (l == __builtin_ctzll(have)) {                        // the lowest lane that has it, and there the lowest expert
-            int at = -1;
-            double score = 0.0;
+            int at = 0;
 #pragma unroll
-            for (int i = V - 1; i >= 0; --i)
-                if (key[i] == most) {
-                    at = i;
-                    score = s[i];
-                }
+            for (int i = V - 1; i >= 0; --i) at = key[i] == most ? i : at;
 #pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (i == at) key[i] = kNever;
-            picked_e[r][j] = none ? -1 : l * V + at;
-            picked_s[r][j] = none ? 0.0 : score;
+            for (int i = 0; i < V; ++i) key[i] = i == at ? kNever : key[i];
+            picked[r][j] = most == kNever ? -1 : l * V + at;
         }
     }
     __syncthreads();
     double sum = 0.0;
-    for (int j = l; j < a.topk; j += L) sum += picked_s[r][j];
+    for (int j = l; j < a.topk; j += L) {
+        const int e = picked[r][j];
+        sum += e < 0 ? 0.0 : scores[r][image_place<L, V>(e)];
+    }
     sum = over_row<L>(sum, sum_of{});
     if (!live) return;
     for (int j = l; j < a.topk; j += L) {
-        const int e = picked_e[r][j];
-        double w = picked_s[r][j];
-        if (a.renormalise && e >= 0) w = sum == 0.0 ? 0.0 : w / sum;
+        const int e = picked[r][j];
+        double w = e < 0 ? 0.0 : scores[r][image_place<L, V>(e)];
+        if (a.renormalise) w = sum == 0.0 || e < 0 ? 0.0 : w / sum;
         a.ids[row * a.topk + j] = e;
-        a.weights[row * a.topk + j] = e < 0 ? 0.0f : (float)(w * (double)a.scale);
-        if (a.load && e >= 0) atomicAdd(a.load + e, 1);
+        a.weights[row * a.topk + j] = (float)(w * (double)a.scale);
     }
 }
 
+// How many choices are each expert's: whole numbers, whose sums do not hang on their order.
+constexpr int kLoadThreads = 1024, kLoadChoices = 4096;          // of a workgroup
+__global__ __launch_bounds__(kLoadThreads) void k_route_load(const int32_t* ids, int32_t* load, int64_t choices, int experts)
+{
+    __shared__ int count[SP24_MOST_EXPERTS];
+    for (int e = threadIdx.x; e < experts; e += kLoadThreads) count[e] = 0;
+    __syncthreads();
+    for (int64_t first = (int64_t)blockIdx.x * kLoadChoices; first < choices; first += (int64_t)gridDim.x * kLoadChoices) {
+#pragma unroll
+        for (int u = 0; u < kLoadChoices / kLoadThreads; ++u) {
+            const int64_t i = first + u * kLoadThreads + threadIdx.x;
+            const int e = i < choices ? ids[i] : -1;
+            if (e >= 0) atomicAdd(&count[e], 1);
+        }
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < experts; e += kLoadThreads)
+        if (count[e] != 0) atomicAdd(load + e, count[e]);
+}
 __global__ void k_no_load(int32_t* load, int experts)
 {
     for (int e = threadIdx.x; e < experts; e += blockDim.x) load[e] = 0;
@@ -173,22 +311,22 @@ __global__ __launch_bounds__(kRouteThreads) void k_route_grad(RouteGradArgs a, u
     const int64_t row = ((int64_t)from + blockIdx.x) * kRows + r;
     const bool live = row < a.N;
     float x[V];
-    double s[V], g[V];
+    float ds[V] = {};
+    double s[V], rest[V], g[V];
+    const int have = live ? min(max(E - l * V, 0), V) : 0;
+    load_logits(a.logits, row * a.ldl + l * V, have, a.t, x);
+    if (a.dscores) load_run<SP24_F32>(a.dscores, row * E + l * V, have, 0.0f, ds);
+    scores_of_row<L>(x, a.softmax, s, rest);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const int e = l * V + i;
-        x[i] = live && e < E ? logit_of(a.logits, row * a.ldl + e, a.t) : -__builtin_inff();
-        g[i] = a.dscores && live && e < E ? (double)a.dscores[row * E + e] : 0.0;
-    }
-    scores_of_row<L>(x, a.softmax, s);
+    for (int i = 0; i < V; ++i) g[i] = (double)ds[i];
 #pragma unroll
-    for (int i = 0; i < V; ++i) scores[r][l * V + i] = s[i];
+    for (int i = 0; i < V; ++i) scores[r][i * L + l] = s[i];
     __syncthreads();
     double total = 0.0, along = 0.0;
     for (int j = l; j < a.topk; j += L) {
         int e = live ? a.ids[row * a.topk + j] : -1;
         if (e < 0 || e >= E) e = -1;
-        const double dw = e < 0 ? 0.0 : (double)a.dweights[row * a.topk + j], w = e < 0 ? 0.0 : scores[r][e];
+        const double dw = e < 0 ? 0.0 : (double)a.dweights[row * a.topk + j], w = e < 0 ? 0.0 : scores[r][image_place<L, V>(e)];
         total += w;
         along += dw * w;
         at[r][j] = e;
@@ -213,50 +351,62 @@ __global__ __launch_bounds__(kRouteThreads) void k_route_grad(RouteGradArgs a, u
         for (int i = 0; i < V; ++i) mean += x[i] == -__builtin_inff() ? 0.0 : g[i] * s[i];
         mean = over_row<L>(mean, sum_of{});
     }
-    if (!live) return;
+    float d[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const int e = l * V + i;
-        if (e >= E) continue;
-        const double d = x[i] == -__builtin_inff() ? 0.0 : s[i] * (a.softmax ? g[i] - mean : (1.0 - s[i]) * g[i]);
-        const int64_t to = row * a.lddl + e;
-        if (a.t == SP24_F32) store_out<SP24_F32>(a.dlogits, to, (float)d);
-        else if (a.t == SP24_BF16) store_out<SP24_BF16>(a.dlogits, to, (float)d);
-        else store_out<SP24_F16>(a.dlogits, to, (float)d);
-    }
+    for (int i = 0; i < V; ++i) d[i] = x[i] == -__builtin_inff() ? 0.0f : (float)(s[i] * (a.softmax ? g[i] - mean : rest[i] * g[i]));
+    const int64_t to = row * a.lddl + l * V;
+    if (a.t == SP24_F32) store_run<SP24_F32>(a.dlogits, to, have, d);
+    else if (a.t == SP24_BF16) store_run<SP24_BF16>(a.dlogits, to, have, d);
+    else store_run<SP24_F16>(a.dlogits, to, have, d);
 }
 
-// f(integral_constant lanes, integral_constant values a lane) for a row of this many experts
+// f(integral_constant lanes, integral_constant values a lane) for rows of this many experts.  Few rows are a wavefront each, whose chain of operations
+// is the time; many share wavefronts, which issue the less for each.  In a graph, us, top 8 of 256: 512 rows on 64 lanes 4.8, on 32 5.9; 2048 5.95 and
+// 6.1; 4096 8.6 and 7.2; 16384 23.9 and 18.5.  Top 6 of 64: 512 rows on 64 lanes 3.5, on 16 3.9; 2048 4.05 both; 8192 8.2 and 4.8.  (Half the lanes again:
+// 8192 rows of 64 5.4, of 256 10.6, but 4096 rows 8.6.)
 template <class F>
-static sp24_status by_experts(int experts, F&& f)
+static sp24_status by_experts(int experts, int64_t rows, F&& f)
 {
-    auto with = [&](auto l, auto v) { return f(l, v); };
     using std::integral_constant;
-    if (experts <= 8) return with(integral_constant<int, 8>{}, integral_constant<int, 1>{});
-    if (experts <= 16) return with(integral_constant<int, 16>{}, integral_constant<int, 1>{});
-    if (experts <= 32) return with(integral_constant<int, 32>{}, integral_constant<int, 1>{});
-    if (experts <= 64) return with(integral_constant<int, 64>{}, integral_constant<int, 1>{});
-    if (experts <= 128) return with(integral_constant<int, 32>{}, integral_constant<int, 4>{});
-    if (experts <= 256) return with(integral_constant<int, 32>{}, integral_constant<int, 8>{});
-    if (experts <= 512) return with(integral_constant<int, 64>{}, integral_constant<int, 8>{});
-    return with(integral_constant<int, 64>{}, integral_constant<int, 16>{});
+    auto with = [&](auto few_lanes, auto few_values, auto lanes, auto values) { return rows <= 2048 ? f(few_lanes, few_values) : f(lanes, values); };
+    const integral_constant<int, 1> one;
+    const integral_constant<int, 2> two;
+    const integral_constant<int, 4> four;
+    const integral_constant<int, 8> eight;
+    const integral_constant<int, 16> sixteen;
+    const integral_constant<int, 32> half;
+    const integral_constant<int, 64> all;
+    if (experts <= 8) return f(eight, one);
+    if (experts <= 16) return f(sixteen, one);
+    if (experts <= 32) return with(half, one, sixteen, two);
+    if (experts <= 64) return with(all, one, sixteen, four);
+    if (experts <= 128) return with(all, two, half, four);
+    if (experts <= 256) return with(all, four, half, eight);
+    if (experts <= 512) return f(all, eight);
+    return f(all, sixteen);
 }
 
 sp24_status launch_moe_route(const RouteArgs& a, hipStream_t st)
 {
-    if (a.load) k_no_load<<<1, 256, 0, st>>>(a.load, a.experts);
-    return by_experts(a.experts, [&](auto l, auto v) {
+    if (a.load && a.N == 0) k_no_load<<<1, 256, 0, st>>>(a.load, a.experts);
+    const sp24_status s = by_experts(a.experts, a.N, [&](auto l, auto v) {
         constexpr int L = decltype(l)::value, V = decltype(v)::value, kRows = kRouteThreads / L;
         return launch_in_parts((a.N + kRows - 1) / kRows, kRouteThreads, [&](unsigned from, unsigned grid) {
-            if (a.groups > 1) k_route<L, V, true><<<grid, kRouteThreads, 0, st>>>(a, from);
-            else k_route<L, V, false><<<grid, kRouteThreads, 0, st>>>(a, from);
+            const int size = a.experts / a.groups;
+            if (a.groups == 1) k_route<L, V, kNoGroups><<<grid, kRouteThreads, 0, st>>>(a, from);
+            else if (size % V == 0 && ((size / V) & (size / V - 1)) == 0) k_route<L, V, kLaneGroups><<<grid, kRouteThreads, 0, st>>>(a, from);
+            else k_route<L, V, kAnyGroups><<<grid, kRouteThreads, 0, st>>>(a, from);
         });
     });
+    if (s != SP24_OK || !a.load || a.N == 0) return s;
+    const int64_t choices = a.N * a.topk;
+    k_route_load<<<(unsigned)std::min<int64_t>((choices + kLoadChoices - 1) / kLoadChoices, 64), kLoadThreads, 0, st>>>(a.ids, a.load, choices, a.experts);
+    return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
 }
 
 sp24_status launch_moe_route_grad(const RouteGradArgs& a, hipStream_t st)
 {
-    return by_experts(a.experts, [&](auto l, auto v) {
+    return by_experts(a.experts, a.N, [&](auto l, auto v) {
         constexpr int L = decltype(l)::value, V = decltype(v)::value, kRows = kRouteThreads / L;
         return launch_in_parts((a.N + kRows - 1) / kRows, kRouteThreads, [&](unsigned from, unsigned grid) {
             k_route_grad<L, V><<<grid, kRouteThreads, 0, st>>>(a, from);
