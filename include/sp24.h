@@ -642,24 +642,35 @@ sp24_status sp24_linear_backward_checkpoint(const void* dY, const void* zcodes, 
                                             int64_t N, int64_t lddy, int64_t ldz, int64_t lddz, int64_t lddzt, sp24_act act, const int32_t* offsets,
                                             int experts, sp24_dtype code, sp24_dtype t, void* workspace, size_t workspace_bytes, void* stream);
 
+typedef enum {
+    SP24_A_KMAJOR = 0, /* A [M][lda]                                                                       */
+    SP24_A_MMAJOR = 1  /* A as its transpose [K][lda]: the rows of tokens, as sp24_linear_backward writes dZ */
+} sp24_aorder;
+
 /*
- * The weights' gradient from rows kept in 8 bits: D = A x B, A: M x K of type in = SP24_F16 or SP24_BF16 (the dZt of the layer's gradient, K its tokens),
- * B: the K x N values that `codes` and `scale` stand for, each rounded to `in`, the matrix instructions' operand (codes times scale has at most 2^-8 of a
- * block's largest value of precision: this is no more than half of that for the largest, less for all others).  Binary32 sums.  D: M x N of type
- * `in` or SP24_F32.  K may be any number, 0 included, which gives zeros.  Rows of A must be 16-byte aligned; what lies between K and the next 16-byte
- * boundary of a row may be read and is not used.
+ * The weights' gradient from rows kept in 8 bits: D = A x B, A: M x K of type in = SP24_F16 or SP24_BF16 in either order (dZ or its transpose, K
+ * the tokens), B: the K x N values that `codes` and `scale` stand for, each rounded to `in` (which is off by at most 2^-8 of the value for SP24_BF16, where
+ * a code is off by half a step, 2^-8 of its block's largest value).  Binary32 sums.  D: M x N of type `in` or SP24_F32.  K may be any number, 0 included,
+ * which gives zeros.  Rows of A must be 16-byte aligned; what lies between a row's end and the next 16-byte boundary may be read and is not used.  lda and N
+ * below 2^21, else SP24_ERR_SHAPE.
+ * workspace: device, 16-byte aligned, sp24_checkpoint_workspace_bytes(K, N) bytes: the restored rows of this one product (contents before the call are
+ * ignored, after it unspecified; calls sharing one must not overlap in time).
  */
-sp24_status sp24_gemm_dense_checkpoint(const void* A, const void* codes, const float* scale, void* D, int64_t M, int64_t N, int64_t K, int64_t lda,
-                                       int64_t ldc, int64_t ldd, sp24_dtype in, sp24_dtype code, sp24_dtype out, void* stream);
+size_t sp24_checkpoint_workspace_bytes(int64_t rows, int64_t H);
+sp24_status sp24_gemm_dense_checkpoint(const void* A, sp24_aorder order, const void* codes, const float* scale, void* D, int64_t M, int64_t N,
+                                       int64_t K, int64_t lda, int64_t ldc, int64_t ldd, sp24_dtype in, sp24_dtype code, sp24_dtype out,
+                                       void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * sp24_gemm_dense_grouped with its second operand kept in 8 bits: D_e = A[:, segment e] x B[segment e, :].  `rows` NULL: row r of B is row r of
- * `codes`, which has `row_count` rows then (tokens == row_count).  Else row r of B is row rows[r] / topk of the `tokens` rows of codes, the rows of sorted choices from the tokens' kept
- * ones, and zeros where rows[r] is -1 (or names no token).  offsets and the limits as there, with any N.
+ * `codes`, which has `row_count` rows then (tokens == row_count).  Else row r of B is row rows[r] / topk of the `tokens` rows of codes, the rows of sorted
+ * choices from the tokens' kept ones, and zeros where rows[r] is -1 (or names no token).  offsets as there, any N; orders of A, limits and workspace (for
+ * row_count rows) as above.
  */
-sp24_status sp24_gemm_dense_grouped_checkpoint(const void* A, const void* codes, const float* scale, const int32_t* rows, void* D, const int32_t* offsets,
-                                               int experts, int64_t M, int64_t N, int64_t row_count, int64_t tokens, int topk, int64_t lda, int64_t ldc,
-                                               int64_t ldd, sp24_dtype in, sp24_dtype code, sp24_dtype out, void* stream);
+sp24_status sp24_gemm_dense_grouped_checkpoint(const void* A, sp24_aorder order, const void* codes, const float* scale, const int32_t* rows, void* D,
+                                               const int32_t* offsets, int experts, int64_t M, int64_t N, int64_t row_count, int64_t tokens,
+                                               int topk, int64_t lda, int64_t ldc, int64_t ldd, sp24_dtype in, sp24_dtype code, sp24_dtype out,
+                                               void* workspace, size_t workspace_bytes, void* stream);
 
 /* Static, NUL-terminated description of a status code. */
 const char* sp24_status_string(sp24_status s);

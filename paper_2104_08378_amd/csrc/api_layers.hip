@@ -473,44 +473,85 @@ sp24_status sp24_restore_rows(const void* codes, const float* scale, const int32
     return launch_restore_rows(RestoreArgs{codes, scale, rows, out, N, R, H, ldc, ldo, topk, (int)act, code, t}, static_cast<hipStream_t>(stream));
 }
 
-// What both products from kept rows check.  K: columns of A; tokens: rows of the codes
-static sp24_status gemm_kept(const KeptMmArgs& a, void* stream)
+size_t sp24_checkpoint_workspace_bytes(int64_t rows, int64_t H)
+{
+    if (rows < 0 || H < 1 || rows > kMostRows || H > kMostRows || !blocks_fit(rows, H)) return 0;
+    return (size_t)rows * ((H + 7) / 8 * 8) * 2;
+}
+
+// Both products from kept rows: the rows are restored to the workspace, from which the product takes them.  K: columns of A; tokens: rows of the codes
+struct KeptProduct {
+    const void* A;
+    sp24_aorder order;
+    const void* codes;
+    const float* scale;
+    const int32_t *rows, *offsets;
+    void* D;
+    int64_t M, N, K, tokens, lda, ldc, ldd;
+    int topk, experts;
+    sp24_dtype in, code, out;
+    void* workspace;
+    size_t workspace_bytes;
+};
+static sp24_status gemm_kept(const KeptProduct& a, void* stream)
 {
     if (!is_float16(a.in) || !is_code(a.code) || !(a.out == SP24_F32 || a.out == a.in)) return SP24_ERR_DTYPE;
-    if (a.M < 0 || a.N < 0 || a.K < 0 || a.tokens < 0 || a.M > kMostRows || a.N > kMostRows || a.K > kMostRows || a.tokens > kMostRows || a.topk < 1) return SP24_ERR_SHAPE;
+    if (a.order != SP24_A_KMAJOR && a.order != SP24_A_MMAJOR) return SP24_ERR_LAYOUT;
+    if (a.M < 0 || a.N < 0 || a.K < 0 || a.tokens < 0 || a.M > kMostMm || a.N > kMostMm || a.K > kMostMm || a.tokens > kMostRows || a.topk < 1) return SP24_ERR_SHAPE;
     if (a.M == 0 || a.N == 0) return SP24_OK;
-    if (!blocks_fit(a.tokens, a.N)) return SP24_ERR_SHAPE;
+    const int64_t pitch = (a.N + 7) / 8 * 8;
+    const bool turned = a.order == SP24_A_MMAJOR;
+    if (!blocks_fit(a.tokens, a.N) || !blocks_fit(a.K, a.N)) return SP24_ERR_SHAPE;
     const int os = esize_of(a.out);
+    const size_t need = sp24_checkpoint_workspace_bytes(a.K, a.N);
     if (a.K > 0) {
-        SP24_TRY(check_matrix(a.A, a.M, a.K, a.lda, 2));
-        if (a.lda >= (int64_t)1 << 23) return SP24_ERR_SHAPE;           // 32-bit offsets inside a tile
+        SP24_TRY(check_matrix(a.A, turned ? a.K : a.M, turned ? a.M : a.K, a.lda, 2));
+        if (a.lda >= (int64_t)1 << 21 || pitch >= (int64_t)1 << 21) return SP24_ERR_SHAPE;      // 32-bit offsets inside a tile
         if (a.tokens > 0) {
             SP24_TRY(check_matrix(a.codes, a.tokens, a.N, a.ldc, 1, false));
             SP24_TRY(check_vector(a.scale));
         }
         if (a.rows) SP24_TRY(check_vector(a.rows));
+        if (!a.workspace) return SP24_ERR_NULL;
+        if (!aligned16(a.workspace)) return SP24_ERR_ALIGN;
+        if (a.workspace_bytes < need) return SP24_ERR_SHAPE;
     }
     SP24_TRY(check_matrix(a.D, a.M * a.experts, a.N, a.ldd, os, false));
-    if (overlaps(matrix(a.D, a.M * a.experts, a.N, a.ldd, os),
-                 {matrix(a.A, a.M, a.K, a.lda, 2), matrix(a.codes, a.tokens, a.N, a.ldc, 1), vec(a.scale, a.tokens * kept_blocks(a.N), 4), vec(a.rows, a.K, 4),
-                  vec(a.offsets, a.experts + 1, 4)}))
-        return SP24_ERR_SHAPE;
-    return launch_gemm_kept(a, static_cast<hipStream_t>(stream));
+    const Span d = matrix(a.D, a.M * a.experts, a.N, a.ldd, os), A = turned ? matrix(a.A, a.K, a.M, a.lda, 2) : matrix(a.A, a.M, a.K, a.lda, 2),
+               c = matrix(a.codes, a.tokens, a.N, a.ldc, 1), sc = vec(a.scale, a.tokens * kept_blocks(a.N), 4), ro = vec(a.rows, a.K, 4),
+               of = vec(a.offsets, a.experts + 1, 4), ws = Span{a.workspace, need};
+    if (overlaps(d, {A, c, sc, ro, of, ws}) || overlaps(ws, {A, c, sc, ro, of})) return SP24_ERR_SHAPE;
+    hipStream_t const st = static_cast<hipStream_t>(stream);
+    if (a.K > 0) SP24_TRY(launch_restore_rows(RestoreArgs{a.codes, a.scale, a.rows, a.workspace, a.tokens, a.K, a.N, a.ldc, pitch, a.topk, SP24_ACT_NONE, a.code, a.in}, st));
+    if (turned) {
+        TokenArgs t{};
+        static_cast<MmArgs&>(t) = MmArgs{a.A, nullptr, a.workspace, a.D, a.M, a.N, a.K, a.lda, pitch, a.ldd, a.in, a.out, SP24_B_NMAJOR, SP24_LAYOUT_CANONICAL, false};
+        t.offsets = a.offsets;
+        return launch_gemm_tokens(t, a.experts, st);
+    }
+    if (!a.offsets) return sp24_gemm_dense(a.A, a.workspace, a.D, a.M, a.N, a.K, a.lda, pitch, a.ldd, a.in, a.out, SP24_B_NMAJOR, stream);
+    SegmentArgs t{};
+    static_cast<MmArgs&>(t) = MmArgs{a.A, nullptr, a.workspace, a.D, a.M, a.N, a.K, a.lda, pitch, a.ldd, a.in, a.out, SP24_B_NMAJOR, SP24_LAYOUT_CANONICAL, false};
+    t.offsets = a.offsets;
+    return launch_gemm_grouped(t, a.experts, st);
 }
 
-sp24_status sp24_gemm_dense_checkpoint(const void* A, const void* codes, const float* scale, void* D, int64_t M, int64_t N, int64_t K, int64_t lda, int64_t ldc,
-                                       int64_t ldd, sp24_dtype in, sp24_dtype code, sp24_dtype out, void* stream)
+sp24_status sp24_gemm_dense_checkpoint(const void* A, sp24_aorder order, const void* codes, const float* scale, void* D, int64_t M, int64_t N, int64_t K,
+                                       int64_t lda, int64_t ldc, int64_t ldd, sp24_dtype in, sp24_dtype code, sp24_dtype out, void* workspace,
+                                       size_t workspace_bytes, void* stream)
 {
-    return gemm_kept(KeptMmArgs{A, codes, scale, nullptr, nullptr, D, M, N, K, K, lda, ldc, ldd, 1, 1, in, code, out}, stream);
+    return gemm_kept(KeptProduct{A, order, codes, scale, nullptr, nullptr, D, M, N, K, K, lda, ldc, ldd, 1, 1, in, code, out, workspace, workspace_bytes}, stream);
 }
 
-sp24_status sp24_gemm_dense_grouped_checkpoint(const void* A, const void* codes, const float* scale, const int32_t* rows, void* D, const int32_t* offsets,
-                                               int experts, int64_t M, int64_t N, int64_t row_count, int64_t tokens, int topk, int64_t lda, int64_t ldc,
-                                               int64_t ldd, sp24_dtype in, sp24_dtype code, sp24_dtype out, void* stream)
+sp24_status sp24_gemm_dense_grouped_checkpoint(const void* A, sp24_aorder order, const void* codes, const float* scale, const int32_t* rows, void* D,
+                                               const int32_t* offsets, int experts, int64_t M, int64_t N, int64_t row_count, int64_t tokens, int topk,
+                                               int64_t lda, int64_t ldc, int64_t ldd, sp24_dtype in, sp24_dtype code, sp24_dtype out, void* workspace,
+                                               size_t workspace_bytes, void* stream)
 {
     if (experts < 1 || experts > SP24_MOST_EXPERTS || row_count % kSegmentRows != 0 || (!rows && row_count > 0 && tokens != row_count)) return SP24_ERR_SHAPE;
     if (M > 0 && N > 0) SP24_TRY(check_vector(offsets));
-    return gemm_kept(KeptMmArgs{A, codes, scale, rows, offsets, D, M, N, row_count, tokens, lda, ldc, ldd, topk, experts, in, code, out}, stream);
+    return gemm_kept(KeptProduct{A, order, codes, scale, rows, offsets, D, M, N, row_count, tokens, lda, ldc, ldd, topk, experts, in, code, out, workspace,
+                                 workspace_bytes}, stream);
 }
 
 } // extern "C"

@@ -612,69 +612,93 @@ PyObject* linear_backward_checkpoint(PyObject* self, PyObject* const* args, Py_s
     Scratch ws(c, 4, sp24_linear_backward_workspace_bytes(M, N, grouped), *dY);
     if (c.ok && !c.none(4)) here(c, c.tensor(4));
     if (!c.ok) return not_handled();
-    const int64_t pitch = (N + 7) / 8 * 8;                     // 16-byte rows, which the weights' gradient asks for
-    at::Tensor dZ, dZt = make({M, pitch}, type, *dY), db = grouped ? make({experts, M}, at::kFloat, *dY) : make({M}, at::kFloat, *dY);
-    if (pitch != N) dZt = dZt.narrow(1, 0, N);
-    if (copy) dZ = make({N, M}, type, *dY);
+    const int64_t pitch = (M + 7) / 8 * 8, lddy = ld(*dY);     // 16-byte rows, which the weights' gradient asks for
     const void* pd = dY->data_ptr();
-    void *pdz = copy ? dZ.data_ptr() : nullptr, *pt = dZt.data_ptr(), *st = stream();
+    const bool own = copy || reinterpret_cast<uintptr_t>(pd) % 16 != 0 || lddy % 8 != 0;
+    at::Tensor dZ = own ? make({N, pitch}, type, *dY) : *dY, db = grouped ? make({experts, M}, at::kFloat, *dY) : make({M}, at::kFloat, *dY);
+    if (own && pitch != M) dZ = dZ.narrow(1, 0, M);
+    void *pdz = own ? dZ.data_ptr() : nullptr, *st = stream();
     float* pb = static_cast<float*>(db.data_ptr());
-    const int64_t lddy = ld(*dY);
     const sp24_status s = without_gil([&] {
-        return sp24_linear_backward_checkpoint(pd, pz, ps, pdz, pt, pb, M, N, lddy, ldz, M, pitch, act, po, (int)experts, code, t, ws.p, ws.bytes, st);
+        return sp24_linear_backward_checkpoint(pd, pz, ps, pdz, nullptr, pb, M, N, lddy, ldz, pitch, 0, act, po, (int)experts, code, t, ws.p, ws.bytes, st);
     });
     if (s != SP24_OK) return refused(self, s, "sp24_linear_backward_checkpoint");
-    return tuple(copy ? wrap(dZ) : again(args[0]), wrap(dZt), wrap(db));
+    at::Tensor turned = dZ.t();
+    return tuple(own ? wrap(dZ) : again(args[0]), wrap(turned), wrap(db));
 }
 
-// (A, checkpoint, out_dtype, out)
+// A matrix that is row-major or the transpose of one (argument 0): its order and row stride
+struct Ordered {
+    const at::Tensor* t = nullptr;
+    sp24_aorder order = SP24_A_KMAJOR;
+    int64_t ld_ = 0;
+    explicit Ordered(Call& c)
+    {
+        t = c.tensor(0);
+        c.require(c.ok && t->dim() == 2);
+        if (!c.ok) return;
+        here(c, t);
+        const int64_t M = t->size(0), K = t->size(1);
+        const int64_t by_row = M > 1 ? t->stride(0) : std::max(t->stride(0), K), by_column = K > 1 ? t->stride(1) : std::max(t->stride(1), M);
+        if ((t->stride(1) == 1 || K <= 1) && by_row % 8 == 0) ld_ = by_row;
+        else {
+            c.require(t->stride(0) == 1 || M <= 1);
+            order = SP24_A_MMAJOR;
+            ld_ = by_column;
+        }
+    }
+};
+
+// (A, checkpoint, out_dtype, out, workspace)
 PyObject* gemm_dense_checkpoint(PyObject* self, PyObject* const* args, Py_ssize_t)
 {
     Call c{args, true};
-    const at::Tensor* A = c.rowmajor(0);
+    const Ordered a(c);
     const Kept k(c, 1);
     const at::ScalarType out = c.dtype(2);
     if (!c.ok) return not_handled();
-    here(c, A);
-    const int64_t M = A->size(0), K = k.N, N = k.H, ldk = k.ld_, shape[2] = {M, N};
-    c.require(A->size(1) == K);
-    const sp24_dtype ti = type_of(A->scalar_type(), c.ok), to = type_of(out, c.ok), code = type_of(k.codes->scalar_type(), c.ok);
-    Result d(c, 3, shape, out, A);
+    const int64_t M = a.t->size(0), K = k.N, N = k.H, shape[2] = {M, N};
+    c.require(a.t->size(1) == K);
+    const sp24_dtype ti = type_of(a.t->scalar_type(), c.ok), to = type_of(out, c.ok), code = type_of(k.codes->scalar_type(), c.ok);
+    Result d(c, 3, shape, out, a.t);
     here(c, d.t);
+    Scratch ws(c, 4, sp24_checkpoint_workspace_bytes(K, N), *a.t);
+    if (c.ok && !c.none(4)) here(c, c.tensor(4));
     if (!c.ok) return not_handled();
-    const void *pa = A->data_ptr(), *pc = k.data();
+    const void *pa = a.t->data_ptr(), *pc = k.data();
     const float* ps = k.scales();
     void *pd = d.t->data_ptr(), *st = stream();
-    const int64_t lda = ld(*A), ldd = ld(*d.t);
-    const sp24_status s = without_gil([&] { return sp24_gemm_dense_checkpoint(pa, pc, ps, pd, M, N, K, lda, ldk, ldd, ti, code, to, st); });
+    const int64_t ldd = ld(*d.t);
+    const sp24_status s = without_gil([&] { return sp24_gemm_dense_checkpoint(pa, a.order, pc, ps, pd, M, N, K, a.ld_, k.ld_, ldd, ti, code, to, ws.p, ws.bytes, st); });
     return s == SP24_OK ? d.object() : refused(self, s, "sp24_gemm_dense_checkpoint");
 }
 
-// (A, checkpoint, offsets, out_dtype, rows, topk, out): a new result only
+// (A, checkpoint, offsets, out_dtype, rows, topk, out, workspace): a new result only
 PyObject* gemm_dense_grouped_checkpoint(PyObject* self, PyObject* const* args, Py_ssize_t)
 {
     Call c{args, true};
-    const at::Tensor *A = c.rowmajor(0), *offsets = c.contiguous(2);
+    const Ordered a(c);
     const Kept k(c, 1);
+    const at::Tensor* offsets = c.contiguous(2);
     const at::ScalarType out = c.dtype(3);
     const int topk = small(c, 5);
     c.require(c.none(6));
     if (!c.ok) return not_handled();
-    here(c, A);
     here(c, offsets);
-    const int64_t experts = offsets->numel() - 1, M = A->size(0), R = A->size(1), N = k.H, tokens = k.N, ldk = k.ld_;
+    const int64_t experts = offsets->numel() - 1, M = a.t->size(0), R = a.t->size(1), N = k.H, tokens = k.N;
     c.require(offsets->scalar_type() == at::kInt && experts >= 1 && experts <= SP24_MOST_EXPERTS && (!c.none(4) || tokens == R));
     const int32_t* rows = entries_here<const int32_t>(c, 4, R, at::kInt);
-    const sp24_dtype ti = type_of(A->scalar_type(), c.ok), to = type_of(out, c.ok), code = c.ok ? type_of(k.codes->scalar_type(), c.ok) : SP24_I8;
+    Scratch ws(c, 7, sp24_checkpoint_workspace_bytes(R, N), *a.t);
+    if (c.ok && !c.none(7)) here(c, c.tensor(7));
+    const sp24_dtype ti = type_of(a.t->scalar_type(), c.ok), to = type_of(out, c.ok), code = c.ok ? type_of(k.codes->scalar_type(), c.ok) : SP24_I8;
     if (!c.ok) return not_handled();
-    at::Tensor D = make({experts, M, N}, out, *A);
-    const void *pa = A->data_ptr(), *pc = k.data();
+    at::Tensor D = make({experts, M, N}, out, *a.t);
+    const void *pa = a.t->data_ptr(), *pc = k.data();
     const float* ps = k.scales();
     const int32_t* po = static_cast<const int32_t*>(offsets->data_ptr());
     void *pd = D.data_ptr(), *st = stream();
-    const int64_t lda = ld(*A);
     const sp24_status s = without_gil([&] {
-        return sp24_gemm_dense_grouped_checkpoint(pa, pc, ps, rows, pd, po, (int)experts, M, N, R, tokens, topk, lda, ldk, N, ti, code, to, st);
+        return sp24_gemm_dense_grouped_checkpoint(pa, a.order, pc, ps, rows, pd, po, (int)experts, M, N, R, tokens, topk, a.ld_, k.ld_, N, ti, code, to, ws.p, ws.bytes, st);
     });
     return s == SP24_OK ? wrap(D) : refused(self, s, "sp24_gemm_dense_grouped_checkpoint");
 }

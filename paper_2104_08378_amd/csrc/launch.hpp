@@ -58,6 +58,8 @@ struct MmArgs {
     // (M rows of ldd values each); out must then be F32 or I32, and conv and epi off.
     int k_slices, slice_steps;
     static constexpr bool kOwnStore = false;   // (arguments derived from these may bring their own way out)
+    static constexpr bool kMMajorA = false;    // (dense: A as its transpose, a row of M for every k)
+    static constexpr bool kPaddedColumns = false;      // (N-major B: its rows are whole 16-byte chunks whatever N is)
 };
 
 // General kernel: any M, N; both layouts; both B orders.  One wavefront per 32x32 tile of D.  Of the sparse products only
@@ -244,23 +246,13 @@ struct RestoreArgs {
 };
 sp24_status launch_restore_rows(const RestoreArgs& a, hipStream_t st);
 
-// D = A x what the codes stand for, of all rows or (offsets) segment by segment
-struct KeptMmArgs {
-    const void *A, *codes;
-    const float* scale;
-    const int32_t *rows, *offsets;        // rows null: column k of A meets row k of the codes; offsets null: one segment
-    void* D;
-    int64_t M, N, K, tokens, lda, ldc, ldd;      // K: columns of A; tokens: rows of the codes
-    int topk, experts;
-    sp24_dtype in, code, out;
-};
-sp24_status launch_gemm_kept(const KeptMmArgs& a, hipStream_t st);
-
 struct LinearArgs;                        // linear.hpp
 struct GroupedArgs;
 struct SegmentArgs;
 sp24_status launch_linear(const LinearArgs& a, hipStream_t st);
 sp24_status launch_linear_grouped(const GroupedArgs& a, hipStream_t st);
 sp24_status launch_gemm_grouped(const SegmentArgs& a, int experts, hipStream_t st);
+struct TokenArgs;
+sp24_status launch_gemm_tokens(const TokenArgs& a, int experts, hipStream_t st);
 
 } // namespace sp24

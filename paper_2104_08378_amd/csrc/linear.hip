@@ -113,4 +113,10 @@ sp24_status launch_gemm_grouped(const SegmentArgs& a, int experts, hipStream_t s
     return a.out == SP24_F32 ? run_segments<SP24_BF16, SP24_F32>(a, experts, st) : run_segments<SP24_BF16, SP24_BF16>(a, experts, st);
 }
 
+sp24_status launch_gemm_tokens(const TokenArgs& a, int experts, hipStream_t st)
+{
+    if (a.in == SP24_F16) return a.out == SP24_F32 ? gemm_tokens<SP24_F16, SP24_F32>(a, experts, st) : gemm_tokens<SP24_F16, SP24_F16>(a, experts, st);
+    return a.out == SP24_F32 ? gemm_tokens<SP24_BF16, SP24_F32>(a, experts, st) : gemm_tokens<SP24_BF16, SP24_BF16>(a, experts, st);
+}
+
 } // namespace sp24

@@ -131,6 +131,7 @@ struct GroupedArgs : LinearArgs {
 
 // The dense product of every segment: K (the rows) runs over segment blockIdx.y, whose result is that image of D.
 struct SegmentArgs : MmArgs {
+    static constexpr bool kPaddedColumns = true;
     const int32_t* offsets;
 
     template <int BM, int BN> __device__ __forceinline__ bool enter(int, int&)
@@ -139,6 +140,26 @@ struct SegmentArgs : MmArgs {
         int64_t first, last;
         segment_of(offsets, e, K, first, last);
         A = reinterpret_cast<const uint8_t*>(A) + first * es;
+        B = reinterpret_cast<const uint8_t*>(B) + first * ldb * es;
+        D = reinterpret_cast<uint8_t*>(D) + e * M * ldd * esize_of(out);
+        K = last - first;
+        return true;
+    }
+};
+
+// The same with A as its transpose, a row of M for every token: both operands as a layer's backward pass has them.  offsets null: one segment of
+// all K tokens.
+struct TokenArgs : MmArgs {
+    static constexpr bool kMMajorA = true, kPaddedColumns = true;
+    const int32_t* offsets;
+
+    template <int BM, int BN> __device__ __forceinline__ bool enter(int, int&)
+    {
+        if (!offsets) return true;
+        const int es = esize_of(in), e = blockIdx.y;
+        int64_t first, last;
+        segment_of(offsets, e, K, first, last);
+        A = reinterpret_cast<const uint8_t*>(A) + first * lda * es;
         B = reinterpret_cast<const uint8_t*>(B) + first * ldb * es;
         D = reinterpret_cast<uint8_t*>(D) + e * M * ldd * esize_of(out);
         K = last - first;
@@ -328,6 +349,7 @@ template <int DT, class ARGS> sp24_status layer_tiled(const ARGS& a, LayerTile t
 template <int DT, class ARGS> sp24_status layer_staged(const ARGS& a, hipStream_t st);
 sp24_status launch_linear_stream(const LinearArgs& a, hipStream_t st);
 sp24_status launch_grouped_stream(const GroupedArgs& a, hipStream_t st);
+template <int DT, int OUT> sp24_status gemm_tokens(const TokenArgs& a, int experts, hipStream_t st);
 
 // f(integral_constant<int, the input type>{})
 template <class F>

@@ -842,7 +842,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_spmm_pipe(ARGS a, int tiles
 template <int DT, int OUT, int WM, int WN, int TM, int TN, int NS, int BSRC, class ARGS = MmArgs>
 __global__ __launch_bounds__(64 * WM * WN, 1) void k_gemm_pipe(ARGS a, int tiles_m, int tiles_n)
 {
-    constexpr bool CONV = BSRC == 1, NMAJ = BSRC == 2;
+    constexpr bool CONV = BSRC == 1, NMAJ = BSRC == 2, MMAJ = ARGS::kMMajorA;       // MMAJ: A stored as its transpose, a row for every k
     constexpr int ES = is8<DT> ? 1 : 2;
     constexpr int BK = kRowBytes / ES;
     constexpr int NW = WM * WN;
@@ -872,17 +872,21 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_gemm_pipe(ARGS a, int tiles
 
     const int64_t lda_bytes = a.lda * ES, ldb_bytes = a.ldb * ES;
     const int64_t b_step = NMAJ ? (int64_t)BK * ldb_bytes : (int64_t)kRowBytes;
-    const uint8_t* a_blk = reinterpret_cast<const uint8_t*>(a.A) + (int64_t)tm * BM * lda_bytes + (int64_t)share.first * kRowBytes;
+    const int64_t a_step = MMAJ ? (int64_t)BK * lda_bytes : (int64_t)kRowBytes;
+    const uint8_t* a_blk = reinterpret_cast<const uint8_t*>(a.A) + (MMAJ ? (int64_t)tm * BM * ES : (int64_t)tm * BM * lda_bytes) + share.first * a_step;
     const uint8_t* b_blk = reinterpret_cast<const uint8_t*>(a.B) + (NMAJ ? (int64_t)tn * BN * ES : (int64_t)tn * BN * ldb_bytes) +
                            share.first * b_step;
     uint32_t a_off[NJA], b_off[NJB];
-    dma_offsets<BM, NW>((int64_t)tm * BM, a.M, lda_bytes, wave, lane, a_off);
+    if constexpr (MMAJ) dma_offsets_nmajor<BM, NW, ES>((int64_t)tm * BM, (a.M + 7) / 8 * 8, lda_bytes, wave, lane, a_off);
+    else dma_offsets<BM, NW>((int64_t)tm * BM, a.M, lda_bytes, wave, lane, a_off);
     conv_rows<BN, NW, ES> b_conv;
     if constexpr (CONV) b_conv.init(a.conv, (int64_t)tn * BN, a.N, wave, lane);
-    else if constexpr (NMAJ) dma_offsets_nmajor<BN, NW, ES>((int64_t)tn * BN, a.N, ldb_bytes, wave, lane, b_off);
+    else if constexpr (NMAJ) dma_offsets_nmajor<BN, NW, ES>((int64_t)tn * BN, ARGS::kPaddedColumns ? (a.N + 7) / 8 * 8 : a.N, ldb_bytes, wave, lane, b_off);
     else dma_offsets<BN, NW>((int64_t)tn * BN, a.N, ldb_bytes, wave, lane, b_off);
     nmajor_frags<BN, TN, ES> b_nm;
     if constexpr (NMAJ) b_nm.init(wn, lane);
+    nmajor_frags<BM, TM, ES> a_nm;
+    if constexpr (MMAJ) a_nm.init(wm, lane);
 
     acc_t acc[TM][TN];
 #pragma unroll
@@ -897,7 +901,8 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_gemm_pipe(ARGS a, int tiles
         if constexpr (!CONV) {
 #pragma unroll
             for (int j = 0; j < NJA; ++j)
-                lds_dma_tail<false>(a_blk + (int64_t)step * kRowBytes, a_off[j], past_k_kmajor<BM, NW>(j, wave, lane, tail),
+                lds_dma_tail<false>(a_blk + (int64_t)step * a_step, a_off[j],
+                                    MMAJ ? past_k_nmajor<BM, NW, ES>(j, wave, lane, tail) : past_k_kmajor<BM, NW>(j, wave, lane, tail),
                                     stage_ptr(u) + deal_a::id(wave, j) * 1024);
 #pragma unroll
             for (int j = 0; j < NJB; ++j)
@@ -907,7 +912,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_gemm_pipe(ARGS a, int tiles
         }
     };
     auto dma = [&](int step, const ConvTap& tap, int u) {
-        dma_rows<BM, NW>(a_blk + (int64_t)step * kRowBytes, a_off, stage_ptr(u), wave);
+        dma_rows<BM, NW>(a_blk + (int64_t)step * a_step, a_off, stage_ptr(u), wave);
         if constexpr (CONV) {
 #pragma unroll
             for (int j = 0; j < NJB; ++j)
@@ -937,7 +942,10 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_gemm_pipe(ARGS a, int tiles
     // the fragments of sub-step jj (32 bytes of K) of a stage
     auto read_frags = [&](const uint8_t* base, int jj, int4v (&xa)[TM], int4v (&xb)[TN]) {
 #pragma unroll
-        for (int i = 0; i < TM; ++i) xa[i] = *reinterpret_cast<const int4v*>(base + fa_off[jj] + i * 32 * kRowBytes);
+        for (int i = 0; i < TM; ++i) {
+            if constexpr (MMAJ) xa[i] = __builtin_bit_cast(int4v, a_nm.piece(base, jj, i));
+            else xa[i] = *reinterpret_cast<const int4v*>(base + fa_off[jj] + i * 32 * kRowBytes);
+        }
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
             if constexpr (NMAJ) xb[j] = __builtin_bit_cast(int4v, b_nm.piece(base + BM * kRowBytes, jj, j));
@@ -970,7 +978,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_gemm_pipe(ARGS a, int tiles
     constexpr int kBehindBarrier = TM * TN * NV / kSlots;       // transfers issued in sub-step 3
     constexpr int kWaitAndReads = waitcnt_vm((NS - 2) * NV) & ~(15 << 8);
     auto dma_one = [&](int step, const ConvTap& tap, int u, int x) {
-        if (x < NJA) lds_dma16(a_blk + (int64_t)step * kRowBytes, a_off[x], stage_ptr(u) + deal_a::id(wave, x) * 1024);
+        if (x < NJA) lds_dma16(a_blk + (int64_t)step * a_step, a_off[x], stage_ptr(u) + deal_a::id(wave, x) * 1024);
         else if constexpr (CONV) b_conv.issue(x - NJA, reinterpret_cast<const uint8_t*>(a.B), a.conv, tap, stage_ptr(u) + BM * kRowBytes, wave);
         else lds_dma16(b_blk + (int64_t)step * b_step, b_off[x - NJA], stage_ptr(u) + BM * kRowBytes + deal_b::id(wave, x - NJA) * 1024);
     };
@@ -1047,7 +1055,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void k_gemm_pipe(ARGS a, int tiles
         __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (NMAJ && !is8<DT>) {
+        if constexpr (NMAJ && !MMAJ && !is8<DT>) {
             // K ends inside a 16-byte piece of A's rows: what lies there behind K is not the matrix's, and a NaN would outlast B's zeros
             if (tail % 16 != 0) {
                 for (int row = tid; row < BM; row += 64 * NW) {

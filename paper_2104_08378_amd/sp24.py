@@ -102,9 +102,11 @@ def lib():
         L.sp24_checkpoint_rows.argtypes = [vp] * 3 + [i64] * 4 + [i32, i32, vp]
         L.sp24_restore_rows.argtypes = [vp] * 4 + [i64, i64, i32, i64, i64, i64, i32, i32, i32, vp]
         L.sp24_linear_backward_checkpoint.argtypes = [vp] * 6 + [i64] * 6 + [i32, vp, i32, i32, i32, vp, st, vp]
-        L.sp24_gemm_dense_checkpoint.argtypes = [vp] * 4 + [i64] * 6 + [i32, i32, i32, vp]
-        L.sp24_gemm_dense_grouped_checkpoint.argtypes = [vp] * 6 + [i32] + [i64] * 4 + [i32] + [i64] * 3 + [i32, i32, i32, vp]
-        for name in ("sp24_rmsnorm_backward_workspace_bytes", "sp24_linear_backward_workspace_bytes", "sp24_moe_sort_workspace_bytes"):
+        L.sp24_checkpoint_workspace_bytes.argtypes = [i64, i64]
+        L.sp24_gemm_dense_checkpoint.argtypes = [vp, i32, vp, vp, vp] + [i64] * 6 + [i32, i32, i32, vp, st, vp]
+        L.sp24_gemm_dense_grouped_checkpoint.argtypes = [vp, i32] + [vp] * 5 + [i32] + [i64] * 4 + [i32] + [i64] * 3 + [i32, i32, i32, vp, st, vp]
+        for name in ("sp24_rmsnorm_backward_workspace_bytes", "sp24_linear_backward_workspace_bytes", "sp24_moe_sort_workspace_bytes",
+                     "sp24_checkpoint_workspace_bytes"):
             getattr(L, name).restype = st
         for name in ("sp24_rmsnorm", "sp24_quantize_rows", "sp24_rmsnorm_backward", "sp24_linear", "sp24_linear_backward", "sp24_moe_sort", "sp24_moe_gather",
                      "sp24_moe_combine", "sp24_moe_combine_backward", "sp24_linear_grouped", "sp24_gemm_dense_grouped", "sp24_moe_route", "sp24_moe_route_backward",
@@ -1038,7 +1040,8 @@ def sp24_restore_rows(checkpoint, out_dtype, act="none", rows=None, topk=1, out=
 
 
 def sp24_linear_backward_checkpoint(dY, preact, act, offsets=None, workspace=None):
-    """sp24_linear_backward with ``preact`` a Checkpoint (None without an activation)."""
+    """sp24_linear_backward with ``preact`` a Checkpoint (None without an activation): (dZ [N, M], dZ.t(), dbias).  (The transpose is a view, which
+    sp24_gemm_dense_checkpoint takes as it is: dZ's rows are 16-byte aligned for it, a copy of dY's where those are not.)"""
     done = (_host or _load_host()).sp24_linear_backward_checkpoint(dY, preact, act, offsets, workspace)
     if done is not None:
         return done
@@ -1051,51 +1054,80 @@ def sp24_linear_backward_checkpoint(dY, preact, act, offsets=None, workspace=Non
             raise ValueError("preact must have dY's shape")
     _here(dY, codes, scale, offsets, workspace)
     experts = 0 if offsets is None else offsets.numel() - 1
-    dZ = torch.empty((N, M), dtype=dY.dtype, device=dY.device) if code != NO_ACT else None
-    pitch = -(-N // 8) * 8
-    dZt = torch.empty((M, pitch), dtype=dY.dtype, device=dY.device)[:, :N]
+    dZ = dY
+    if code != NO_ACT or dY.data_ptr() % 16 or _ld(dY) % 8:
+        dZ = torch.empty((N, -(-M // 8) * 8), dtype=dY.dtype, device=dY.device)[:, :M]
     dbias = torch.empty((M,) if offsets is None else (experts, M), dtype=torch.float32, device=dY.device)
     ws, ws_bytes = _scratch(workspace, lib().sp24_linear_backward_workspace_bytes(M, N, int(offsets is not None)), dY.device)
-    _check(lib().sp24_linear_backward_checkpoint(dY.data_ptr(), _ptr(codes), _ptr(scale), _ptr(dZ), dZt.data_ptr(), dbias.data_ptr(), M, N, _ld(dY),
-                                                 0 if codes is None else _ld(codes), M, pitch, code, _vector(offsets, experts + 1, "offsets", torch.int32), experts,
-                                                 I8 if codes is None else _DT[codes.dtype], _DT[dY.dtype], _ptr(ws), ws_bytes, _stream()),
-           "sp24_linear_backward_checkpoint")
-    return dY if dZ is None else dZ, dZt, dbias
+    _check(lib().sp24_linear_backward_checkpoint(dY.data_ptr(), _ptr(codes), _ptr(scale), None if dZ is dY else dZ.data_ptr(), None, dbias.data_ptr(), M, N,
+                                                 _ld(dY), 0 if codes is None else _ld(codes), -(-M // 8) * 8, 0, code,
+                                                 _vector(offsets, experts + 1, "offsets", torch.int32), experts, I8 if codes is None else _DT[codes.dtype],
+                                                 _DT[dY.dtype], _ptr(ws), ws_bytes, _stream()), "sp24_linear_backward_checkpoint")
+    return dZ, dZ.t(), dbias
 
 
-def sp24_gemm_dense_checkpoint(A, checkpoint, out_dtype, out=None):
-    """A [M, K] @ what the rows of a Checkpoint [K, N] stand for: the weights' gradient from rows kept in 8 bits."""
-    done = (_host or _load_host()).sp24_gemm_dense_checkpoint(A, checkpoint, out_dtype, out)
+A_KMAJOR, A_MMAJOR = 0, 1
+
+
+def _a_order(A):
+    """(order, row stride) of a matrix that is row-major or the transpose of one."""
+    if _dev(A, "A").dim() != 2:
+        raise ValueError("A must be a matrix")
+    M, K = A.shape
+    by_row = A.stride(0) if M > 1 else max(A.stride(0), K)
+    by_column = A.stride(1) if K > 1 else max(A.stride(1), M)
+    if (A.stride(1) == 1 or K <= 1) and by_row % 8 == 0:
+        return A_KMAJOR, by_row
+    if A.stride(0) == 1 or M <= 1:
+        return A_MMAJOR, by_column
+    if A.stride(1) != 1 and K > 1:
+        raise ValueError("A must be row-major or the transpose of a row-major matrix")
+    return A_KMAJOR, by_row
+
+
+def sp24_checkpoint_workspace_bytes(rows, H):
+    """Bytes of workspace that the product from ``rows`` kept rows of H values needs."""
+    return lib().sp24_checkpoint_workspace_bytes(rows, H)
+
+
+def sp24_gemm_dense_checkpoint(A, checkpoint, out_dtype, out=None, workspace=None):
+    """A [M, K] @ what the rows of a Checkpoint [K, N] stand for: the weights' gradient from rows kept in 8 bits.  A is row-major, or the transpose of dZ
+    [K, M] as sp24_linear_backward_checkpoint gives it."""
+    done = (_host or _load_host()).sp24_gemm_dense_checkpoint(A, checkpoint, out_dtype, out, workspace)
     if done is not None:
         return done
-    _rowmajor(A, "A")
+    order, lda = _a_order(A)
     codes, scale, K, N = _kept(checkpoint)
-    _here(A, codes, scale, out)
+    _here(A, codes, scale, out, workspace)
     M = A.shape[0]
     if A.shape[1] != K:
         raise ValueError("inner dimensions differ")
     D = _out(out, (M, N), out_dtype, A.device)
-    _check(lib().sp24_gemm_dense_checkpoint(A.data_ptr(), codes.data_ptr(), scale.data_ptr(), D.data_ptr(), M, N, K, _ld(A), _ld(codes), _ld(D), _DT[A.dtype],
-                                            _DT[codes.dtype], _DT[out_dtype], _stream()), "sp24_gemm_dense_checkpoint")
+    ws, ws_bytes = _scratch(workspace, sp24_checkpoint_workspace_bytes(K, N), A.device)
+    _check(lib().sp24_gemm_dense_checkpoint(A.data_ptr(), order, codes.data_ptr(), scale.data_ptr(), D.data_ptr(), M, N, K, lda, _ld(codes), _ld(D), _DT[A.dtype],
+                                            _DT[codes.dtype], _DT[out_dtype], _ptr(ws), ws_bytes, _stream()), "sp24_gemm_dense_checkpoint")
     return D
 
 
-def sp24_gemm_dense_grouped_checkpoint(A, checkpoint, offsets, out_dtype, rows=None, topk=1, out=None):
+def sp24_gemm_dense_grouped_checkpoint(A, checkpoint, offsets, out_dtype, rows=None, topk=1, out=None, workspace=None):
     """D [experts, M, N]: A [M, R] @ B [R, N] over the rows of every segment, B the rows of a Checkpoint, or (``rows`` [R] of sp24_moe_sort) those of its
     choices' tokens, zeros where there is no choice."""
-    done = (_host or _load_host()).sp24_gemm_dense_grouped_checkpoint(A, checkpoint, offsets, out_dtype, rows, topk, out)
+    done = (_host or _load_host()).sp24_gemm_dense_grouped_checkpoint(A, checkpoint, offsets, out_dtype, rows, topk, out, workspace)
     if done is not None:
         return done
-    _rowmajor(A, "A"), _dev(offsets, "offsets")
+    order, lda = _a_order(A)
+    _dev(offsets, "offsets")
     codes, scale, tokens, N = _kept(checkpoint)
-    _here(A, codes, scale, offsets, rows, out)
+    _here(A, codes, scale, offsets, rows, out, workspace)
     (M, R), experts = A.shape, offsets.numel() - 1
     if rows is None and R != tokens:
         raise ValueError("inner dimensions differ")
     D = torch.empty((max(experts, 0), M, N), dtype=out_dtype, device=A.device) if out is None else out
     if out is not None and (tuple(_dev(D, "out").shape) != (experts, M, N) or D.dtype != out_dtype or not D.is_contiguous()):
         raise ValueError("out must be a contiguous tensor [experts, M, N] of out_dtype")
-    _check(lib().sp24_gemm_dense_grouped_checkpoint(A.data_ptr(), codes.data_ptr(), scale.data_ptr(), _vector(rows, R, "rows", torch.int32), D.data_ptr(),
-                                                    _vector(offsets, experts + 1, "offsets", torch.int32), experts, M, N, R, tokens, topk, _ld(A), _ld(codes), N,
-                                                    _DT[A.dtype], _DT[codes.dtype], _DT[out_dtype], _stream()), "sp24_gemm_dense_grouped_checkpoint")
+    ws, ws_bytes = _scratch(workspace, sp24_checkpoint_workspace_bytes(R, N), A.device)
+    _check(lib().sp24_gemm_dense_grouped_checkpoint(A.data_ptr(), order, codes.data_ptr(), scale.data_ptr(), _vector(rows, R, "rows", torch.int32), D.data_ptr(),
+                                                    _vector(offsets, experts + 1, "offsets", torch.int32), experts, M, N, R, tokens, topk, lda, _ld(codes), N,
+                                                    _DT[A.dtype], _DT[codes.dtype], _DT[out_dtype], _ptr(ws), ws_bytes, _stream()),
+           "sp24_gemm_dense_grouped_checkpoint")
     return D

@@ -152,7 +152,7 @@ def test_gradient_through_the_activation(N, M, act, dtype, code):
     want = ref.d(dy) * ref.slope(z, act)
     err = ref.d(dy).abs() * (14 * 2.0 ** -24) * (1 + z.abs())
     ref.close(dz, want, err, "dz")
-    assert torch.equal(dzt, dz.t()) and dzt.stride(0) % 8 == 0
+    assert torch.equal(dzt, dz.t()) and dz.stride(0) % 8 == 0
     ref.close(db, want.sum(0), err.sum(0) + want.abs().sum(0) * (N + 4) * 2.0 ** -24, "db")
     # the same numbers in 32 bits, had again and rounded to the type: nothing in 16 bits comes between here
     if N % 16 == 0:
@@ -192,7 +192,13 @@ def product(M, N, K, dtype, code, out, spare=0, c_spare=0, c_offset=0):
     D = sp24.sp24_gemm_dense_checkpoint(A, c, out)
     ref.close(D, ref.d(a) @ b, (ref.d(a).abs() @ b.abs()) * ((K + 4) * 2.0 ** -24), str((M, N, K, dtype, code, out)))
     target = torch.full((M, N + 3), NAN, dtype=out, device="cuda")[:, :N]
-    assert torch.equal(sp24.sp24_gemm_dense_checkpoint(A, c, out, out=target), D) and target.data_ptr()
+    assert torch.equal(sp24.sp24_gemm_dense_checkpoint(A, c, out, out=target), D)
+    # the transpose of the tokens' rows, NaN behind them: the same products, added in another order
+    rows = torch.full((K, -(-M // 8) * 8 + spare), NAN, dtype=dtype, device="cuda")[:, :M]
+    rows.copy_(a.t())
+    D = sp24.sp24_gemm_dense_checkpoint(rows.t(), c, out, workspace=torch.full((K * (-(-N // 8) * 8),), NAN, dtype=dtype, device="cuda"))
+    ref.close(D, ref.d(a) @ b, (ref.d(a).abs() @ b.abs()) * ((K + 4) * 2.0 ** -24), str((M, N, K, dtype, code, out)))
+    assert torch.equal(sp24.sp24_gemm_dense_checkpoint(rows.t(), c, out, out=target), D)
 
 
 @pytest.mark.parametrize("code", [I8, F8])
@@ -248,6 +254,8 @@ def test_experts_weights_gradient(M, N, lengths, spare, dtype, code):
     A = torch.full((M, R + 8), NAN, dtype=dtype, device="cuda")[:, :R]
     A.copy_(a)
     o = offsets.tolist()
+    T = torch.full((R, -(-M // 8) * 8 + 8), NAN, dtype=dtype, device="cuda")[:, :M]
+    T.copy_(a.t())
 
     def check(D, b, out):
         assert D.shape == (len(lengths), M, N)
@@ -259,6 +267,7 @@ def test_experts_weights_gradient(M, N, lengths, spare, dtype, code):
     b = rounded(routing_ref.stands_for(*c), dtype)
     for out in (F32, dtype):
         check(sp24.sp24_gemm_dense_grouped_checkpoint(A, c, offsets, out), b, out)
+        check(sp24.sp24_gemm_dense_grouped_checkpoint(T.t(), c, offsets, out), b, out)
     # a row kept for every token; some rows without a choice, some of a choice of no token
     tokens, topk = max(R // 3, 1), 2
     c = kept(rows_of(g, tokens, N, F32), code)
@@ -268,6 +277,7 @@ def test_experts_weights_gradient(M, N, lengths, spare, dtype, code):
     out = torch.full((len(lengths), M, N), NAN, dtype=dtype, device="cuda")
     check(sp24.sp24_gemm_dense_grouped_checkpoint(A, c, offsets, dtype, rows=rows.cuda(), topk=topk, out=out), b, dtype)
     check(sp24.sp24_gemm_dense_grouped_checkpoint(A, c, offsets, F32, rows=rows.cuda(), topk=topk), b, F32)
+    check(sp24.sp24_gemm_dense_grouped_checkpoint(T.t(), c, offsets, F32, rows=rows.cuda(), topk=topk), b, F32)
 
 
 def test_rows_of_no_choice_hide_what_is_not_finite():

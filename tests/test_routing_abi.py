@@ -5,7 +5,7 @@ import pytest
 
 from paper_2104_08378_amd import sp24
 
-OK, NULL, SHAPE, ALIGN, DTYPE = 0, 1, 2, 3, 4
+OK, NULL, SHAPE, ALIGN, DTYPE, LAYOUT = 0, 1, 2, 3, 4, 5
 STEP = 0x10000000
 A, B, C, D, E, F, G = (STEP * i for i in range(1, 8))          # fake, aligned, far apart
 f = ctypes.c_float
@@ -77,17 +77,21 @@ def test_linear_backward():
 
 def test_products():
     L = sp24.lib()
+    W, BIG = 7 * STEP, 1 << 28
+    assert L.sp24_checkpoint_workspace_bytes(37, 61) == 37 * 64 * 2 and L.sp24_checkpoint_workspace_bytes(0, 64) == 0 and L.sp24_checkpoint_workspace_bytes(8, 0) == 0
 
-    def plain(a=A, c=B, s=C, d=D, M=64, N=64, K=37, lda=40, ldc=64, ldd=64, i=sp24.BF16, code=sp24.I8, o=sp24.F32):
-        return L.sp24_gemm_dense_checkpoint(a, c, s, d, M, N, K, lda, ldc, ldd, i, code, o, None)
+    def plain(a=A, c=B, s=C, d=D, M=64, N=64, K=37, lda=40, ldc=64, ldd=64, i=sp24.BF16, code=sp24.I8, o=sp24.F32, order=0, ws=W, bytes=BIG):
+        return L.sp24_gemm_dense_checkpoint(a, order, c, s, d, M, N, K, lda, ldc, ldd, i, code, o, ws, bytes, None)
     assert plain(a=0) == NULL and plain(c=0) == NULL and plain(s=0) == NULL and plain(d=0) == NULL and plain(a=A + 8) == ALIGN and plain(lda=41) == ALIGN and plain(lda=32) == SHAPE
     assert plain(ldc=63) == SHAPE and plain(ldd=63) == SHAPE and plain(s=C + 2) == ALIGN and plain(d=D + 2) == ALIGN and plain(K=-1) == SHAPE and plain(M=-1) == SHAPE
-    assert plain(lda=1 << 23) == SHAPE and plain(i=sp24.I8) == DTYPE and plain(i=sp24.F32) == DTYPE and plain(code=sp24.BF16) == DTYPE and plain(o=sp24.F16) == DTYPE
+    assert plain(lda=1 << 21) == SHAPE and plain(i=sp24.I8) == DTYPE and plain(i=sp24.F32) == DTYPE and plain(code=sp24.BF16) == DTYPE and plain(o=sp24.F16) == DTYPE
     assert plain(d=A) == SHAPE and plain(d=B) == SHAPE and plain(d=C) == SHAPE and plain(M=0) == OK and plain(N=0) == OK
+    assert plain(order=2) == LAYOUT and plain(order=1) == SHAPE and plain(order=1, lda=65) == ALIGN and plain(order=1, lda=64, ws=0) == NULL
+    assert plain(ws=0) == NULL and plain(ws=W + 8) == ALIGN and plain(bytes=37 * 128 - 1) == SHAPE and plain(ws=A) == SHAPE and plain(ws=B) == SHAPE and plain(d=W) == SHAPE
 
-    def grouped(a=A, c=B, s=C, rows=D, d=E, of=F, n=4, M=64, N=60, R=32, tokens=20, k=2, lda=32, ldc=64, ldd=64, i=sp24.BF16, code=sp24.F8, o=sp24.F32):
-        return L.sp24_gemm_dense_grouped_checkpoint(a, c, s, rows, d, of, n, M, N, R, tokens, k, lda, ldc, ldd, i, code, o, None)
+    def grouped(a=A, c=B, s=C, rows=D, d=E, of=F, n=4, M=64, N=60, R=32, tokens=20, k=2, lda=32, ldc=64, ldd=64, i=sp24.BF16, code=sp24.F8, o=sp24.F32, order=0, ws=W, bytes=BIG):
+        return L.sp24_gemm_dense_grouped_checkpoint(a, order, c, s, rows, d, of, n, M, N, R, tokens, k, lda, ldc, ldd, i, code, o, ws, bytes, None)
     assert grouped(a=0) == NULL and grouped(c=0) == NULL and grouped(s=0) == NULL and grouped(d=0) == NULL and grouped(of=0) == NULL and grouped(of=F + 2) == ALIGN
     assert grouped(rows=0) == SHAPE and grouped(rows=D + 1) == ALIGN and grouped(R=24) == SHAPE and grouped(n=0) == SHAPE and grouped(n=1025) == SHAPE and grouped(k=0) == SHAPE
     assert grouped(tokens=-1) == SHAPE and grouped(lda=24) == SHAPE and grouped(d=D) == SHAPE and grouped(d=F) == SHAPE and grouped(d=B) == SHAPE and grouped(i=sp24.F8) == DTYPE
-    assert grouped(M=0) == OK
+    assert grouped(M=0) == OK and grouped(order=1) == SHAPE and grouped(order=1, lda=68) == ALIGN and grouped(ws=F) == SHAPE and grouped(bytes=32 * 128 - 1) == SHAPE
