@@ -653,10 +653,10 @@ typedef enum {
  * a code is off by half a step, 2^-8 of its block's largest value).  Binary32 sums.  D: M x N of type `in` or SP24_F32.  K may be any number, 0 included,
  * which gives zeros.  Rows of A must be 16-byte aligned; what lies between a row's end and the next 16-byte boundary may be read and is not used.  lda and N
  * below 2^21, else SP24_ERR_SHAPE.
- * workspace: device, 16-byte aligned, sp24_checkpoint_workspace_bytes(K, N) bytes: the restored rows of this one product (contents before the call are
- * ignored, after it unspecified; calls sharing one must not overlap in time).
+ * workspace: device, 16-byte aligned, sp24_gemm_dense_checkpoint_workspace_bytes(M, N, K, 0) bytes: the restored rows of this one product, and partial
+ * products where few tiles have many tokens (contents before the call are ignored, after it unspecified; calls sharing one must not overlap in time).
  */
-size_t sp24_checkpoint_workspace_bytes(int64_t rows, int64_t H);
+size_t sp24_gemm_dense_checkpoint_workspace_bytes(int64_t M, int64_t N, int64_t K, int grouped);
 sp24_status sp24_gemm_dense_checkpoint(const void* A, sp24_aorder order, const void* codes, const float* scale, void* D, int64_t M, int64_t N,
                                        int64_t K, int64_t lda, int64_t ldc, int64_t ldd, sp24_dtype in, sp24_dtype code, sp24_dtype out,
                                        void* workspace, size_t workspace_bytes, void* stream);
@@ -664,8 +664,8 @@ sp24_status sp24_gemm_dense_checkpoint(const void* A, sp24_aorder order, const v
 /*
  * sp24_gemm_dense_grouped with its second operand kept in 8 bits: D_e = A[:, segment e] x B[segment e, :].  `rows` NULL: row r of B is row r of
  * `codes`, which has `row_count` rows then (tokens == row_count).  Else row r of B is row rows[r] / topk of the `tokens` rows of codes, the rows of sorted
- * choices from the tokens' kept ones, and zeros where rows[r] is -1 (or names no token).  offsets as there, any N; orders of A, limits and workspace (for
- * row_count rows) as above.
+ * choices from the tokens' kept ones, and zeros where rows[r] is -1 (or names no token).  offsets as there, any N; orders of A, limits and workspace (K =
+ * row_count, grouped = 1) as above.
  */
 sp24_status sp24_gemm_dense_grouped_checkpoint(const void* A, sp24_aorder order, const void* codes, const float* scale, const int32_t* rows, void* D,
                                                const int32_t* offsets, int experts, int64_t M, int64_t N, int64_t row_count, int64_t tokens,

@@ -473,10 +473,13 @@ sp24_status sp24_restore_rows(const void* codes, const float* scale, const int32
     return launch_restore_rows(RestoreArgs{codes, scale, rows, out, N, R, H, ldc, ldo, topk, (int)act, code, t}, static_cast<hipStream_t>(stream));
 }
 
-size_t sp24_checkpoint_workspace_bytes(int64_t rows, int64_t H)
+// the restored rows of a product
+static size_t restored_bytes(int64_t K, int64_t N) { return (size_t)K * ((N + 7) / 8 * 8) * 2; }
+
+size_t sp24_gemm_dense_checkpoint_workspace_bytes(int64_t M, int64_t N, int64_t K, int grouped)
 {
-    if (rows < 0 || H < 1 || rows > kMostRows || H > kMostRows || !blocks_fit(rows, H)) return 0;
-    return (size_t)rows * ((H + 7) / 8 * 8) * 2;
+    if (M < 1 || N < 1 || K < 0 || M > kMostMm || N > kMostMm || K > kMostMm || !blocks_fit(K, N)) return 0;
+    return restored_bytes(K, N) + (grouped ? 0 : token_split(M, N, K).bytes);
 }
 
 // Both products from kept rows: the rows are restored to the workspace, from which the product takes them.  K: columns of A; tokens: rows of the codes
@@ -503,7 +506,7 @@ static sp24_status gemm_kept(const KeptProduct& a, void* stream)
     const bool turned = a.order == SP24_A_MMAJOR;
     if (!blocks_fit(a.tokens, a.N) || !blocks_fit(a.K, a.N)) return SP24_ERR_SHAPE;
     const int os = esize_of(a.out);
-    const size_t need = sp24_checkpoint_workspace_bytes(a.K, a.N);
+    const size_t need = sp24_gemm_dense_checkpoint_workspace_bytes(a.M, a.N, a.K, a.offsets != nullptr);
     if (a.K > 0) {
         SP24_TRY(check_matrix(a.A, turned ? a.K : a.M, turned ? a.M : a.K, a.lda, 2));
         if (a.lda >= (int64_t)1 << 21 || pitch >= (int64_t)1 << 21) return SP24_ERR_SHAPE;      // 32-bit offsets inside a tile
@@ -527,7 +530,8 @@ static sp24_status gemm_kept(const KeptProduct& a, void* stream)
         TokenArgs t{};
         static_cast<MmArgs&>(t) = MmArgs{a.A, nullptr, a.workspace, a.D, a.M, a.N, a.K, a.lda, pitch, a.ldd, a.in, a.out, SP24_B_NMAJOR, SP24_LAYOUT_CANONICAL, false};
         t.offsets = a.offsets;
-        return launch_gemm_tokens(t, a.experts, st);
+        const size_t rows = restored_bytes(a.K, a.N);
+        return launch_gemm_tokens(t, a.experts, need > rows ? static_cast<uint8_t*>(a.workspace) + rows : nullptr, st);
     }
     if (!a.offsets) return sp24_gemm_dense(a.A, a.workspace, a.D, a.M, a.N, a.K, a.lda, pitch, a.ldd, a.in, a.out, SP24_B_NMAJOR, stream);
     SegmentArgs t{};

@@ -9,22 +9,39 @@ namespace sp24 {
 template <int DT, int OUT>
 sp24_status gemm_tokens(const TokenArgs& a, int experts, hipStream_t st)
 {
-    auto run = [&](auto kernel, int rows, int columns, int threads) {
+    auto run = [&](auto kernel, int rows, int columns, int threads, int images) {
         const int64_t tiles_m = (a.M + rows - 1) / rows, tiles_n = (a.N + columns - 1) / columns;
-        return launch_tiles(tiles_m * tiles_n, experts, threads, [&](dim3 grid, dim3 block) { kernel<<<grid, block, 0, st>>>(a, (int)tiles_m, (int)tiles_n); });
+        return launch_tiles(tiles_m * tiles_n, images, threads, [&](dim3 grid, dim3 block) { kernel<<<grid, block, 0, st>>>(a, (int)tiles_m, (int)tiles_n); });
     };
-    if (a.offsets) {
-        if ((a.N + 255) / 256 * 256 * 4 > (a.N + 127) / 128 * 128 * 5) return run(k_gemm_pipe<DT, OUT, 4, 2, 1, 2, 2, 2, TokenArgs>, 128, 128, 512);
-        return run(k_gemm_pipe<DT, OUT, 2, 4, 2, 2, 3, 2, TokenArgs>, 128, 256, 512);
+    // K split: partial products of 128 x 128 tiles, a slice of the tokens each, in binary32
+    if (a.k_slices > 1) {
+        if constexpr (OUT == SP24_F32) {
+            // (eight wavefronts of 64 x 32 while units are left, as below)
+            const int64_t groups = ((a.M + 127) / 128) * ((a.N + 127) / 128) * a.k_slices;
+            if (groups <= 176) return run(k_gemm_pipe<DT, OUT, 2, 4, 2, 1, 4, 2, TokenArgs>, 128, 128, 512, a.k_slices);
+            return run(k_gemm_pipe<DT, OUT, 2, 2, 2, 2, 4, 2, TokenArgs>, 128, 128, 256, a.k_slices);
+        } else return SP24_ERR_LAUNCH;
     }
     const int64_t cols = (a.N + 127) / 128, small = ((a.M + 127) / 128) * cols, tall = ((a.M + 255) / 256) * cols, big = ((a.M + 255) / 256) * ((a.N + 255) / 256);
-    const double cover_big = (double)(((a.M + 255) / 256) * 256) * (double)(((a.N + 255) / 256) * 256), cover_small = (double)small * 128 * 128;
-    if (small <= 128) return run(k_gemm_pipe<DT, OUT, 4, 1, 1, 2, 6, 2, TokenArgs>, 128, 64, 256);
-    if (small <= 176) return run(k_gemm_pipe<DT, OUT, 4, 2, 1, 2, 4, 2, TokenArgs>, 128, 128, 512);
-    if (small <= 256) return run(k_gemm_pipe<DT, OUT, 2, 2, 2, 2, 4, 2, TokenArgs>, 128, 128, 256);
-    if (tall <= 256) return run(k_gemm_pipe<DT, OUT, 4, 2, 2, 2, 3, 2, TokenArgs>, 256, 128, 512);
-    if (big >= 129 && cover_big <= 1.35 * cover_small) return run(k_gemm_pipe<DT, OUT, 4, 2, 2, 4, 2, 2, TokenArgs>, 256, 256, 512);
-    return run(k_gemm_pipe<DT, OUT, 2, 4, 2, 2, 3, 2, TokenArgs>, 128, 256, 512);
+    const bool covered = (double)big * 256 * 256 <= 1.35 * (double)small * 128 * 128;
+    // Segments: large tiles, whose fewer transfers and reads of LDS weigh more than the steps that a short segment's tile has to fill its stages (us, restoring
+    // included: eight of 2048 x 1024 from 8192 choices on 128 x 256 53.1, on 256 x 256 46.7; 32 of 1024 x 512 from 16384 39.4, 36.8; 16 of 1024 x 1024 from
+    // 2048 20.2, 19.2); half as large ones where they make too few, and columns of 128 where wider ones are mostly padding.
+    if (a.offsets) {
+        if (big * experts >= 129 && covered) return run(k_gemm_pipe<DT, OUT, 4, 2, 2, 4, 2, 2, TokenArgs>, 256, 256, 512, experts);
+        if ((a.N + 255) / 256 * 256 * 4 > (a.N + 127) / 128 * 128 * 5) return run(k_gemm_pipe<DT, OUT, 4, 2, 1, 2, 2, 2, TokenArgs>, 128, 128, 512, experts);
+        return run(k_gemm_pipe<DT, OUT, 2, 4, 2, 2, 3, 2, TokenArgs>, 128, 256, 512, experts);
+    }
+    // All tokens: the tile whose workgroups still find a unit each, as for the product of an M x K operand (us, restoring included): 512 x 512 x 8192 on 64 x 64
+    // 41.2, 128 x 64 47.7, 128 x 128 51.3; 2048 x 1024 x 4096 on 64 x 64 37.6, 128 x 64 30.5, 128 x 128 32.6; 4096 x 1024 x 8192 on 128 x 128, four wavefronts 79.9,
+    // eight 82.1, 256 x 128 94.3; 8192 x 2048 x 2048 on 256 x 256 65.8, 256 x 128 69.1, 128 x 128 76.2.
+    if (small <= 64) return run(k_gemm_pipe<DT, OUT, 2, 2, 1, 1, 9, 2, TokenArgs>, 64, 64, 256, 1);
+    if (small <= 128) return run(k_gemm_pipe<DT, OUT, 4, 1, 1, 2, 6, 2, TokenArgs>, 128, 64, 256, 1);
+    if (small <= 176) return run(k_gemm_pipe<DT, OUT, 2, 4, 2, 1, 4, 2, TokenArgs>, 128, 128, 512, 1);
+    if (small <= 256) return run(k_gemm_pipe<DT, OUT, 2, 2, 2, 2, 4, 2, TokenArgs>, 128, 128, 256, 1);
+    if (tall <= 256) return run(k_gemm_pipe<DT, OUT, 4, 2, 2, 2, 3, 2, TokenArgs>, 256, 128, 512, 1);
+    if (big >= 129 && covered) return run(k_gemm_pipe<DT, OUT, 4, 2, 2, 4, 2, 2, TokenArgs>, 256, 256, 512, 1);
+    return run(k_gemm_pipe<DT, OUT, 2, 4, 2, 2, 3, 2, TokenArgs>, 128, 256, 512, 1);
 }
 
 } // namespace sp24

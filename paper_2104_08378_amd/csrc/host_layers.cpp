@@ -662,7 +662,7 @@ PyObject* gemm_dense_checkpoint(PyObject* self, PyObject* const* args, Py_ssize_
     const sp24_dtype ti = type_of(a.t->scalar_type(), c.ok), to = type_of(out, c.ok), code = type_of(k.codes->scalar_type(), c.ok);
     Result d(c, 3, shape, out, a.t);
     here(c, d.t);
-    Scratch ws(c, 4, sp24_checkpoint_workspace_bytes(K, N), *a.t);
+    Scratch ws(c, 4, sp24_gemm_dense_checkpoint_workspace_bytes(M, N, K, 0), *a.t);
     if (c.ok && !c.none(4)) here(c, c.tensor(4));
     if (!c.ok) return not_handled();
     const void *pa = a.t->data_ptr(), *pc = k.data();
@@ -688,7 +688,7 @@ PyObject* gemm_dense_grouped_checkpoint(PyObject* self, PyObject* const* args, P
     const int64_t experts = offsets->numel() - 1, M = a.t->size(0), R = a.t->size(1), N = k.H, tokens = k.N;
     c.require(offsets->scalar_type() == at::kInt && experts >= 1 && experts <= SP24_MOST_EXPERTS && (!c.none(4) || tokens == R));
     const int32_t* rows = entries_here<const int32_t>(c, 4, R, at::kInt);
-    Scratch ws(c, 7, sp24_checkpoint_workspace_bytes(R, N), *a.t);
+    Scratch ws(c, 7, sp24_gemm_dense_checkpoint_workspace_bytes(M, N, R, 1), *a.t);
     if (c.ok && !c.none(7)) here(c, c.tensor(7));
     const sp24_dtype ti = type_of(a.t->scalar_type(), c.ok), to = type_of(out, c.ok), code = c.ok ? type_of(k.codes->scalar_type(), c.ok) : SP24_I8;
     if (!c.ok) return not_handled();

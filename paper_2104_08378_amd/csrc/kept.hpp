@@ -11,8 +11,13 @@ template <int CODE>
 __device__ __forceinline__ void code_values4(uint32_t w, float (&v)[4])
 {
     if constexpr (CODE == SP24_I8) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = (float)(int8_t)(w >> (8 * i));
+        // 2^23 + (code + 128) as its bits, a byte moved into the low end of a constant; the difference is exact.  (A conversion of an integer costs as much as
+        // four of these.)
+        const uint32_t u = w ^ 0x80808080u;
+        v[0] = __uint_as_float(__builtin_amdgcn_perm(0x4B000000u, u, 0x07060500u)) - 8388736.0f;
+        v[1] = __uint_as_float(__builtin_amdgcn_perm(0x4B000000u, u, 0x07060501u)) - 8388736.0f;
+        v[2] = __uint_as_float(__builtin_amdgcn_perm(0x4B000000u, u, 0x07060502u)) - 8388736.0f;
+        v[3] = __uint_as_float(__builtin_amdgcn_perm(0x4B000000u, u, 0x07060503u)) - 8388736.0f;
     } else {
         typedef float f32x2 __attribute__((ext_vector_type(2)));
         const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);

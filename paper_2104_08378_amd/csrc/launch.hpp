@@ -253,6 +253,13 @@ sp24_status launch_linear(const LinearArgs& a, hipStream_t st);
 sp24_status launch_linear_grouped(const GroupedArgs& a, hipStream_t st);
 sp24_status launch_gemm_grouped(const SegmentArgs& a, int experts, hipStream_t st);
 struct TokenArgs;
-sp24_status launch_gemm_tokens(const TokenArgs& a, int experts, hipStream_t st);
+struct TokenSplit {
+    int slices, steps;                    // of the tokens; steps of 64 tokens to one
+    int64_t ldw;
+    size_t bytes;                         // of the partial products (0: not split)
+};
+TokenSplit token_split(int64_t M, int64_t N, int64_t K);
+// partial: token_split().bytes of a product that is to be split, or null
+sp24_status launch_gemm_tokens(const TokenArgs& a, int experts, void* partial, hipStream_t st);
 
 } // namespace sp24

@@ -4,19 +4,23 @@
 // Bound by memory: dY and Z are read once, both forms of dZ written once.  A workgroup takes 64 rows x 64 (128) values through LDS in binary32,
 // so that the sums see them unrounded; rows of 65 (129) words there, of which the columns' reads (8 rows x 8 a wavefront) find no
 // bank twice, and the rows' writes none (two).  Sums: 16 rows (the unit of segments) in row order, then those in order.
-// 4096 x 4096 bf16 with GELU, the sums' second kernel included: 31.6 us, 134 MB at 4.2 TB/s; without an activation 14.9, 67 MB at 4.5.
+// 4096 x 4096 bf16 with GELU, the sums' second kernel included: 31.6 us, 134 MB at 4.2 TB/s; without an activation 14.9, 67 MB at 4.5.  Z kept in 8 bits and
+// no transposed form, 8192 x 4096: 32 us, 161 MB at 5.0.
 //
 // dZ is rounded to 16 bits, which both of its products read (the matrix instructions' operands): gradients of 4096 x 1024 weights from 4096
 // tokens are off by 0.0023 of their size in bf16, where rounding the results alone leaves 0.0017.  The bias's gradient sums unrounded values.
 #include "kept.hpp"
 #include "launch.hpp"
+#include "linear.hpp"
 
 namespace sp24 {
 
 constexpr int kGradTile = 64;           // rows of a tile
+constexpr int kFewExperts = 32;         // whose segments four groups of threads go through one after the other
 
-// ZT: what Z is held in, the values' type or codes with a scale for each block of 128
-template <int T, int ZT, int WIDTH>
+// ZT: what Z is held in, the values' type or codes with a scale for each block of 128.  FEW: there is one tile of rows, and the sums need no
+// second launch: they are added sixteen rows at a time, in row order.
+template <int T, int ZT, int WIDTH, bool FEW>
 __global__ __launch_bounds__(4 * WIDTH) void k_linear_grad(LinearGradArgs a, int tiles_m, unsigned from)
 {
     constexpr int kPitch = WIDTH + 1, CH = WIDTH / 8;
@@ -72,7 +76,26 @@ __global__ __launch_bounds__(4 * WIDTH) void k_linear_grad(LinearGradArgs a, int
             store_values8<T>(a.dZt, (m0 + f) * a.lddzt + n0 + t, rows, v);
         }
     }
-    if (a.partial) {
+    if constexpr (FEW) {
+        const int f = tid % WIDTH, p = tid / WIDTH;
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum += tile[(p * 16 + i) * kPitch + f];           // (rows past N are zeros)
+        part[p][f] = sum;
+        __syncthreads();
+        if (m0 + f >= a.M) return;
+        if (!a.offsets) {
+            if (p == 0) a.dbias[m0 + f] = ((part[0][f] + part[1][f]) + part[2][f]) + part[3][f];
+        } else {
+            for (int e = p; e < a.experts; e += 4) {
+                int64_t from_row, to_row;
+                segment_of(a.offsets, e, a.N, from_row, to_row);
+                float total = 0.0f;
+                for (int64_t k = from_row / 16; k < to_row / 16; ++k) total += part[k][f];
+                a.dbias[(int64_t)e * a.M + m0 + f] = total;
+            }
+        }
+    } else if (a.partial) {
         const int f = tid % WIDTH, p = tid / WIDTH;
         float sum = 0.0f;
 #pragma unroll
@@ -88,16 +111,16 @@ __global__ __launch_bounds__(4 * WIDTH) void k_linear_grad(LinearGradArgs a, int
     }
 }
 
-template <int WIDTH>
+template <int WIDTH, bool FEW>
 static sp24_status run_linear_grad(const LinearGradArgs& a, hipStream_t st)
 {
     const int64_t tiles_m = (a.M + WIDTH - 1) / WIDTH, tiles_n = (a.N + kGradTile - 1) / kGradTile;
     return launch_in_parts(tiles_m * tiles_n, 4 * WIDTH, [&](unsigned from, unsigned grid) {
         auto run = [&](auto t) {
             constexpr int T = decltype(t)::value;
-            if (a.zcode == SP24_I8) k_linear_grad<T, SP24_I8, WIDTH><<<grid, 4 * WIDTH, 0, st>>>(a, (int)tiles_m, from);
-            else if (a.zcode == SP24_F8) k_linear_grad<T, SP24_F8, WIDTH><<<grid, 4 * WIDTH, 0, st>>>(a, (int)tiles_m, from);
-            else k_linear_grad<T, T, WIDTH><<<grid, 4 * WIDTH, 0, st>>>(a, (int)tiles_m, from);
+            if (a.zcode == SP24_I8) k_linear_grad<T, SP24_I8, WIDTH, FEW><<<grid, 4 * WIDTH, 0, st>>>(a, (int)tiles_m, from);
+            else if (a.zcode == SP24_F8) k_linear_grad<T, SP24_F8, WIDTH, FEW><<<grid, 4 * WIDTH, 0, st>>>(a, (int)tiles_m, from);
+            else if constexpr (!FEW) k_linear_grad<T, T, WIDTH, FEW><<<grid, 4 * WIDTH, 0, st>>>(a, (int)tiles_m, from);
         };
         if (a.t == SP24_F16) run(std::integral_constant<int, SP24_F16>{});
         else run(std::integral_constant<int, SP24_BF16>{});
@@ -106,10 +129,13 @@ static sp24_status run_linear_grad(const LinearGradArgs& a, hipStream_t st)
 
 sp24_status launch_linear_grad(const LinearGradArgs& a, hipStream_t st)
 {
+    // One tile of rows, Z kept in 8 bits (the sums beside a 16-bit Z keep their order, and with it their bits): 64 x 2048 5.9 -> 4.4 us, of segments 6.4 -> 5.4.  (All
+    // tiles of a column in one workgroup: 128 rows 7.1, against 6.1 with the second launch, 256 rows 12.4 against 6.2.)
+    if (a.zcode != a.t && a.dbias && a.N > 0 && a.N <= kGradTile && a.experts <= kFewExperts) return run_linear_grad<64, true>(a, st);
     // Large ones with an activation, whose two operands come in rows of 256 bytes a tile then: 4096 x 4096 with GELU 35.6 -> 32.9 us.  Without
     // one 15.2 and 16.0, and few tiles (4096 x 512) 8.7 and 9.0.
     const bool wide = a.act != SP24_ACT_NONE && a.M * a.N >= (int64_t)1 << 22;
-    const sp24_status s = wide ? run_linear_grad<128>(a, st) : run_linear_grad<64>(a, st);
+    const sp24_status s = wide ? run_linear_grad<128, false>(a, st) : run_linear_grad<64, false>(a, st);
     if (s != SP24_OK || !a.dbias || a.M == 0) return s;
     return launch_column_sums(a.partial, (a.N + a.unit - 1) / a.unit, a.M, a.offsets, a.offsets ? a.experts : 1, a.unit, a.dbias, st);
 }

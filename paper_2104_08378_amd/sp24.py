@@ -102,11 +102,11 @@ def lib():
         L.sp24_checkpoint_rows.argtypes = [vp] * 3 + [i64] * 4 + [i32, i32, vp]
         L.sp24_restore_rows.argtypes = [vp] * 4 + [i64, i64, i32, i64, i64, i64, i32, i32, i32, vp]
         L.sp24_linear_backward_checkpoint.argtypes = [vp] * 6 + [i64] * 6 + [i32, vp, i32, i32, i32, vp, st, vp]
-        L.sp24_checkpoint_workspace_bytes.argtypes = [i64, i64]
+        L.sp24_gemm_dense_checkpoint_workspace_bytes.argtypes = [i64, i64, i64, i32]
         L.sp24_gemm_dense_checkpoint.argtypes = [vp, i32, vp, vp, vp] + [i64] * 6 + [i32, i32, i32, vp, st, vp]
         L.sp24_gemm_dense_grouped_checkpoint.argtypes = [vp, i32] + [vp] * 5 + [i32] + [i64] * 4 + [i32] + [i64] * 3 + [i32, i32, i32, vp, st, vp]
         for name in ("sp24_rmsnorm_backward_workspace_bytes", "sp24_linear_backward_workspace_bytes", "sp24_moe_sort_workspace_bytes",
-                     "sp24_checkpoint_workspace_bytes"):
+                     "sp24_gemm_dense_checkpoint_workspace_bytes"):
             getattr(L, name).restype = st
         for name in ("sp24_rmsnorm", "sp24_quantize_rows", "sp24_rmsnorm_backward", "sp24_linear", "sp24_linear_backward", "sp24_moe_sort", "sp24_moe_gather",
                      "sp24_moe_combine", "sp24_moe_combine_backward", "sp24_linear_grouped", "sp24_gemm_dense_grouped", "sp24_moe_route", "sp24_moe_route_backward",
@@ -1085,9 +1085,9 @@ def _a_order(A):
     return A_KMAJOR, by_row
 
 
-def sp24_checkpoint_workspace_bytes(rows, H):
-    """Bytes of workspace that the product from ``rows`` kept rows of H values needs."""
-    return lib().sp24_checkpoint_workspace_bytes(rows, H)
+def sp24_gemm_dense_checkpoint_workspace_bytes(M, N, K, grouped=False):
+    """Bytes of workspace that the product M x N from K kept rows needs."""
+    return lib().sp24_gemm_dense_checkpoint_workspace_bytes(M, N, K, int(grouped))
 
 
 def sp24_gemm_dense_checkpoint(A, checkpoint, out_dtype, out=None, workspace=None):
@@ -1103,7 +1103,7 @@ def sp24_gemm_dense_checkpoint(A, checkpoint, out_dtype, out=None, workspace=Non
     if A.shape[1] != K:
         raise ValueError("inner dimensions differ")
     D = _out(out, (M, N), out_dtype, A.device)
-    ws, ws_bytes = _scratch(workspace, sp24_checkpoint_workspace_bytes(K, N), A.device)
+    ws, ws_bytes = _scratch(workspace, sp24_gemm_dense_checkpoint_workspace_bytes(M, N, K), A.device)
     _check(lib().sp24_gemm_dense_checkpoint(A.data_ptr(), order, codes.data_ptr(), scale.data_ptr(), D.data_ptr(), M, N, K, lda, _ld(codes), _ld(D), _DT[A.dtype],
                                             _DT[codes.dtype], _DT[out_dtype], _ptr(ws), ws_bytes, _stream()), "sp24_gemm_dense_checkpoint")
     return D
@@ -1125,7 +1125,7 @@ def sp24_gemm_dense_grouped_checkpoint(A, checkpoint, offsets, out_dtype, rows=N
     D = torch.empty((max(experts, 0), M, N), dtype=out_dtype, device=A.device) if out is None else out
     if out is not None and (tuple(_dev(D, "out").shape) != (experts, M, N) or D.dtype != out_dtype or not D.is_contiguous()):
         raise ValueError("out must be a contiguous tensor [experts, M, N] of out_dtype")
-    ws, ws_bytes = _scratch(workspace, sp24_checkpoint_workspace_bytes(R, N), A.device)
+    ws, ws_bytes = _scratch(workspace, sp24_gemm_dense_checkpoint_workspace_bytes(M, N, R, True), A.device)
     _check(lib().sp24_gemm_dense_grouped_checkpoint(A.data_ptr(), order, codes.data_ptr(), scale.data_ptr(), _vector(rows, R, "rows", torch.int32), D.data_ptr(),
                                                     _vector(offsets, experts + 1, "offsets", torch.int32), experts, M, N, R, tokens, topk, lda, _ld(codes), N,
                                                     _DT[A.dtype], _DT[codes.dtype], _DT[out_dtype], _ptr(ws), ws_bytes, _stream()),

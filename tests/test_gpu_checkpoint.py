@@ -163,6 +163,23 @@ def test_gradient_through_the_activation(N, M, act, dtype, code):
             ref.close(b2[e], want[a:b].sum(0), err[a:b].sum(0) + want[a:b].abs().sum(0) * (N + 4) * 2.0 ** -24, "db")
 
 
+@pytest.mark.parametrize("N,experts", [(16, 1), (32, 7), (64, 32), (64, 33), (48, 200), (80, 4)])
+def test_bias_gradients_of_few_rows(N, experts):
+    """One tile of rows, whose sums need no second launch, and its neighbours; rows behind the last segment are nobody's."""
+    g = torch.Generator().manual_seed(N + experts)
+    M = 200
+    dy, c = torch.randn(N, M, generator=g).to(BF16), kept(torch.randn(N, M, generator=g), I8)
+    ends = sorted(torch.randint(0, N // 16 + 1, (experts,), generator=g).tolist())
+    offsets = torch.tensor([0] + [16 * e for e in ends], dtype=torch.int32, device="cuda")
+    want = ref.d(dy) * ref.slope(routing_ref.stands_for(*c), "gelu")
+    err = ref.d(dy).abs() * (14 * 2.0 ** -24) * (1 + routing_ref.stands_for(*c).abs())
+    db = sp24.sp24_linear_backward_checkpoint(dy.cuda(), c, "gelu", offsets=offsets)[2]
+    o = offsets.tolist()
+    for e in range(experts):
+        part = slice(o[e], o[e + 1])
+        ref.close(db[e], want[part].sum(0), err[part].sum(0) + want[part].abs().sum(0) * (N + 4) * 2.0 ** -24, str(e))
+
+
 def test_gradient_through_a_large_activation():
     """The tiles of large matrices."""
     g = torch.Generator().manual_seed(2)
@@ -196,7 +213,7 @@ def product(M, N, K, dtype, code, out, spare=0, c_spare=0, c_offset=0):
     # the transpose of the tokens' rows, NaN behind them: the same products, added in another order
     rows = torch.full((K, -(-M // 8) * 8 + spare), NAN, dtype=dtype, device="cuda")[:, :M]
     rows.copy_(a.t())
-    D = sp24.sp24_gemm_dense_checkpoint(rows.t(), c, out, workspace=torch.full((K * (-(-N // 8) * 8),), NAN, dtype=dtype, device="cuda"))
+    D = sp24.sp24_gemm_dense_checkpoint(rows.t(), c, out, workspace=torch.full((sp24.sp24_gemm_dense_checkpoint_workspace_bytes(M, N, K) // 2,), NAN, dtype=dtype, device="cuda"))
     ref.close(D, ref.d(a) @ b, (ref.d(a).abs() @ b.abs()) * ((K + 4) * 2.0 ** -24), str((M, N, K, dtype, code, out)))
     assert torch.equal(sp24.sp24_gemm_dense_checkpoint(rows.t(), c, out, out=target), D)
 
@@ -218,7 +235,8 @@ def test_weights_gradient_of_any_size(M, N, c_spare, c_offset, dtype, code):
         product(M, N, K, dtype, code, F32 if K % 2 else dtype, 0, c_spare, c_offset)
 
 
-@pytest.mark.parametrize("M,N,K", [(4096, 1024, 200), (4096, 2304, 136), (2304, 2048, 72), (1024, 8192, 330), (8192, 640, 77), (512, 512, 2000)])
+@pytest.mark.parametrize("M,N,K", [(4096, 1024, 200), (4096, 2304, 136), (2304, 2048, 72), (1024, 8192, 330), (8192, 640, 77), (512, 512, 2000),
+                                   (500, 500, 5005), (1000, 1030, 3000), (1500, 1001, 4100), (128, 40, 9001), (2048, 1024, 4160)])
 def test_weights_gradient_on_every_tile(M, N, K):
     product(M, N, K, BF16, I8, BF16)
     product(M, N, K, F16, F8, F32)

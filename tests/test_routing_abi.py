@@ -78,7 +78,11 @@ def test_linear_backward():
 def test_products():
     L = sp24.lib()
     W, BIG = 7 * STEP, 1 << 28
-    assert L.sp24_checkpoint_workspace_bytes(37, 61) == 37 * 64 * 2 and L.sp24_checkpoint_workspace_bytes(0, 64) == 0 and L.sp24_checkpoint_workspace_bytes(8, 0) == 0
+    size = L.sp24_gemm_dense_checkpoint_workspace_bytes
+    assert size(64, 61, 37, 0) == 37 * 64 * 2 and size(64, 61, 32, 1) == 32 * 64 * 2 and size(64, 64, 0, 0) == 0 and size(0, 64, 8, 0) == 0 and size(64, 0, 8, 0) == 0 and size(64, 64, -1, 0) == 0
+    assert size(512, 510, 8192, 1) == 8192 * 512 * 2                   # (segments are not split)
+    split = size(512, 510, 8192, 0) - 8192 * 512 * 2
+    assert split % (512 * 512 * 4) == 0 and 2 <= split // (512 * 512 * 4) <= 16 and size(4096, 1024, 8192, 0) == 8192 * 1024 * 2
 
     def plain(a=A, c=B, s=C, d=D, M=64, N=64, K=37, lda=40, ldc=64, ldd=64, i=sp24.BF16, code=sp24.I8, o=sp24.F32, order=0, ws=W, bytes=BIG):
         return L.sp24_gemm_dense_checkpoint(a, order, c, s, d, M, N, K, lda, ldc, ldd, i, code, o, ws, bytes, None)
