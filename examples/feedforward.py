@@ -5,6 +5,7 @@
 ``QuantisedBlock``  norm and 8-bit rows in one pass, up-projection with its activation, 8-bit rows again, down-projection onto the residual stream
 ``Experts``         one projection of every expert: pruned so that the transposed weights satisfy the pattern too, forward, gradients, update
 ``ExpertBlock``     norm, tokens sorted to their experts, both projections, and back onto the residual stream; its gradients
+``RoutedBlock``     the same behind a router of its own, with everything that the gradients need kept in 8 bits
 """
 import os
 import sys
@@ -94,6 +95,45 @@ class ExpertBlock:
         return dict(x=dx, norm=dnorm, up=dup, down=ddown, bias=dbias.reshape(-1), weights=dweights)
 
 
+class RoutedBlock(ExpertBlock):
+    """Keeps a byte, not two, for every value of the rows in front of and behind the activation, of the experts' results, and of the normed rows, which are
+    kept once a token, whatever the number of its experts."""
+
+    def __init__(self, norm, up, down, bias, router, experts, topk, **routing):
+        super().__init__(norm, up, down, bias, experts)
+        self.router, self.topk, self.routing = router.to(torch.bfloat16), topk, routing
+
+    def __call__(self, x, stream, balance=None):
+        """(the new residual stream, how many choices every expert has, what the gradients need).  balance [experts]: added to the scores for the choice."""
+        n = sp24.sp24_rmsnorm(x, self.norm, residual=stream, want_rstd=True)
+        logits = sp24.sp24_gemm_dense(n.y, self.router, torch.float32)
+        r = sp24.sp24_moe_route(logits, self.topk, bias=balance, want_load=True, **self.routing)
+        offsets, slots, rows = sp24.sp24_moe_sort(r.ids, self.experts)
+        z = torch.empty(rows.numel(), self.up.V.shape[0] // self.experts, dtype=torch.bfloat16, device=x.device)
+        h = self.up(sp24.sp24_moe_gather(n.y, rows, self.topk), offsets, bias=self.bias, act="gelu", preact=z)
+        ys = self.down(h, offsets)
+        out = sp24.sp24_moe_combine(ys, slots, r.weights, residual=n.hidden)
+        return out, r.load, (n.hidden, n.rstd, logits, r, offsets, slots, rows, *(sp24.sp24_checkpoint_rows(t) for t in (n.y, z, h, ys)))
+
+    def backward(self, dout, kept):
+        hidden, rstd, logits, r, offsets, slots, rows, y, z, h, ys = kept
+        how = {k: v for k, v in self.routing.items() if k in ("score", "renormalise", "scale")}
+        dys, dweights = sp24.sp24_moe_combine_backward(dout, sp24.sp24_restore_rows(ys, torch.bfloat16), slots, rows, r.weights)
+        ddown = sp24.sp24_gemm_dense_grouped_checkpoint(dys.t(), h, offsets, torch.bfloat16).view(self.down.master.shape)
+        dh = sp24.sp24_linear_grouped(self.down.Vt, self.down.meta_t, dys, offsets, torch.bfloat16, layout="tiled")
+        dz, dzt, dbias = sp24.sp24_linear_backward_checkpoint(dh, z, "gelu", offsets=offsets)
+        dup = sp24.sp24_gemm_dense_grouped_checkpoint(dzt, y, offsets, torch.bfloat16, rows=rows, topk=self.topk).view(self.up.master.shape)
+        dxs = sp24.sp24_linear_grouped(self.up.Vt, self.up.meta_t, dz, offsets, torch.bfloat16, layout="tiled")
+        # the router's rows are as wide as there are experts; the products ask for whole 16 bytes
+        dl = torch.zeros(logits.shape[0], -(-self.experts // 8) * 8, dtype=torch.bfloat16, device=logits.device)[:, :self.experts]
+        dl.copy_(sp24.sp24_moe_route_backward(logits, r.ids, dweights, **how))
+        drouter = sp24.sp24_gemm_dense_checkpoint(dl.t(), y, torch.float32)
+        dy = sp24.sp24_moe_combine(dxs, slots, residual=sp24.sp24_gemm_dense(dl, self.router, torch.bfloat16, b_order="n"))
+        dx, dnorm = sp24.sp24_rmsnorm_backward(dy, hidden, self.norm, rstd, dhidden=dout)
+        return dict(x=dx, norm=dnorm, up=sp24.sp24_mask_apply(dup, self.up.meta, layout="tiled"), down=sp24.sp24_mask_apply(ddown, self.down.meta, layout="tiled"),
+                    bias=dbias.reshape(-1), router=drouter)
+
+
 def decode(g, H=1024, F=4096, tokens=16):
     """Relative distance of the 8-bit block from the same weights in float32."""
     n = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
@@ -128,7 +168,22 @@ def fine_tune(g, H=256, F=512, experts=8, topk=2, tokens=512, steps=12, rate=0.5
     return losses
 
 
+def balance(g, H=256, F=512, experts=8, topk=2, tokens=512, steps=8, rate=0.02):
+    """The largest share of the choices that one expert has, step by step, while the bias follows the load."""
+    n = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    block = RoutedBlock(1 + 0.1 * n(H), n(experts * F, H) / H ** 0.5, n(experts * H, F) / F ** 0.5, 0.1 * n(experts * F), n(experts, H) / H ** 0.5, experts, topk,
+                        score="sigmoid", groups=4, groups_kept=2, scale=2.0)
+    x, stream = n(tokens, H).to(torch.bfloat16) + 0.5 * n(H).to(torch.bfloat16), n(tokens, H).to(torch.bfloat16)
+    bias, shares = torch.zeros(experts, device="cuda"), []
+    for _ in range(steps):
+        load = block(x, stream, bias)[1].float()
+        shares.append(float(load.max() / load.sum()))
+        bias += rate * torch.sign(load.mean() - load)
+    return shares
+
+
 if __name__ == "__main__":
     generator = torch.Generator(device="cuda").manual_seed(0)
     print("decoding in 8 bits against float32, relative distance: %.4f" % decode(generator))
     print("fine-tuning experts, loss by step: " + " ".join("%.4f" % v for v in fine_tune(generator)))
+    print("balancing experts, largest share by step: " + " ".join("%.3f" % v for v in balance(generator)))
