@@ -20,15 +20,16 @@ constexpr int kFewExperts = 32;         // whose segments four groups of threads
 
 // ZT: what Z is held in, the values' type or codes with a scale for each block of 128.  FEW: there is one tile of rows, and the sums need no
 // second launch: they are added sixteen rows at a time, in row order.
-template <int T, int ZT, int WIDTH, bool FEW>
-__global__ __launch_bounds__(4 * WIDTH) void k_linear_grad(LinearGradArgs a, int tiles_m, unsigned from)
+template <int T, int ZT, int WIDTH, int ROWS, bool FEW>
+__global__ __launch_bounds__(ROWS * WIDTH / 16) void k_linear_grad(LinearGradArgs a, int tiles_m, unsigned from)
 {
     constexpr int kPitch = WIDTH + 1, CH = WIDTH / 8;
-    __shared__ float tile[kGradTile * kPitch];
-    __shared__ float part[4][WIDTH];
+    constexpr int kAtOnce = ROWS / 2;                                  // rows that the threads load together
+    __shared__ float tile[ROWS * kPitch];
+    __shared__ float part[ROWS / 16][WIDTH];
     const int tid = threadIdx.x;
     const unsigned at = from + blockIdx.x;
-    const int64_t m0 = (int64_t)(at % tiles_m) * WIDTH, n0 = (int64_t)(at / tiles_m) * kGradTile;
+    const int64_t m0 = (int64_t)(at % tiles_m) * WIDTH, n0 = (int64_t)(at / tiles_m) * ROWS;
     const int c = tid % CH;
     const int64_t m = m0 + c * 8;
     const int have = (int)min(a.M - m, (int64_t)8);
@@ -37,7 +38,7 @@ __global__ __launch_bounds__(4 * WIDTH) void k_linear_grad(LinearGradArgs a, int
     float scale[2] = {};
 #pragma unroll
     for (int it = 0; it < 2; ++it) {
-        const int64_t n = n0 + it * 32 + tid / CH;
+        const int64_t n = n0 + it * kAtOnce + tid / CH;
         if (n < a.N && have > 0) {
             dy[it] = load_raw8<T>(a.dY, n * a.lddy + m, have);
             if (a.act != SP24_ACT_NONE) {
@@ -50,7 +51,7 @@ __global__ __launch_bounds__(4 * WIDTH) void k_linear_grad(LinearGradArgs a, int
     }
 #pragma unroll
     for (int it = 0; it < 2; ++it) {
-        const int t = it * 32 + tid / CH;
+        const int t = it * kAtOnce + tid / CH;
         float v[8], x[8];
         values_of<T>(dy[it], v);
         if (a.act != SP24_ACT_NONE) {
@@ -67,7 +68,7 @@ __global__ __launch_bounds__(4 * WIDTH) void k_linear_grad(LinearGradArgs a, int
     if (a.dZt) {
 #pragma unroll
         for (int it = 0; it < 2; ++it) {
-            const int f = it * (WIDTH / 2) + (tid >> 3), t = (tid & 7) * 8;
+            const int f = it * (WIDTH / 2) + tid / (ROWS / 8), t = tid % (ROWS / 8) * 8;
             const int rows = (int)min(a.N - n0 - t, (int64_t)8);
             if (m0 + f >= a.M || rows <= 0) continue;
             float v[8];
@@ -85,9 +86,11 @@ __global__ __launch_bounds__(4 * WIDTH) void k_linear_grad(LinearGradArgs a, int
         __syncthreads();
         if (m0 + f >= a.M) return;
         if (!a.offsets) {
-            if (p == 0) a.dbias[m0 + f] = ((part[0][f] + part[1][f]) + part[2][f]) + part[3][f];
+            float total = 0.0f;
+            for (int k = 0; p == 0 && k < ROWS / 16; ++k) total += part[k][f];
+            if (p == 0) a.dbias[m0 + f] = total;
         } else {
-            for (int e = p; e < a.experts; e += 4) {
+            for (int e = p; e < a.experts; e += ROWS / 16) {
                 int64_t from_row, to_row;
                 segment_of(a.offsets, e, a.N, from_row, to_row);
                 float total = 0.0f;
@@ -106,21 +109,22 @@ __global__ __launch_bounds__(4 * WIDTH) void k_linear_grad(LinearGradArgs a, int
         } else {
             part[p][f] = sum;
             __syncthreads();
-            if (p == 0 && m0 + f < a.M) a.partial[n0 / kGradTile * a.M + m0 + f] = ((part[0][f] + part[1][f]) + part[2][f]) + part[3][f];
+            if (p == 0 && m0 + f < a.M) a.partial[n0 / ROWS * a.M + m0 + f] = ((part[0][f] + part[1][f]) + part[2][f]) + part[3][f];
         }
     }
 }
 
-template <int WIDTH, bool FEW>
+template <int WIDTH, int ROWS, bool FEW>
 static sp24_status run_linear_grad(const LinearGradArgs& a, hipStream_t st)
 {
-    const int64_t tiles_m = (a.M + WIDTH - 1) / WIDTH, tiles_n = (a.N + kGradTile - 1) / kGradTile;
-    return launch_in_parts(tiles_m * tiles_n, 4 * WIDTH, [&](unsigned from, unsigned grid) {
+    const int64_t tiles_m = (a.M + WIDTH - 1) / WIDTH, tiles_n = (a.N + ROWS - 1) / ROWS;
+    constexpr int kThreads = ROWS * WIDTH / 16;
+    return launch_in_parts(tiles_m * tiles_n, kThreads, [&](unsigned from, unsigned grid) {
         auto run = [&](auto t) {
             constexpr int T = decltype(t)::value;
-            if (a.zcode == SP24_I8) k_linear_grad<T, SP24_I8, WIDTH, FEW><<<grid, 4 * WIDTH, 0, st>>>(a, (int)tiles_m, from);
-            else if (a.zcode == SP24_F8) k_linear_grad<T, SP24_F8, WIDTH, FEW><<<grid, 4 * WIDTH, 0, st>>>(a, (int)tiles_m, from);
-            else if constexpr (!FEW) k_linear_grad<T, T, WIDTH, FEW><<<grid, 4 * WIDTH, 0, st>>>(a, (int)tiles_m, from);
+            if (a.zcode == SP24_I8) k_linear_grad<T, SP24_I8, WIDTH, ROWS, FEW><<<grid, kThreads, 0, st>>>(a, (int)tiles_m, from);
+            else if (a.zcode == SP24_F8) k_linear_grad<T, SP24_F8, WIDTH, ROWS, FEW><<<grid, kThreads, 0, st>>>(a, (int)tiles_m, from);
+            else if constexpr (!FEW) k_linear_grad<T, T, WIDTH, ROWS, FEW><<<grid, kThreads, 0, st>>>(a, (int)tiles_m, from);
         };
         if (a.t == SP24_F16) run(std::integral_constant<int, SP24_F16>{});
         else run(std::integral_constant<int, SP24_BF16>{});
@@ -129,13 +133,16 @@ static sp24_status run_linear_grad(const LinearGradArgs& a, hipStream_t st)
 
 sp24_status launch_linear_grad(const LinearGradArgs& a, hipStream_t st)
 {
-    // One tile of rows, Z kept in 8 bits (the sums beside a 16-bit Z keep their order, and with it their bits): 64 x 2048 5.9 -> 4.4 us, of segments 6.4 -> 5.4.  (All
-    // tiles of a column in one workgroup: 128 rows 7.1, against 6.1 with the second launch, 256 rows 12.4 against 6.2.)
-    if (a.zcode != a.t && a.dbias && a.N > 0 && a.N <= kGradTile && a.experts <= kFewExperts) return run_linear_grad<64, true>(a, st);
+    // One tile of 64, 128 or 256 rows, Z kept in 8 bits (the sums beside a 16-bit Z keep their order, and with it their bits): 64 x 2048 5.9 -> 4.1 us, 128 x 2048
+    // 6.1 -> 4.2, 256 x 2048 6.2 -> 5.3, of segments 6.4 -> 4.4, 6.5 -> 4.5 and 6.6 -> 5.7.  (Tiles of 64 one after the other in a workgroup: 128 rows 7.1, 256 rows 12.4.)
+    if (a.zcode != a.t && a.dbias && a.N > 0 && a.N <= 256 && a.experts <= kFewExperts) {
+        if (a.N <= 64) return run_linear_grad<64, 64, true>(a, st);
+        return a.N <= 128 ? run_linear_grad<64, 128, true>(a, st) : run_linear_grad<64, 256, true>(a, st);
+    }
     // Large ones with an activation, whose two operands come in rows of 256 bytes a tile then: 4096 x 4096 with GELU 35.6 -> 32.9 us.  Without
     // one 15.2 and 16.0, and few tiles (4096 x 512) 8.7 and 9.0.
     const bool wide = a.act != SP24_ACT_NONE && a.M * a.N >= (int64_t)1 << 22;
-    const sp24_status s = wide ? run_linear_grad<128, false>(a, st) : run_linear_grad<64, false>(a, st);
+    const sp24_status s = wide ? run_linear_grad<128, kGradTile, false>(a, st) : run_linear_grad<64, kGradTile, false>(a, st);
     if (s != SP24_OK || !a.dbias || a.M == 0) return s;
     return launch_column_sums(a.partial, (a.N + a.unit - 1) / a.unit, a.M, a.offsets, a.offsets ? a.experts : 1, a.unit, a.dbias, st);
 }

@@ -163,7 +163,7 @@ def test_gradient_through_the_activation(N, M, act, dtype, code):
             ref.close(b2[e], want[a:b].sum(0), err[a:b].sum(0) + want[a:b].abs().sum(0) * (N + 4) * 2.0 ** -24, "db")
 
 
-@pytest.mark.parametrize("N,experts", [(16, 1), (32, 7), (64, 32), (64, 33), (48, 200), (80, 4)])
+@pytest.mark.parametrize("N,experts", [(16, 1), (32, 7), (64, 32), (64, 33), (48, 200), (80, 4), (128, 8), (144, 30), (256, 16), (256, 33), (272, 5)])
 def test_bias_gradients_of_few_rows(N, experts):
     """One tile of rows, whose sums need no second launch, and its neighbours; rows behind the last segment are nobody's."""
     g = torch.Generator().manual_seed(N + experts)
@@ -178,6 +178,30 @@ def test_bias_gradients_of_few_rows(N, experts):
     for e in range(experts):
         part = slice(o[e], o[e + 1])
         ref.close(db[e], want[part].sum(0), err[part].sum(0) + want[part].abs().sum(0) * (N + 4) * 2.0 ** -24, str(e))
+
+
+@pytest.mark.parametrize("N,M", [(1, 5), (64, 200), (65, 72), (128, 130), (200, 64), (256, 300), (257, 40), (700, 520)])
+def test_both_forms_of_the_gradient_at_the_c_entry(N, M):
+    """dZ and its transpose, each alone and together, and the sums or not."""
+    g = torch.Generator().manual_seed(N + M)
+    dy, c = torch.randn(N, M, generator=g).to(BF16).cuda(), kept(torch.randn(N, M, generator=g), I8)
+    z = routing_ref.stands_for(*c)
+    want, err = ref.d(dy) * ref.slope(z, "silu"), ref.d(dy).abs() * (14 * 2.0 ** -24) * (1 + z.abs())
+    L, stream = sp24.lib(), torch.cuda.current_stream().cuda_stream
+    ws = torch.empty(L.sp24_linear_backward_workspace_bytes(M, N, 0), dtype=torch.uint8, device="cuda")
+    for with_dz, with_t, with_b in ((1, 1, 1), (0, 1, 0), (1, 0, 0), (0, 0, 1), (0, 1, 1), (1, 1, 0)):
+        dz, dzt, db = (torch.full(s, NAN, dtype=t, device="cuda") for s, t in (((N, M + 3), BF16), ((M, N + 5), BF16), ((M,), F32)))
+        status = L.sp24_linear_backward_checkpoint(dy.data_ptr(), c.codes.data_ptr(), c.scale.data_ptr(), dz.data_ptr() if with_dz else None,
+                                                   dzt.data_ptr() if with_t else None, db.data_ptr() if with_b else None, M, N, M, c.codes.stride(0), M + 3, N + 5, sp24.SILU,
+                                                   None, 0, sp24.I8, sp24.BF16, ws.data_ptr(), ws.numel(), stream)
+        assert status == 0
+        for there, got, expect, e in ((with_dz, dz[:, :M], want, err), (with_t, dzt[:, :N], want.t(), err.t()),
+                                      (with_b, db, want.sum(0), err.sum(0) + want.abs().sum(0) * (N + 4) * 2.0 ** -24)):
+            if there:
+                ref.close(got, expect, e, str((with_dz, with_t, with_b)))
+            else:
+                assert bool(torch.isnan(got).all())
+        assert bool(torch.isnan(dz[:, M:]).all()) and bool(torch.isnan(dzt[:, N:]).all())
 
 
 def test_gradient_through_a_large_activation():
