@@ -24,12 +24,16 @@ sp24_status gemm_tokens(const TokenArgs& a, int experts, hipStream_t st)
     }
     const int64_t cols = (a.N + 127) / 128, small = ((a.M + 127) / 128) * cols, tall = ((a.M + 255) / 256) * cols, big = ((a.M + 255) / 256) * ((a.N + 255) / 256);
     const bool covered = (double)big * 256 * 256 <= 1.35 * (double)small * 128 * 128;
-    // Segments: large tiles, whose fewer transfers and reads of LDS weigh more than the steps that a short segment's tile has to fill its stages (us, restoring
-    // included: eight of 2048 x 1024 from 8192 choices on 128 x 256 53.1, on 256 x 256 46.7; 32 of 1024 x 512 from 16384 39.4, 36.8; 16 of 1024 x 1024 from
-    // 2048 20.2, 19.2); half as large ones where they make too few, and columns of 128 where wider ones are mostly padding.
+    // Segments, which the router makes of any length: the longest one's tiles end last, so tiles of 256 x 256, whose longest takes twice as long, are a tenth faster
+    // where all are alike and a third slower where not.  us, restoring included, eight of 2048 x 1024 from 8192 choices, alike and the longest 1.6 and 3 times the
+    // mean: 256 x 256 46, 61, 73; 128 x 256 50, 50, 50; 128 x 128 58, 56, 56; 64 of 1024 x 512 from 16384, alike and not: 47 and 60 to 84, 50 and 52 to 65.  (The longest
+    // first: 0.98 to 1.02 times as long with eight, 0.85 with 64 uneven ones, 1.0 to 1.08 with even ones.)
+    // Few tiles: half as large ones, four stages deep.  Eight of 512 x 512 from 8192 24.5 -> 19.5, uneven 41 -> 29; eight of 1024 x 512 24.6 -> 22.9, 40 -> 30;
+    // four of 1024 x 1024 34.1 -> 33.6, 40 -> 36; but (256 tiles) 16 of 1024 x 512 from 1024 10.5 -> 12.4.  Columns of 128 too where wider ones are mostly padding.
     if (a.offsets) {
-        if (big * experts >= 129 && covered) return run(k_gemm_pipe<DT, OUT, 4, 2, 2, 4, 2, 2, TokenArgs>, 256, 256, 512, experts);
-        if ((a.N + 255) / 256 * 256 * 4 > (a.N + 127) / 128 * 128 * 5) return run(k_gemm_pipe<DT, OUT, 4, 2, 1, 2, 2, 2, TokenArgs>, 128, 128, 512, experts);
+        const int64_t wide = (a.N + 255) / 256;
+        if ((a.M + 127) / 128 * wide * experts <= 128) return run(k_gemm_pipe<DT, OUT, 2, 4, 2, 1, 4, 2, TokenArgs>, 128, 128, 512, experts);
+        if (wide * 256 * 4 > cols * 128 * 5) return run(k_gemm_pipe<DT, OUT, 4, 2, 1, 2, 2, 2, TokenArgs>, 128, 128, 512, experts);
         return run(k_gemm_pipe<DT, OUT, 2, 4, 2, 2, 3, 2, TokenArgs>, 128, 256, 512, experts);
     }
     // All tokens: the tile whose workgroups still find a unit each, as for the product of an M x K operand (us, restoring included): 512 x 512 x 8192 on 64 x 64
