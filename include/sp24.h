@@ -606,7 +606,7 @@ sp24_status sp24_moe_route(const void* logits, const float* bias, int32_t* ids, 
 
 /*
  * Its gradient: dlogits (N x experts of type t, may be logits in place) from dweights (N x topk) and dscores (N x experts floats, contiguous; NULL: none),
- * the choice being held.  ids as sp24_moe_route wrote them; an entry outside 0 .. experts - 1 has no part, one that is there twice has both.
+ * the choice being held.  ids as sp24_moe_route wrote them (topk <= experts); an entry outside 0 .. experts - 1 has no part, one that is there twice has both.
  *   g[e] = dscores[e] + sum over j of [ids[j] = e] h[j],  h = scale * dweights, renormalised scale * (dweights - sum(dweights s) / W) / W,  W = sum s (0: h = 0)
  *   softmax: dlogits = s (g - sum g s);  sigmoid: dlogits = s (1 - s) g;  0 where the logit is -inf
  */

@@ -423,7 +423,8 @@ sp24_status sp24_moe_route_backward(const void* logits, const int32_t* ids, cons
                                     void* stream)
 {
     if (!is_float(t) || !is_score(score)) return SP24_ERR_DTYPE;
-    if (N < 0 || N > kMostRows || experts < 1 || experts > SP24_MOST_EXPERTS || topk < 1 || topk > SP24_MOST_CHOICES || !std::isfinite(scale)) return SP24_ERR_SHAPE;
+    if (N < 0 || N > kMostRows || experts < 1 || experts > SP24_MOST_EXPERTS || !std::isfinite(scale)) return SP24_ERR_SHAPE;
+    if (topk < 1 || topk > SP24_MOST_CHOICES || topk > experts) return SP24_ERR_SHAPE;
     if (N == 0) return SP24_OK;
     const int es = esize_of(t);
     SP24_TRY(check_matrix(logits, N, experts, ldl, es, false));

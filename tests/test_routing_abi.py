@@ -34,7 +34,7 @@ def back(l=A, ids=B, dw=C, ds=D, out=E, N=8, n=64, k=4, score=0, renorm=1, scale
 @pytest.mark.parametrize("bad,want", [
     (dict(l=0), NULL), (dict(ids=0), NULL), (dict(dw=0), NULL), (dict(out=0), NULL), (dict(l=A + 1), ALIGN), (dict(ds=D + 2), ALIGN), (dict(out=E + 2), ALIGN), (dict(ldl=60), SHAPE),
     (dict(ldo=60), SHAPE), (dict(n=0), SHAPE), (dict(n=1025, ldl=2000, ldo=2000), SHAPE), (dict(k=0), SHAPE), (dict(k=65), SHAPE), (dict(scale=INF), SHAPE), (dict(score=-1), DTYPE),
-    (dict(t=sp24.F8), DTYPE), (dict(out=A + 4), SHAPE), (dict(out=A, ldo=72), SHAPE), (dict(out=B), SHAPE), (dict(out=C), SHAPE), (dict(out=D), SHAPE), (dict(N=0, l=0), OK)])
+    (dict(t=sp24.F8), DTYPE), (dict(n=3, k=4), SHAPE), (dict(n=8, k=9), SHAPE), (dict(n=8, k=64), SHAPE), (dict(out=A + 4), SHAPE), (dict(out=A, ldo=72), SHAPE), (dict(out=B), SHAPE), (dict(out=C), SHAPE), (dict(out=D), SHAPE), (dict(N=0, l=0), OK)])
 def test_route_backward(bad, want):
     assert back(**bad) == want
 
