@@ -288,7 +288,8 @@ def segments(g, lengths, spare_rows):
 @pytest.mark.parametrize("code", [I8, F8])
 @pytest.mark.parametrize("dtype", [F16, BF16])
 @pytest.mark.parametrize("M,N,lengths,spare", [(40, 56, [16], 0), (128, 128, [0, 16, 0, 32, 0], 16), (200, 264, [48, 0, 80, 160], 0), (256, 136, [64, 128, 16], 64), (70, 45, [0, 0], 0),
-                                               (300, 520, [336, 16, 0, 208], 32), (1024, 1024, [112, 400], 0)])
+                                               (300, 520, [336, 16, 0, 208], 32), (1024, 1024, [112, 400], 0),
+                                               (1100, 1032, [48, 0, 80, 160, 16], 16), (1100, 264, [16, 64, 0, 32] * 4, 0)])
 def test_experts_weights_gradient(M, N, lengths, spare, dtype, code):
     g = torch.Generator().manual_seed(M + N)
     offsets, R = segments(g, lengths, spare)
@@ -345,3 +346,53 @@ def test_rows_far_into_the_codes():
     dy = torch.randn(K, N, generator=g).to(BF16).cuda()
     for p, q in zip(sp24.sp24_linear_backward_checkpoint(dy, far, "gelu"), sp24.sp24_linear_backward_checkpoint(dy, near, "gelu")):
         assert torch.equal(p, q)
+
+
+@pytest.mark.parametrize("M,N", [(70, 45), (200, 264), (1100, 1032)])
+def test_segments_keep_to_themselves(M, N):
+    """Segments that end inside a step of the products, between rows that are not finite in both operands."""
+    lengths = [16, 48, 80, 16, 112, 16]
+    g = torch.Generator().manual_seed(N)
+    offsets, R = segments(g, lengths, 48)
+    o = offsets.tolist()
+    A, x = torch.randn(R, M, generator=g).to(BF16), rows_of(g, R, N, BF16)
+    bad = torch.zeros(R, dtype=torch.bool)
+    for e in (0, 2, 4):
+        bad[o[e]:o[e + 1]] = True
+    bad[o[-1]:] = True
+    A[bad], x[bad] = NAN, INF
+    c = sp24.sp24_checkpoint_rows(x.cuda(), I8)
+    b = rounded(routing_ref.stands_for(*(t.cpu() for t in c)), BF16)
+    for a in (torch.nn.functional.pad(A, (0, -M % 8)).cuda()[:, :M].t(), torch.nn.functional.pad(A.t(), (0, 8)).cuda()[:, :R]):
+        for rows in (None, torch.arange(R, dtype=torch.int32, device="cuda")):
+            D = sp24.sp24_gemm_dense_grouped_checkpoint(a, c, offsets, F32, rows=rows)
+            for e in (1, 3, 5):
+                ae, be = ref.d(A)[o[e]:o[e + 1]].t(), b[o[e]:o[e + 1]]
+                ref.close(D[e], ae @ be, (ae.abs() @ be.abs()) * ((R + 4) * 2.0 ** -24), str((M, N, e)))
+            assert bool(torch.isnan(D[[0, 2, 4]]).all())
+
+
+def test_operands_past_32_bits():
+    """dZ and restored rows of more than 2^32 bytes, of which only some rows are not zero: the last among them."""
+    M, N, K = 8192, 8320, 300000
+    g = torch.Generator().manual_seed(9)
+    some = torch.tensor([0, 1, 70000, 131072, 262143, 262144, 299990, K - 1])
+    dz, x = torch.zeros(K, M, dtype=BF16, device="cuda"), torch.zeros(K, N, dtype=BF16, device="cuda")
+    a, b = torch.randn(len(some), M, generator=g).to(BF16), rows_of(g, len(some), N, BF16)
+    dz[some.cuda()], x[some.cuda()] = a.cuda(), b.cuda()
+    c = sp24.sp24_checkpoint_rows(x, I8)
+    few = sp24.sp24_checkpoint_rows(b.cuda(), I8)
+    assert torch.equal(c.codes[some.cuda()], few.codes) and torch.equal(c.scale[some.cuda()], few.scale)
+    del x
+    kept_b = rounded(routing_ref.stands_for(*(t.cpu() for t in few)), BF16)
+    at = torch.randint(0, M, (64,), generator=g)
+    want, sums = ref.d(a)[:, at].t() @ kept_b, ref.d(a)[:, at].abs().t() @ kept_b.abs()
+    offsets = torch.tensor([0, 131072, K // 16 * 16], dtype=torch.int32, device="cuda")
+    D = sp24.sp24_gemm_dense_checkpoint(dz.t(), c, F32)
+    ref.close(D[at.cuda()], want, sums * (12 * 2.0 ** -24), "all tokens")
+    D = sp24.sp24_gemm_dense_grouped_checkpoint(dz.t(), c, offsets, F32)
+    ref.close(D.double().sum(0).float()[at.cuda()], want, sums * (12 * 2.0 ** -24), "two segments")
+    back = sp24.sp24_restore_rows(c, BF16)
+    assert torch.equal(back[some.cuda()].cpu(), kept_b.to(BF16)) and int((back != 0).any(1).sum()) == len(some)
+    dZ, _, db = sp24.sp24_linear_backward_checkpoint(back, c, "relu")
+    assert torch.equal(dZ[some.cuda()].cpu(), torch.where(routing_ref.stands_for(*(t.cpu() for t in few)) > 0, kept_b, 0.0).to(BF16))
