@@ -7,11 +7,10 @@
 // All in binary64: of 10^5 tokens' experts some pairs' scores are within a rounding of binary32 of each other, and which one is chosen must
 // not hang on the order of a sum.
 //
-// Bound by vector operations, three quarters of the time busy with them: an exponential of some 30 in binary64 for every logit, and for every choice one
-// comparison a value and a reduction over the row's lanes.  Few rows: a launch and one row's chain of them.  In a graph, us: 16 rows, four of 64 experts 3.0; 8192 rows, six of
-// 64 4.7, eight of 256 11.3, by logistic scores with bias out of four of eight groups 11.9 (1.4 is what their 8.9 MB take); 2048 rows of 1024 10.9; the gradient of
-// 8192 rows of 256 with that of the scores 11.5 (25 MB: 4.1).  (Choosing by keys rounded to binary32, and in full where two are the same there: 0.95 to 1.03
-// times as long for binary32 logits, 1.05 for bf16 ones, which are the same more often.)
+// Bound by vector operations, three quarters of the time busy with them: an exponential of some 35 in binary64 for every logit, and for every choice the
+// reduction over the row's lanes and a search in the one that has it.  Few rows: a launch and one row's chain of them.  In a graph, us: 16 rows, four of 64 experts
+// 2.9; 8192 rows, six of 64 4.5, eight of 256 9.8, by logistic scores with bias out of four of eight groups 10.6 (1.4 is what their 8.9 MB take); 2048 rows of
+// 1024 10.0; the gradient of 8192 rows of 256 with that of the scores 11.5 (25 MB: 4.1).
 #include <algorithm>
 
 #include "launch.hpp"
@@ -55,6 +54,36 @@ __device__ __forceinline__ double over_row(double v, OP op)
     if constexpr (L >= 16) v = op(v, dpp_of<0x140>(v));          // the other half of sixteen
     if constexpr (L >= 32) v = over_halves<false>(v, op);
     if constexpr (L >= 64) v = over_halves<true>(v, op);
+    return v;
+}
+template <int L>
+__device__ __forceinline__ uint32_t most_of_row(uint32_t v)
+{
+    if constexpr (L >= 2) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, true));
+    if constexpr (L >= 4) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, true));
+    if constexpr (L >= 8) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xF, 0xF, true));
+    if constexpr (L >= 16) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xF, 0xF, true));
+    if constexpr (L >= 32) {
+        const auto h = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        v = max(h[0], h[1]);
+    }
+    if constexpr (L >= 64) {
+        const auto h = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        v = max(h[0], h[1]);
+    }
+    return v;
+}
+// bits of a number (no NaN) as a whole one of the same order
+__device__ __forceinline__ uint32_t in_order(float v)
+{
+    const uint32_t b = __float_as_uint(v);
+    return b ^ ((uint32_t)((int)b >> 31) | 0x80000000u);
+}
+// The larger of two that are no NaN: the compiler's own has each quieted first, an operation each.
+__device__ __forceinline__ double larger(double a, double b)
+{
+    double v;
+    asm("v_max_f64 %0, %1, %2" : "=v"(v) : "v"(a), "v"(b));
     return v;
 }
 struct larger_of { __device__ __forceinline__ double operator()(double a, double b) const { return __builtin_fmax(a, b); } };
@@ -114,6 +143,7 @@ __device__ __forceinline__ void store_run(void* p, int64_t i, int have, const fl
 }
 
 constexpr double kNever = -__builtin_inf();
+constexpr uint32_t kChosen = 0xFFEFFFFFu;                        // upper half of -1.8e308
 
 // The scores of a row's experts, 0 for those whose logit is -inf, and (rest) 1 - s of a logistic one without the difference.  A NaN (or, softmax,
 // +inf) makes NaN of what it takes part in.  Exponents are 0 and less.
@@ -250,19 +280,43 @@ __global__ __launch_bounds__(kRouteThreads) void k_route(RouteArgs a, unsigned f
 #pragma unroll
         for (int i = 0; i < V; ++i) key[i] = keys[r][i * L + l];
     }
+    // One after the other.  The row's largest is found by the lanes' best rounded to binary32, which keeps their order and takes one operation a step; where
+    // two lanes are the same there, by all bits (reductions in binary64 always: 8192 rows, eight of 256, 11.2 us for 9.8, bf16 logits, which are often the same, 11.1
+    // for 10.0).  A chosen one's upper half becomes that of a number below all others (the lower stays, so it is one word).
+    uint32_t upper[V], lower[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const uint64_t bits = __builtin_bit_cast(uint64_t, key[i]);
+        upper[i] = (uint32_t)(bits >> 32);
+        lower[i] = (uint32_t)bits;
+    }
+    auto value = [&](int i) { return __builtin_bit_cast(double, ((uint64_t)upper[i] << 32) | lower[i]); };
+    auto lane_best = [&] {
+        double best = value(0);
+#pragma unroll
+        for (int i = 1; i < V; ++i) best = larger(best, value(i));
+        return best;
+    };
+    double best = lane_best();
     for (int j = 0; j < a.topk; ++j) {
-        double best = key[0];
-#pragma unroll
-        for (int i = 1; i < V; ++i) best = __builtin_fmax(best, key[i]);
-        const double most = over_row<L>(best, larger_of{});
-        const uint64_t have = __ballot(best == most) >> ((threadIdx.x & 63) / L * L);
-        if (l == __builtin_ctzll(have)) {                        // the lowest lane that has it, and there the lowest expert
+        const uint32_t small = in_order((float)best), most = most_of_row<L>(small);
+        bool mine = small == most;
+        const uint64_t have = __ballot(mine);
+        if (__builtin_popcountll(have) > 64 / L) {
+            const uint64_t full = __ballot(best == over_row<L>(best, larger_of{})) >> ((threadIdx.x & 63) / L * L);
+            mine = l == __builtin_ctzll(full);                   // the lowest lane that has it, and there the lowest expert
+        }
+        if (mine) {
             int at = 0;
+            bool found[V];
 #pragma unroll
-            for (int i = V - 1; i >= 0; --i) at = key[i] == most ? i : at;
+            for (int i = 0; i < V; ++i) found[i] = value(i) == best;
 #pragma unroll
-            for (int i = 0; i < V; ++i) key[i] = i == at ? kNever : key[i];
-            picked[r][j] = most == kNever ? -1 : l * V + at;
+            for (int i = V - 1; i >= 0; --i) at = found[i] ? i : at;
+#pragma unroll
+            for (int i = 0; i < V; ++i) upper[i] = at == i ? kChosen : upper[i];
+            picked[r][j] = most <= in_order(-__builtin_inff()) ? -1 : l * V + at;
+            best = lane_best();
         }
     }
     __syncthreads();
