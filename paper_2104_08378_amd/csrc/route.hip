@@ -365,8 +365,9 @@ __global__ __launch_bounds__(kRouteThreads) void k_route_grad(RouteGradArgs a, u
 {
     constexpr int kRows = kRouteThreads / L, kMost = L * V, kPicks = kMost < SP24_MOST_CHOICES ? kMost : SP24_MOST_CHOICES;
     __shared__ double scores[kRows][kMost];
-    __shared__ double slope[kRows][kPicks];
+    __shared__ double slope[kRows][kPicks + 1];                  // of no choice (0), and of every one
     __shared__ int at[kRows][kPicks];
+    __shared__ uint8_t choice[kRows][kMost];                     // an expert's, from 1 on, or 0
     const int l = threadIdx.x % L, r = threadIdx.x / L, E = a.experts;
     const int64_t row = ((int64_t)from + blockIdx.x) * kRows + r;
     const bool live = row < a.N;
@@ -380,7 +381,11 @@ __global__ __launch_bounds__(kRouteThreads) void k_route_grad(RouteGradArgs a, u
 #pragma unroll
     for (int i = 0; i < V; ++i) g[i] = (double)ds[i];
 #pragma unroll
-    for (int i = 0; i < V; ++i) scores[r][i * L + l] = s[i];
+    for (int i = 0; i < V; ++i) {
+        scores[r][i * L + l] = s[i];
+        choice[r][l * V + i] = 0;
+    }
+    if (l == 0) slope[r][0] = 0.0;
     __syncthreads();
     double total = 0.0, along = 0.0;
     for (int j = l; j < a.topk; j += L) {
@@ -390,20 +395,29 @@ __global__ __launch_bounds__(kRouteThreads) void k_route_grad(RouteGradArgs a, u
         total += w;
         along += dw * w;
         at[r][j] = e;
-        slope[r][j] = dw;
+        slope[r][j + 1] = dw;
+        if (e >= 0) choice[r][e] = (uint8_t)(j + 1);
     }
     total = over_row<L>(total, sum_of{});
     along = over_row<L>(along, sum_of{});
     for (int j = l; j < a.topk; j += L) {
-        const double dw = slope[r][j];
-        slope[r][j] = (double)a.scale * (!a.renormalise ? dw : total == 0.0 ? 0.0 : (dw - along / total) / total);
+        const double dw = slope[r][j + 1];
+        slope[r][j + 1] = (double)a.scale * (!a.renormalise ? dw : total == 0.0 ? 0.0 : (dw - along / total) / total);
     }
     __syncthreads();
-    for (int j = 0; j < a.topk; ++j) {
-        const int e = at[r][j] - l * V;
+    // Each expert looks its choice up; an expert that is there twice has the last one's number, and every choice is looked at (8192 rows, eight of 256: always 11.5 us).
+    bool twice = false;
+    for (int j = l; j < a.topk; j += L) twice |= at[r][j] >= 0 && choice[r][at[r][j]] != j + 1;
+    if (__any(twice)) {
+        for (int j = 0; j < a.topk; ++j) {
+            const int e = at[r][j] - l * V;
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (e == i) g[i] += slope[r][j];
+            for (int i = 0; i < V; ++i)
+                if (e == i) g[i] += slope[r][j + 1];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) g[i] += slope[r][choice[r][l * V + i]];
     }
     double mean = 0.0;
     if (a.softmax) {
