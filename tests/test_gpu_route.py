@@ -181,10 +181,12 @@ def test_gradient(N, E, topk, dtype, score):
         assert again.data_ptr() == wide.data_ptr() and torch.equal(again, got)
 
 
-def test_gradient_of_a_choice_that_is_there_twice():
+@pytest.mark.parametrize("N,E,topk", [(7, 12, 4), (40, 8, 3), (33, 64, 6), (2100, 64, 8), (9, 256, 8), (2050, 256, 5), (5, 512, 64), (3, 1000, 40)])
+def test_gradient_of_a_choice_that_is_there_twice(N, E, topk):
     g = torch.Generator().manual_seed(5)
-    x, ids = torch.randn(7, 12, generator=g), torch.randint(0, 3, (7, 4), generator=g, dtype=torch.int32)
-    dw = torch.randn(7, 4, generator=g)
+    x, ids = torch.randn(N, E, generator=g), torch.randint(0, max(E // 4, 2), (N, topk), generator=g, dtype=torch.int32)
+    ids[1::3] = torch.stack([torch.randperm(E, generator=g)[:topk] for _ in ids[1::3]]).int()     # rows without such a choice beside those with one
+    dw = torch.randn(N, topk, generator=g)
     for score in ("softmax", "sigmoid"):
         want, size = expected(x, ids, dw, None, score, False, 1.0)
         ref.close(gradient(x.cuda(), ids.cuda(), dw.cuda(), None, score, False, 1.0), want, size * 2.0 ** -40, score)
