@@ -39,8 +39,10 @@ sp24_status gemm_tokens(const TokenArgs& a, int experts, hipStream_t st)
     // All tokens: the tile whose workgroups still find a unit each, as for the product of an M x K operand (us, restoring included): 512 x 512 x 8192 on 64 x 64
     // 41.2, 128 x 64 47.7, 128 x 128 51.3; 2048 x 1024 x 4096 on 64 x 64 37.6, 128 x 64 30.5, 128 x 128 32.6; 4096 x 1024 x 8192 on 128 x 128, four wavefronts 79.9,
     // eight 82.1, 256 x 128 94.3; 8192 x 2048 x 2048 on 256 x 256 65.8, 256 x 128 69.1, 128 x 128 76.2.
-    if (small <= 64) return run(k_gemm_pipe<DT, OUT, 2, 2, 1, 1, 9, 2, TokenArgs>, 64, 64, 256, 1);
-    if (small <= 128) return run(k_gemm_pipe<DT, OUT, 4, 1, 1, 2, 6, 2, TokenArgs>, 128, 64, 256, 1);
+    // Four stages: 640 x 1000 x 509 with two to five and nine 9.9, 8.7, 8.5, 8.7, 9.8; 768 x 768 x 2048 21.3, 15.0, 13.9, 14.2, 15.0; on 128 x 64 1024 x 1024 x 1024 with
+    // two to six 13.3, 10.5, 10.0, 10.2, 11.1: transfers ahead of what a short K has cost their time before the first product.
+    if (small <= 64) return run(k_gemm_pipe<DT, OUT, 2, 2, 1, 1, 4, 2, TokenArgs>, 64, 64, 256, 1);
+    if (small <= 128) return run(k_gemm_pipe<DT, OUT, 4, 1, 1, 2, 4, 2, TokenArgs>, 128, 64, 256, 1);
     if (small <= 176) return run(k_gemm_pipe<DT, OUT, 2, 4, 2, 1, 4, 2, TokenArgs>, 128, 128, 512, 1);
     if (small <= 256) return run(k_gemm_pipe<DT, OUT, 2, 2, 2, 2, 4, 2, TokenArgs>, 128, 128, 256, 1);
     if (tall <= 256) return run(k_gemm_pipe<DT, OUT, 4, 2, 2, 2, 3, 2, TokenArgs>, 256, 128, 512, 1);
