@@ -96,7 +96,7 @@ PyObject* product_splitk(PyObject* self, PyObject* const* args, Py_ssize_t)
     const at::Tensor* ws = nullptr;
     if (c.ok && c.none(w)) {
         const int64_t need = (int64_t)sp24_splitk_workspace_bytes(a.M, x.N, a.K, ti);
-        own = at::empty({std::max<int64_t>(need, 16)}, at::TensorOptions().dtype(at::kByte).device(a.A->device()));
+        own = make({std::max<int64_t>(need, 16)}, at::kByte, *a.A);
         ws = &own;
     } else ws = c.contiguous(w);
     if (!c.ok) return not_handled();
@@ -256,8 +256,8 @@ PyObject* compress(PyObject* self, PyObject* const* args, Py_ssize_t)
     const sp24_dtype t = type_of(A->scalar_type(), c.ok);
     if (!c.ok) return not_handled();
     const int64_t M = A->size(0), K = A->size(1), lda = A->stride(0);
-    at::Tensor V = at::empty({M, K / 2}, at::TensorOptions().dtype(A->scalar_type()).device(A->device()));
-    at::Tensor meta = at::empty({M, K / 8}, at::TensorOptions().dtype(at::kByte).device(A->device()));
+    at::Tensor V = make({M, K / 2}, A->scalar_type(), *A);
+    at::Tensor meta = make({M, K / 8}, at::kByte, *A);
     const void* pa = A->data_ptr();
     void *pv = V.data_ptr(), *pm = meta.data_ptr(), *st = stream();
     const sp24_status s = without_gil([&] { return sp24_compress(pa, pv, pm, M, K, lda, t, l, st); });

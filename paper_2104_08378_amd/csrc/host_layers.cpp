@@ -30,8 +30,6 @@ T* entries(Call& c, int i, int64_t n, at::ScalarType type)
 }
 const float* floats(Call& c, int i, int64_t n) { return entries<const float>(c, i, n, at::kFloat); }
 
-at::Tensor make(at::IntArrayRef shape, at::ScalarType type, const at::Tensor& like) { return at::empty(shape, at::TensorOptions().dtype(type).device(like.device())); }
-
 // the caller's workspace (argument i), or a new one where some is needed
 struct Scratch {
     at::Tensor own;
@@ -615,8 +613,9 @@ PyObject* linear_backward_checkpoint(PyObject* self, PyObject* const* args, Py_s
     const int64_t pitch = (M + 7) / 8 * 8, lddy = ld(*dY);     // 16-byte rows, which the weights' gradient asks for
     const void* pd = dY->data_ptr();
     const bool own = copy || reinterpret_cast<uintptr_t>(pd) % 16 != 0 || lddy % 8 != 0;
-    at::Tensor dZ = own ? make({N, pitch}, type, *dY) : *dY, db = grouped ? make({experts, M}, at::kFloat, *dY) : make({M}, at::kFloat, *dY);
-    if (own && pitch != M) dZ = dZ.narrow(1, 0, M);
+    const int64_t shape[2] = {N, M}, strides[2] = {pitch, 1};
+    at::Tensor dZ = !own ? *dY : pitch == M ? make(shape, type, *dY) : at::Tensor(at::detail::empty_strided_cuda(shape, strides, type, dY->device())),
+               db = grouped ? make({experts, M}, at::kFloat, *dY) : make({M}, at::kFloat, *dY);
     void *pdz = own ? dZ.data_ptr() : nullptr, *st = stream();
     float* pb = static_cast<float*>(db.data_ptr());
     const sp24_status s = without_gil([&] {
