@@ -29,11 +29,13 @@ sp24_status gemm_tokens(const TokenArgs& a, int experts, hipStream_t st)
     // mean: 256 x 256 46, 61, 73; 128 x 256 50, 50, 50; 128 x 128 58, 56, 56; 64 of 1024 x 512 from 16384, alike and not: 47 and 60 to 84, 50 and 52 to 65.  (The longest
     // first: 0.98 to 1.02 times as long with eight, 0.85 with 64 uneven ones, 1.0 to 1.08 with even ones.)
     // Few tiles: half as large ones, four stages deep.  Eight of 512 x 512 from 8192 24.5 -> 19.5, uneven 41 -> 29; eight of 1024 x 512 24.6 -> 22.9, 40 -> 30;
-    // four of 1024 x 1024 34.1 -> 33.6, 40 -> 36; but (256 tiles) 16 of 1024 x 512 from 1024 10.5 -> 12.4.  Columns of 128 too where wider ones are mostly padding.
+    // four of 1024 x 1024 34.1 -> 33.6, 40 -> 36; but (256 tiles) 16 of 1024 x 512 from 1024 10.5 -> 12.4.  Columns of 128 too where wider ones are mostly padding,
+    // and where segments are short, two workgroups to a unit then, one's first transfers and results beside the other's products: eight of 4096 x 2048 from 512 choices
+    // 48.9 -> 46.0, uneven 47.5 -> 44.6; 16 of 1344 x 1472 from 94 26.0 -> 22.2; eight of 4096 x 1024 from 1024 32.7 -> 31.9; 16 of 1024 x 1024 from 2048 20.0 -> 21.3.
     if (a.offsets) {
         const int64_t wide = (a.N + 255) / 256;
         if ((a.M + 127) / 128 * wide * experts <= 128) return run(k_gemm_pipe<DT, OUT, 2, 4, 2, 1, 4, 2, TokenArgs>, 128, 128, 512, experts);
-        if (wide * 256 * 4 > cols * 128 * 5) return run(k_gemm_pipe<DT, OUT, 4, 2, 1, 2, 2, 2, TokenArgs>, 128, 128, 512, experts);
+        if (wide * 256 * 4 > cols * 128 * 5 || a.K <= 128 * experts) return run(k_gemm_pipe<DT, OUT, 4, 2, 1, 2, 2, 2, TokenArgs>, 128, 128, 512, experts);
         return run(k_gemm_pipe<DT, OUT, 2, 4, 2, 2, 3, 2, TokenArgs>, 128, 256, 512, experts);
     }
     // All tokens: the tile whose workgroups still find a unit each, as for the product of an M x K operand (us, restoring included): 512 x 512 x 8192 on 64 x 64

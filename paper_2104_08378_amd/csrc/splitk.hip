@@ -18,7 +18,14 @@ __global__ __launch_bounds__(256) void k_splitk_reduce(const ACC* partial, int s
     const int64_t image = M * ldw;
     const ACC* src = partial + row * ldw + col;
     vec4 sum = *reinterpret_cast<const vec4*>(src);
-    for (int s = 1; s < slices; ++s) sum += *reinterpret_cast<const vec4*>(src + (int64_t)s * image);
+    int s = 1;
+    for (; s + 3 < slices; s += 4) {                             // four loads on their way: 512 x 512 in 16 slices 3 us less
+        const ACC* const p = src + (int64_t)s * image;
+        const vec4 v0 = *reinterpret_cast<const vec4*>(p), v1 = *reinterpret_cast<const vec4*>(p + image), v2 = *reinterpret_cast<const vec4*>(p + 2 * image),
+                   v3 = *reinterpret_cast<const vec4*>(p + 3 * image);
+        sum = (((sum + v0) + v1) + v2) + v3;
+    }
+    for (; s < slices; ++s) sum += *reinterpret_cast<const vec4*>(src + (int64_t)s * image);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         if (col + e < N) {
