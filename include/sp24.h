@@ -653,8 +653,8 @@ typedef enum {
  * a code is off by half a step, 2^-8 of its block's largest value).  Binary32 sums.  D: M x N of type `in` or SP24_F32.  K may be any number, 0 included,
  * which gives zeros.  Rows of A must be 16-byte aligned; what lies between a row's end and the next 16-byte boundary may be read and is not used.  lda and N
  * below 2^21, else SP24_ERR_SHAPE.
- * workspace: device, 16-byte aligned, sp24_gemm_dense_checkpoint_workspace_bytes(M, N, K, 0) bytes: the restored rows of this one product, and partial
- * products where few tiles have many tokens (contents before the call are ignored, after it unspecified; calls sharing one must not overlap in time).
+ * workspace: device, 16-byte aligned, sp24_gemm_dense_checkpoint_workspace_bytes(M, N, K, 0) bytes: the restored rows of this one product (of more than a
+ * few tokens), and partial products where few tiles have many (contents before the call are ignored, after it unspecified; calls sharing one must not overlap in time).
  */
 size_t sp24_gemm_dense_checkpoint_workspace_bytes(int64_t M, int64_t N, int64_t K, int grouped);
 sp24_status sp24_gemm_dense_checkpoint(const void* A, sp24_aorder order, const void* codes, const float* scale, void* D, int64_t M, int64_t N,

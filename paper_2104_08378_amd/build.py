@@ -20,7 +20,7 @@ HOST = os.path.join(HERE, "_sp24_host.so")      # native marshalling of the bind
 PROBE = os.path.join(HERE, "sp24_probe")        # stand-alone measurement of the chip's ceilings (csrc/probe.hip)
 HOST_SOURCES = ["host_calls.cpp", "host_layers.cpp"]
 _TYPES = ("f16", "bf16", "i8", "f8")
-SOURCES = ["api.hip", "api_layers.hip", "norm.hip", "linear.hip", "linear_stream.hip", "linear_grad.hip", "experts.hip", "route.hip", "checkpoint.hip", "gemm_tokens_f16.hip", "gemm_tokens_bf16.hip", "prune_compress.hip", "permute.hip", "permute_search.hip", "permute_search_columns.hip", "splitk.hip", "mm_simple.hip", "mm_ksplit.hip", "conv_narrow.hip", "mm_skinny.hip", "mm_stream.hip", "mm_tiled.hip", "mm_staged.hip",
+SOURCES = ["api.hip", "api_layers.hip", "norm.hip", "linear.hip", "linear_stream.hip", "linear_grad.hip", "experts.hip", "route.hip", "checkpoint.hip", "gemm_codes.hip", "gemm_tokens_f16.hip", "gemm_tokens_bf16.hip", "prune_compress.hip", "permute.hip", "permute_search.hip", "permute_search_columns.hip", "splitk.hip", "mm_simple.hip", "mm_ksplit.hip", "conv_narrow.hip", "mm_skinny.hip", "mm_stream.hip", "mm_tiled.hip", "mm_staged.hip",
            "mm_staged_f16.hip", "mm_staged_bf16.hip", "mm_staged_i8.hip", "mm_staged_f8.hip"] + [
     "mm_tiled_%s_%s.hip" % (i, o) for i, o in
     [("f16", "f32"), ("f16", "f16"), ("f16", "bf16"), ("bf16", "f32"), ("bf16", "f16"), ("bf16", "bf16"),

@@ -497,6 +497,10 @@ struct KeptProduct {
     void* workspace;
     size_t workspace_bytes;
 };
+// Up to so many tokens, twice as many of segments, the product takes the codes itself.  In a graph, us: 512 x 512 from 64 5.5 -> 3.4, from 256 6.0 -> 5.2, from 512 6.8 and
+// 7.6; 4096 x 1024 from 64 8.0 -> 5.3, from 256 9.2 -> 7.8; 6328 x 2112 from 128 14.1 -> 13.0, but from 256 17.4 and 18.5; 2048 x 1000 from 400 9.8 and 11.4.  Eight
+// segments of 1024 x 1024 from 256 choices 9.3 -> 7.9, four from 512 9.3 and 10.2; 32 of 2048 x 1024, most of them empty, 28 and 33.
+constexpr int64_t kFewTokens = 256;
 static sp24_status gemm_kept(const KeptProduct& a, void* stream)
 {
     if (!is_float16(a.in) || !is_code(a.code) || !(a.out == SP24_F32 || a.out == a.in)) return SP24_ERR_DTYPE;
@@ -526,11 +530,14 @@ static sp24_status gemm_kept(const KeptProduct& a, void* stream)
                of = vec(a.offsets, a.experts + 1, 4), ws = Span{a.workspace, need};
     if (overlaps(d, {A, c, sc, ro, of, ws}) || overlaps(ws, {A, c, sc, ro, of})) return SP24_ERR_SHAPE;
     hipStream_t const st = static_cast<hipStream_t>(stream);
-    if (a.K > 0) SP24_TRY(launch_restore_rows(RestoreArgs{a.codes, a.scale, a.rows, a.workspace, a.tokens, a.K, a.N, a.ldc, pitch, a.topk, SP24_ACT_NONE, a.code, a.in}, st));
+    const RestoreArgs restore{a.codes, a.scale, a.rows, a.workspace, a.tokens, a.K, a.N, a.ldc, pitch, a.topk, SP24_ACT_NONE, a.code, a.in};
+    const bool few = turned && a.K > 0 && a.K <= (a.offsets ? 2 : 1) * kFewTokens && a.tokens > 0;
+    if (a.K > 0 && !few) SP24_TRY(launch_restore_rows(restore, st));
     if (turned) {
         TokenArgs t{};
         static_cast<MmArgs&>(t) = MmArgs{a.A, nullptr, a.workspace, a.D, a.M, a.N, a.K, a.lda, pitch, a.ldd, a.in, a.out, SP24_B_NMAJOR, SP24_LAYOUT_CANONICAL, false};
         t.offsets = a.offsets;
+        if (few) return launch_gemm_codes(t, restore, a.experts, st);
         const size_t rows = restored_bytes(a.K, a.N);
         return launch_gemm_tokens(t, a.experts, need > rows ? static_cast<uint8_t*>(a.workspace) + rows : nullptr, st);
     }

@@ -261,5 +261,7 @@ struct TokenSplit {
 TokenSplit token_split(int64_t M, int64_t N, int64_t K);
 // partial: token_split().bytes of a product that is to be split, or null
 sp24_status launch_gemm_tokens(const TokenArgs& a, int experts, void* partial, hipStream_t st);
+// the same of few tokens, the rows of B as `r` would restore them
+sp24_status launch_gemm_codes(const TokenArgs& a, const RestoreArgs& r, int experts, hipStream_t st);
 
 } // namespace sp24

@@ -255,12 +255,13 @@ def test_weights_gradient_from_any_number_of_tokens(K, dtype, code):
 @pytest.mark.parametrize("M,N,c_spare,c_offset", [(1, 1, 0, 0), (33, 17, 3, 1), (70, 45, 0, 0), (64, 64, 1, 5), (300, 1411, 0, 3), (5, 8, 9, 1), (129, 127, 0, 0), (2100, 201, 7, 9),
                                                   (260, 520, 0, 0), (1540, 1288, 0, 0), (66600, 104, 0, 0)])
 def test_weights_gradient_of_any_size(M, N, c_spare, c_offset, dtype, code):
-    for K in (3, 77, 130):
+    for K in (3, 77, 130, 290):
         product(M, N, K, dtype, code, F32 if K % 2 else dtype, 0, c_spare, c_offset)
 
 
 @pytest.mark.parametrize("M,N,K", [(4096, 1024, 200), (4096, 2304, 136), (2304, 2048, 72), (1024, 8192, 330), (8192, 640, 77), (512, 512, 2000),
-                                   (500, 500, 5005), (1000, 1030, 3000), (1500, 1001, 4100), (128, 40, 9001), (2048, 1024, 4160)])
+                                   (500, 500, 5005), (1000, 1030, 3000), (1500, 1001, 4100), (128, 40, 9001), (2048, 1024, 4160),
+                                   (4096, 1024, 330), (4096, 2304, 300), (2304, 2048, 290), (8192, 640, 277), (1792, 1500, 259)])
 def test_weights_gradient_on_every_tile(M, N, K):
     product(M, N, K, BF16, I8, BF16)
     product(M, N, K, F16, F8, F32)
@@ -289,7 +290,8 @@ def segments(g, lengths, spare_rows):
 @pytest.mark.parametrize("dtype", [F16, BF16])
 @pytest.mark.parametrize("M,N,lengths,spare", [(40, 56, [16], 0), (128, 128, [0, 16, 0, 32, 0], 16), (200, 264, [48, 0, 80, 160], 0), (256, 136, [64, 128, 16], 64), (70, 45, [0, 0], 0),
                                                (300, 520, [336, 16, 0, 208], 32), (1024, 1024, [112, 400], 0),
-                                               (1100, 1032, [48, 0, 80, 160, 16], 16), (1100, 264, [16, 64, 0, 32] * 4, 0)])
+                                               (1100, 1032, [48, 0, 80, 160, 16], 16), (1100, 264, [16, 64, 0, 32] * 4, 0),
+                                               (1100, 1032, [336, 0, 80, 160, 16], 16), (600, 520, [64, 16, 112, 0] * 4, 48), (1100, 264, [48, 16, 32] * 6, 0)])
 def test_experts_weights_gradient(M, N, lengths, spare, dtype, code):
     g = torch.Generator().manual_seed(M + N)
     offsets, R = segments(g, lengths, spare)
@@ -348,10 +350,11 @@ def test_rows_far_into_the_codes():
         assert torch.equal(p, q)
 
 
+@pytest.mark.parametrize("times", [1, 3])
 @pytest.mark.parametrize("M,N", [(70, 45), (200, 264), (1100, 1032)])
-def test_segments_keep_to_themselves(M, N):
+def test_segments_keep_to_themselves(M, N, times):
     """Segments that end inside a step of the products, between rows that are not finite in both operands."""
-    lengths = [16, 48, 80, 16, 112, 16]
+    lengths = [times * n for n in (16, 48, 80, 16, 112, 16)]
     g = torch.Generator().manual_seed(N)
     offsets, R = segments(g, lengths, 48)
     o = offsets.tolist()
@@ -396,3 +399,14 @@ def test_operands_past_32_bits():
     assert torch.equal(back[some.cuda()].cpu(), kept_b.to(BF16)) and int((back != 0).any(1).sum()) == len(some)
     dZ, _, db = sp24.sp24_linear_backward_checkpoint(back, c, "relu")
     assert torch.equal(dZ[some.cuda()].cpu(), torch.where(routing_ref.stands_for(*(t.cpu() for t in few)) > 0, kept_b, 0.0).to(BF16))
+
+
+@pytest.mark.parametrize("M,N,K", [(512, 520, 255), (512, 520, 256), (2100, 1000, 192), (2100, 1000, 256)])
+def test_products_of_codes_equal_those_of_restored_rows(M, N, K):
+    """Few tokens' products make their rows from the codes; the same operands and the same order of sums give the same bits as rows restored before."""
+    g = torch.Generator().manual_seed(K)
+    a = torch.zeros(320, -(-M // 8) * 8, dtype=BF16, device="cuda")[:, :M]
+    a[:K].copy_(torch.randn(K, M, generator=g))
+    c = sp24.sp24_checkpoint_rows(rows_of(g, 320, N, BF16).cuda(), I8)
+    few = sp24.sp24_gemm_dense_checkpoint(a[:K].t(), sp24.Checkpoint(c.codes[:K], c.scale[:K]), F32)
+    assert torch.equal(few, sp24.sp24_gemm_dense_checkpoint(a.t(), c, F32))
