@@ -436,9 +436,8 @@ __global__ __launch_bounds__(kRouteThreads) void k_route_grad(RouteGradArgs a, u
 }
 
 // f(integral_constant lanes, integral_constant values a lane) for rows of this many experts.  Few rows are a wavefront each, whose chain of operations
-// is the time; many share wavefronts, which issue the less for each.  In a graph, us, top 8 of 256: 512 rows on 64 lanes 4.8, on 32 5.9; 2048 5.95 and
-// 6.1; 4096 8.6 and 7.2; 16384 23.9 and 18.5.  Top 6 of 64: 512 rows on 64 lanes 3.5, on 16 3.9; 2048 4.05 both; 8192 8.2 and 4.8.  (Half the lanes again:
-// 8192 rows of 64 5.4, of 256 10.6, but 4096 rows 8.6.)
+// is the time; many share wavefronts, which issue the less for each.  In a graph, us, top 8 of 256: 512 rows on 64 lanes 4.9, on 32 5.8; 2048 5.3 and
+// 5.8; 3000 6.4 and 6.5; 4096 7.4 and 6.6; 16384 19.4 and 15.8.  Top 6 of 64: 512 rows on 64 lanes 3.3, on 16 3.9; 2048 3.65 and 4.1; 8192 6.7 and 4.6.
 template <class F>
 static sp24_status by_experts(int experts, int64_t rows, F&& f)
 {
