@@ -144,6 +144,7 @@ __device__ __forceinline__ void store_run(void* p, int64_t i, int have, const fl
 }
 
 constexpr double kNever = -__builtin_inf();
+constexpr double kInfinite = 1e300;                              // what +inf is compared as, below a NaN and above all sums of numbers
 constexpr uint32_t kChosen = 0xFFEFFFFFu;                        // upper half of -1.8e308
 
 // The scores of a row's experts, 0 for those whose logit is -inf, and (rest) 1 - s of a logistic one without the difference.  A NaN (or, softmax,
@@ -193,6 +194,12 @@ __device__ __forceinline__ int image_place(int e)
     return e % V * L + e / V;
 }
 
+// What a group is worth whose largest c are these: their sum, and no more than one that is infinite or NaN
+__device__ __forceinline__ double group_value(double first, double second, int best)
+{
+    return best == 1 || second == kNever || first >= kInfinite ? first : first + second;
+}
+
 // How experts are grouped: not; runs of 2^n lanes that hold whole groups; any other way
 enum { kNoGroups, kLaneGroups, kAnyGroups };
 
@@ -223,7 +230,7 @@ __global__ __launch_bounds__(kRouteThreads) void k_route(RouteArgs a, unsigned f
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         const double c = s[i] + (double)bias[i];
-        key[i] = x[i] == -__builtin_inff() ? kNever : c != c ? __builtin_inf() : __builtin_fmin(c, 1e300);
+        key[i] = x[i] == -__builtin_inff() ? kNever : c != c ? __builtin_inf() : __builtin_fmin(c, kInfinite);
         scores[r][i * L + l] = s[i];
         rounded[i] = (float)s[i];
     }
@@ -242,7 +249,7 @@ __global__ __launch_bounds__(kRouteThreads) void k_route(RouteArgs a, unsigned f
             second = __builtin_fmax(__builtin_fmin(first, other), __builtin_fmax(second, next));
             first = __builtin_fmax(first, other);
         }
-        const double value = a.group_best == 1 || second == kNever ? first : first + second;
+        const double value = group_value(first, second, a.group_best);
         // the group stays if fewer than groups_kept are ahead of it
         const int mine = l / lanes;
         int ahead = 0;
@@ -267,7 +274,7 @@ __global__ __launch_bounds__(kRouteThreads) void k_route(RouteArgs a, unsigned f
                 second = __builtin_fmax(second, __builtin_fmin(first, k));
                 first = __builtin_fmax(first, k);
             }
-            values[r][g] = a.group_best == 1 || second == kNever ? first : first + second;
+            values[r][g] = group_value(first, second, a.group_best);
         }
         __syncthreads();
         for (int g = l; g < a.groups; g += L) {
