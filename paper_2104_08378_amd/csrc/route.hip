@@ -469,7 +469,11 @@ static sp24_status by_experts(int experts, int64_t rows, F&& f)
 
 sp24_status launch_moe_route(const RouteArgs& a, hipStream_t st)
 {
-    if (a.load && a.N == 0) k_no_load<<<1, 256, 0, st>>>(a.load, a.experts);
+    if (a.N == 0) {
+        if (!a.load) return SP24_OK;
+        k_no_load<<<1, 256, 0, st>>>(a.load, a.experts);
+        return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
+    }
     const sp24_status s = by_experts(a.experts, a.N, [&](auto l, auto v) {
         constexpr int L = decltype(l)::value, V = decltype(v)::value, kRows = kRouteThreads / L;
         return launch_in_parts((a.N + kRows - 1) / kRows, kRouteThreads, [&](unsigned from, unsigned grid) {
@@ -479,7 +483,7 @@ sp24_status launch_moe_route(const RouteArgs& a, hipStream_t st)
             else k_route<L, V, kAnyGroups><<<grid, kRouteThreads, 0, st>>>(a, from);
         });
     });
-    if (s != SP24_OK || !a.load || a.N == 0) return s;
+    if (s != SP24_OK || !a.load) return s;
     const int64_t choices = a.N * a.topk;
     k_route_load<<<(unsigned)std::min<int64_t>((choices + kLoadChoices - 1) / kLoadChoices, 64), kLoadThreads, 0, st>>>(a.ids, a.load, choices, a.experts);
     return hipGetLastError() == hipSuccess ? SP24_OK : SP24_ERR_LAUNCH;
