@@ -4,6 +4,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/hip/EmptyTensor.h>
+#include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -150,13 +151,28 @@ int64_t ld(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : std::max(
 
 void* stream() { return c10::hip::getCurrentHIPStream().stream(); }
 
-// The result: a new tensor, or the caller's (argument i), which must have exactly the result's shape and type.
-// A new tensor, not by way of torch's dispatcher: 0.47 us for 0.70, where a launch takes 2.7 (routing of 16 tokens a call 5.8 -> 4.8).
+// New memory comes by way of torch's dispatcher only where that does more than allocate: where a dispatch mode is to see it, and where new memory is to be filled
+// (torch.use_deterministic_algorithms).  Past it 0.47 us for 0.70, where a launch takes 2.7 (routing of 16 tokens a call 5.8 -> 4.8).
+inline bool by_dispatcher()
+{
+    const auto& context = at::globalContext();
+    return c10::impl::dispatch_mode_enabled() || (context.deterministicAlgorithms() && context.deterministicFillUninitializedMemory());
+}
 inline at::Tensor make(at::IntArrayRef shape, at::ScalarType type, const at::Tensor& like)
 {
+    if (by_dispatcher()) return at::empty(shape, at::TensorOptions().dtype(type).device(like.device()));
     return at::Tensor(at::detail::empty_cuda(shape, type, like.device(), c10::nullopt));
 }
+// rows x columns with rows of `pitch`
+inline at::Tensor make_pitched(int64_t rows, int64_t columns, int64_t pitch, at::ScalarType type, const at::Tensor& like)
+{
+    if (pitch == columns) return make({rows, columns}, type, like);
+    if (by_dispatcher()) return make({rows, pitch}, type, like).narrow(1, 0, columns);
+    const int64_t shape[2] = {rows, columns}, strides[2] = {pitch, 1};
+    return at::Tensor(at::detail::empty_strided_cuda(shape, strides, type, like.device()));
+}
 
+// The result: a new tensor, or the caller's (argument i), which must have exactly the result's shape and type.
 struct Result {
     at::Tensor fresh;
     const at::Tensor* t = nullptr;

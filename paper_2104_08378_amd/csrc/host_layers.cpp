@@ -613,9 +613,7 @@ PyObject* linear_backward_checkpoint(PyObject* self, PyObject* const* args, Py_s
     const int64_t pitch = (M + 7) / 8 * 8, lddy = ld(*dY);     // 16-byte rows, which the weights' gradient asks for
     const void* pd = dY->data_ptr();
     const bool own = copy || reinterpret_cast<uintptr_t>(pd) % 16 != 0 || lddy % 8 != 0;
-    const int64_t shape[2] = {N, M}, strides[2] = {pitch, 1};
-    at::Tensor dZ = !own ? *dY : pitch == M ? make(shape, type, *dY) : at::Tensor(at::detail::empty_strided_cuda(shape, strides, type, dY->device())),
-               db = grouped ? make({experts, M}, at::kFloat, *dY) : make({M}, at::kFloat, *dY);
+    at::Tensor dZ = own ? make_pitched(N, M, pitch, type, *dY) : *dY, db = grouped ? make({experts, M}, at::kFloat, *dY) : make({M}, at::kFloat, *dY);
     void *pdz = own ? dZ.data_ptr() : nullptr, *st = stream();
     float* pb = static_cast<float*>(db.data_ptr());
     const sp24_status s = without_gil([&] {
