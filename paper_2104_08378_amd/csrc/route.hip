@@ -5,7 +5,7 @@
 //   softmax: dl = s (g - sum g s);  logistic: dl = s (1 - s) g
 //
 // All in binary64: of 10^5 tokens' experts some pairs' scores are within a rounding of binary32 of each other, and which one is chosen must
-// not hang on the order of a sum.
+// not hang on how the sum was taken; within one of binary64 the sum's order decides, which is the same whatever the number of rows.
 //
 // Bound by vector operations, two thirds of the time busy with them: an exponential of some 35 in binary64 for every logit, and for every choice the
 // reduction over the row's lanes and a search in the one that has it.  Few rows: a launch and one row's chain of them.  In a graph, us: 16 rows, four of 64 experts
@@ -57,6 +57,42 @@ __device__ __forceinline__ double over_row(double v, OP op)
     if constexpr (L >= 64) v = over_halves<true>(v, op);
     return v;
 }
+struct larger_of { __device__ __forceinline__ double operator()(double a, double b) const { return __builtin_fmax(a, b); } };
+struct sum_of {
+    __device__ __forceinline__ double operator()(double a, double b) const
+    {
+#pragma clang fp contract(off)
+        return a + b;                                            // (a product that is added is rounded first, wherever it stands)
+    }
+};
+// The sum over a row, neighbouring experts first, then neighbouring pairs and so on, so that it does not hang on how many lanes share the row's experts,
+// which goes by the number of rows: a row's choice would (as fast as a lane's values one after the other).
+template <int COUNT>
+__device__ __forceinline__ double sum_of_neighbours(const double (&v)[COUNT])
+{
+    double part[COUNT];
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) part[i] = v[i];
+#pragma unroll
+    for (int d = 1; d < COUNT; d *= 2)
+#pragma unroll
+        for (int i = 0; i < COUNT; i += 2 * d) part[i] = sum_of{}(part[i], part[i + d]);
+    return part[0];
+}
+template <int L, int V>
+__device__ __forceinline__ double sum_of_row(const double (&v)[V])
+{
+    return over_row<L>(sum_of_neighbours(v), sum_of{});
+}
+// The same of a row's `topk` choices, lane l with choices l, L + l, ...: a run of L choices in every part
+template <int L, int PARTS>
+__device__ __forceinline__ double sum_of_choices(const double (&v)[PARTS], int topk)
+{
+    double part[PARTS];
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) part[i] = i == 0 || i * L < topk ? over_row<L>(v[i], sum_of{}) : 0.0;
+    return sum_of_neighbours(part);
+}
 template <int L>
 __device__ __forceinline__ uint32_t most_of_row(uint32_t v)
 {
@@ -87,8 +123,6 @@ __device__ __forceinline__ double larger(double a, double b)
     asm("v_max_f64 %0, %1, %2" : "=v"(v) : "v"(a), "v"(b));
     return v;
 }
-struct larger_of { __device__ __forceinline__ double operator()(double a, double b) const { return __builtin_fmax(a, b); } };
-struct sum_of { __device__ __forceinline__ double operator()(double a, double b) const { return a + b; } };
 
 // COUNT neighbouring values from element i on, the first `have` of them (the others: `otherwise`); 16 bytes at a time where there are that many
 template <int T, int COUNT>
@@ -157,13 +191,9 @@ __device__ __forceinline__ void scores_of_row(const float (&x)[V], bool softmax,
 #pragma unroll
         for (int i = 0; i < V; ++i) most = fmaxf(most, x[i]);
         const double top = over_row<L>((double)most, larger_of{});
-        double sum = 0.0;
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            s[i] = x[i] == -__builtin_inff() ? 0.0 : exp((double)x[i] - top);
-            sum += s[i];
-        }
-        const double part = 1.0 / over_row<L>(sum, sum_of{});
+        for (int i = 0; i < V; ++i) s[i] = x[i] == -__builtin_inff() ? 0.0 : exp((double)x[i] - top);
+        const double part = 1.0 / sum_of_row<L>(s);
 #pragma unroll
         for (int i = 0; i < V; ++i) s[i] = x[i] == -__builtin_inff() ? 0.0 : s[i] * part;
     } else {
@@ -206,7 +236,7 @@ enum { kNoGroups, kLaneGroups, kAnyGroups };
 template <int L, int V, int GROUPS>
 __global__ __launch_bounds__(kRouteThreads) void k_route(RouteArgs a, unsigned from)
 {
-    constexpr int kRows = kRouteThreads / L, kMost = L * V, kPicks = kMost < SP24_MOST_CHOICES ? kMost : SP24_MOST_CHOICES;
+    constexpr int kRows = kRouteThreads / L, kMost = L * V, kPicks = kMost < SP24_MOST_CHOICES ? kMost : SP24_MOST_CHOICES, kParts = (kPicks + L - 1) / L;
     constexpr bool ANY = GROUPS == kAnyGroups;
     __shared__ double scores[kRows][kMost];
     __shared__ int picked[kRows][kPicks];
@@ -229,7 +259,7 @@ __global__ __launch_bounds__(kRouteThreads) void k_route(RouteArgs a, unsigned f
     float rounded[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        const double c = s[i] + (double)bias[i];
+        const double c = sum_of{}(s[i], (double)bias[i]);
         key[i] = x[i] == -__builtin_inff() ? kNever : c != c ? __builtin_inf() : __builtin_fmin(c, kInfinite);
         scores[r][i * L + l] = s[i];
         rounded[i] = (float)s[i];
@@ -328,12 +358,14 @@ __global__ __launch_bounds__(kRouteThreads) void k_route(RouteArgs a, unsigned f
         }
     }
     __syncthreads();
-    double sum = 0.0;
-    for (int j = l; j < a.topk; j += L) {
-        const int e = picked[r][j];
-        sum += e < 0 ? 0.0 : scores[r][image_place<L, V>(e)];
+    double chosen[kParts] = {};
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) {
+        if (i > 0 && i * L >= a.topk) break;
+        const int j = i * L + l, e = j < a.topk ? picked[r][j] : -1;
+        chosen[i] = e < 0 ? 0.0 : scores[r][image_place<L, V>(e)];
     }
-    sum = over_row<L>(sum, sum_of{});
+    const double sum = sum_of_choices<L>(chosen, a.topk);
     if (!live) return;
     for (int j = l; j < a.topk; j += L) {
         const int e = picked[r][j];
