@@ -5,8 +5,10 @@ import numpy as np
 import pytest
 import torch
 
+import layers_ref as ref
 import routing_ref
 from paper_2104_08378_amd import sp24
+from test_gpu_route import expected
 
 pytestmark = pytest.mark.gpu
 
@@ -61,3 +63,70 @@ def test_a_row_has_the_same_experts_among_few_and_among_many(E):
             few = sp24.sp24_moe_route(x[first:first + FEW], bias=bias, **how)
             for p, q in zip(many[:3], few[:3]):
                 assert p is None or torch.equal(p[first:first + FEW], q)
+
+
+def rows(N, E, dtype, seed):
+    """Logits of N rows: normal ones, and in places rows that are masked, infinite, NaN or full of ties."""
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(N, E, generator=g) * 2
+    kind = torch.arange(N) % 11
+    masked = torch.rand(N, E, generator=g) < 0.9
+    x = torch.where((kind == 3)[:, None] & masked, -INF, x)
+    x = torch.where((kind == 5)[:, None], x.round(), x)
+    x[kind == 7] = torch.randint(18, 50, (int((kind == 7).sum()), E), generator=g).float()
+    x[60::97, E // 2] = NAN
+    x[61::97, E // 3] = INF
+    x[62::97] = -INF
+    x[63::97, 1:] = -INF
+    return x.to(dtype)
+
+
+# (groups of whole power-of-two runs of lanes and groups of any other size, of 2, 4 or 8 experts a lane)
+MANY = [(8, (2, 4)), (16, (4, 16)), (20, (4, 10)), (32, (4, 32)), (64, (4, 64)), (100, (25, 5)), (128, (4, 128)), (160, (5, 8)), (256, (8, 256)), (512, (8, 512)), (1000, (125, 8))]
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("E,groups", MANY)
+def test_many_rows(E, groups, dtype):
+    """All rows against calls of few of them, to the bit, and some against 64 bits."""
+    N = FEW + 37
+    x = rows(N, E, dtype, E)
+    sample = torch.cat((torch.arange(0, 120), torch.arange(FEW - 3, N)))
+    b = 0.1 * torch.randn(E, generator=torch.Generator().manual_seed(1))
+    b[E // 4], b[E // 2 + 1] = -INF, b[0]
+    dev, tiny = x.cuda(), (E + 16) * 2.0 ** -53
+    topk = min(8, E // 2)
+    hows = [dict(score="softmax", bias=b), dict(score="sigmoid", renormalise=False, scale=2.5)]
+    for n in groups:
+        kept = max(n // 2, -(-topk // (E // n)))
+        hows += [dict(score="sigmoid", bias=b, groups=n, groups_kept=kept, group_best=2), dict(score="softmax", groups=n, groups_kept=kept, group_best=1)]
+    for how in hows:
+        on = dict(how, bias=how["bias"].cuda()) if "bias" in how else how
+        got = sp24.sp24_moe_route(dev, topk, want_scores=True, want_load=True, **on)
+        few = [sp24.sp24_moe_route(dev[i:i + FEW // 2], topk, want_scores=True, **on) for i in range(0, N, FEW // 2)]
+        for a, part in zip(got[:3], zip(*few)):
+            assert torch.equal(a.view(torch.int32), torch.cat(part[:len(few)]).view(torch.int32)), how
+        ids, weights, scores, _ = routing_ref.route(x[sample], topk, **how)
+        assert torch.equal(got.ids.cpu()[sample].long(), ids.long()), how
+        ref.close(got.scores.cpu()[sample], scores, torch.nan_to_num(scores) * tiny, "scores")
+        ref.close(got.weights.cpu()[sample], weights, torch.nan_to_num(weights.abs()) * tiny * 2, "weights")
+        flat = got.ids.reshape(-1).long()
+        assert torch.equal(got.load.long(), torch.bincount(flat[flat >= 0], minlength=E)), how
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("E,topk", [(8, 3), (16, 16), (20, 4), (32, 8), (64, 40), (100, 8), (128, 64), (160, 6), (256, 8), (1000, 10)])
+def test_gradient_of_many_rows(E, topk, dtype, score):
+    N = FEW + 5
+    g = torch.Generator().manual_seed(E)
+    x = (torch.randn(N, E, generator=g) * 2).to(dtype)
+    x[::7, 0] = -INF
+    ids = x.float().topk(topk, dim=1).indices.to(torch.int32)
+    ids[1::5, 0], ids[2::50], ids[3::50, -1] = -1, -1, E
+    dw, ds = torch.randn(N, topk, generator=g).cuda(), torch.randn(N, E, generator=g).cuda()
+    for renormalise, d, scale in ((True, ds, 0.5), (True, None, 1.0), (False, ds, 2.5)):
+        want, size = expected(x, ids, dw, d, score, renormalise, scale)
+        got = sp24.sp24_moe_route_backward(x.cuda(), ids.cuda(), dw, score=score, renormalise=renormalise, scale=scale, dscores=d)
+        # (as for few rows: a few thousand operations of 2^-53, and the rounding on the way to 32 bits)
+        ref.close(got, want, size * 4096 * 2.0 ** -53 + want.abs() * 2.0 ** -24, str((E, topk, dtype, score, renormalise)))
