@@ -4,7 +4,7 @@ import torch
 from torch.utils._python_dispatch import TorchDispatchMode
 
 from paper_2104_08378_amd import sp24
-from test_gpu_routed_block import Declines, flat
+from test_gpu_routed_block import Declines, calls, flat
 
 pytestmark = pytest.mark.gpu
 
@@ -65,3 +65,27 @@ def test_new_memory_is_filled_where_torch_is_told_to(monkeypatch, python_path):
         torch.use_deterministic_algorithms(False)
     assert dz.stride() == (8, 1) and bool(torch.isnan(torch.as_strided(dz, (47, 3), (8, 1), 5)).all())
     assert torch.equal(dz, want[0]) and torch.equal(dzt, want[1]) and torch.equal(db, want[2])
+
+
+class Insists:
+    """Stands in for the native module and takes no call that it declines."""
+
+    def __init__(self, host):
+        self.host, self.taken = host, set()
+
+    def __getattr__(self, name):
+        def call(*a):
+            got = getattr(self.host, name)(*a)
+            assert got is not None, name
+            self.taken.add(name)
+            return got
+        return call
+
+
+def test_the_calls_are_taken_natively(monkeypatch):
+    host = Insists(sp24._load_host())
+    monkeypatch.setattr(sp24, "_host", host)
+    for call in calls():
+        call()
+    assert host.taken >= {"sp24_moe_route", "sp24_moe_route_backward", "sp24_checkpoint_rows", "sp24_restore_rows", "sp24_linear_backward_checkpoint",
+                          "sp24_gemm_dense_checkpoint", "sp24_gemm_dense_grouped_checkpoint", "sp24_moe_sort"}
