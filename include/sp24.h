@@ -649,12 +649,12 @@ typedef enum {
 
 /*
  * The weights' gradient from rows kept in 8 bits: D = A x B, A: M x K of type in = SP24_F16 or SP24_BF16 in either order (dZ or its transpose, K
- * the tokens), B: the K x N values that `codes` and `scale` stand for, each rounded to `in` (which is off by at most 2^-8 of the value for SP24_BF16, where
- * a code is off by half a step, 2^-8 of its block's largest value).  Binary32 sums.  D: M x N of type `in` or SP24_F32.  K may be any number, 0 included,
+ * the tokens), B: the K x N values that `codes` and `scale` stand for, each rounded to `in` (off by at most 2^-8 of the value for SP24_BF16, 2^-11 for SP24_F16, where
+ * a code is off by up to half a step: SP24_I8 1 / 254 of its block's largest value, SP24_F8 2^-4 of the value, or 2^-10 of the scale where the code is below 2^-6).  Binary32 sums.  D: M x N of type `in` or SP24_F32.  K may be any number, 0 included,
  * which gives zeros.  Rows of A must be 16-byte aligned; what lies between a row's end and the next 16-byte boundary may be read and is not used.  lda and N
  * below 2^21, else SP24_ERR_SHAPE.
- * workspace: device, 16-byte aligned, sp24_gemm_dense_checkpoint_workspace_bytes(M, N, K, 0) bytes: the restored rows of this one product (of more than a
- * few tokens), and partial products where few tiles have many (contents before the call are ignored, after it unspecified; calls sharing one must not overlap in time).
+ * workspace: device, 16-byte aligned, sp24_gemm_dense_checkpoint_workspace_bytes(M, N, K, 0) bytes: the restored rows of this one product (asked for, not
+ * used, for few tokens too), and partial products where few tiles have many (contents before the call are ignored, after it unspecified; calls sharing one must not overlap in time).
  */
 size_t sp24_gemm_dense_checkpoint_workspace_bytes(int64_t M, int64_t N, int64_t K, int grouped);
 sp24_status sp24_gemm_dense_checkpoint(const void* A, sp24_aorder order, const void* codes, const float* scale, void* D, int64_t M, int64_t N,
@@ -664,8 +664,9 @@ sp24_status sp24_gemm_dense_checkpoint(const void* A, sp24_aorder order, const v
 /*
  * sp24_gemm_dense_grouped with its second operand kept in 8 bits: D_e = A[:, segment e] x B[segment e, :].  `rows` NULL: row r of B is row r of
  * `codes`, which has `row_count` rows then (tokens == row_count).  Else row r of B is row rows[r] / topk of the `tokens` rows of codes, the rows of sorted
- * choices from the tokens' kept ones, and zeros where rows[r] is -1 (or names no token).  offsets as there, any N; orders of A, limits and workspace (K =
- * row_count, grouped = 1) as above.
+ * choices from the tokens' kept ones, and zeros where rows[r] is -1 (or names no token); such a row inside a segment takes part, as there: an infinity or NaN in
+ * its column of A makes NaN of a row of D.  offsets as there, any N; orders of A, limits and workspace (K = row_count, grouped = 1) as above: a restored
+ * row for every choice, not for every token.
  */
 sp24_status sp24_gemm_dense_grouped_checkpoint(const void* A, sp24_aorder order, const void* codes, const float* scale, const int32_t* rows, void* D,
                                                const int32_t* offsets, int experts, int64_t M, int64_t N, int64_t row_count, int64_t tokens,

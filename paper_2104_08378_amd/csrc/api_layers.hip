@@ -499,7 +499,8 @@ struct KeptProduct {
 };
 // Up to so many tokens, twice as many of segments, the product takes the codes itself.  In a graph, us: 512 x 512 from 64 5.5 -> 3.4, from 256 6.0 -> 5.2, from 512 6.8 and
 // 7.6; 4096 x 1024 from 64 8.0 -> 5.3, from 256 9.2 -> 7.8; 6328 x 2112 from 128 14.1 -> 13.0, but from 256 17.4 and 18.5; 2048 x 1000 from 400 9.8 and 11.4.  Eight
-// segments of 1024 x 1024 from 256 choices 9.3 -> 7.9, four from 512 9.3 and 10.2; 32 of 2048 x 1024, most of them empty, 28 and 33.
+// segments of 1024 x 1024 from 256 choices 9.3 -> 7.9, four from 512 9.3 and 10.2; 32 of 2048 x 1024 from 8 choices (row_count 128), most of them empty, 28 and 33.  The
+// rule goes by the tokens alone: many rows of weights from nearly so many, and many empty segments, are up to a sixth slower by it.
 constexpr int64_t kFewTokens = 256;
 static sp24_status gemm_kept(const KeptProduct& a, void* stream)
 {
