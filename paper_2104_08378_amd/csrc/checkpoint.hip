@@ -4,7 +4,7 @@
 //
 // Bound by memory: a 16-bit value costs 3 bytes one way and 3 the other.  Sixteen lanes hold a block, eight values each, so that its largest
 // magnitude takes four exchanges of neighbouring lanes and no LDS.  8192 x 4096 bf16 from HBM: kept in 22.0 us, 101 MB at 4.6 TB/s, had again in 22 (4.6), with GELU
-// 24; 16 x 8192 2.2, a launch.  (More rows a thread, two to eight, were 2 % faster to 20 % slower; workgroups of 512 level.)
+// 24; 16 x 8192 2.2, a launch.  From binary32, 4096 x 4096, 14 from the last-level cache.  (More rows a thread, two to eight, were 2 % faster to 20 % slower; workgroups of 512 level.)
 #include "kept.hpp"
 #include "launch.hpp"
 

@@ -9,8 +9,8 @@
 //
 // Bound by vector operations, two thirds of the time busy with them: an exponential of some 35 in binary64 for every logit, and for every choice the
 // reduction over the row's lanes and a search in the one that has it.  Few rows: a launch and one row's chain of them.  In a graph, us: 16 rows, four of 64 experts
-// 2.9; 8192 rows, six of 64 4.5, eight of 256 9.8, by logistic scores with bias out of four of eight groups 10.6 (1.4 is what their 8.9 MB take); 2048 rows of
-// 1024 10.0; the gradient of 8192 rows of 256 with that of the scores 9.0 (25 MB: 4.1).  (An exponential
+// 2.9; 8192 rows, six of 64 4.5, eight of 256 9.8, by logistic scores with bias out of four of eight groups 10.6 (1.4 is what their 8.9 MB take), six of 160
+// out of three of eight groups, which are no run of whole lanes, 13.3; 2048 rows of 1024 10.0; the gradient of 8192 rows of 256 with that of the scores 9.0 (25 MB: 4.1).  (An exponential
 // for arguments below 0 alone, of 25 operations in place of 37, changed none of it.)
 #include <algorithm>
 
